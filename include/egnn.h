@@ -487,6 +487,71 @@ int egnn_pack_rows(egnn_ctx* ctx, const float* x, int32_t n_rows_x, const int32_
 int egnn_unpack_rows(egnn_ctx* ctx, const void* buf, int32_t n_rows, int32_t half, float* x_full, int32_t first_row,
                      void* stream);
 
+/* ---- a trained block beside the message passing: group norm with SiLU, rows times the matrix of their group,
+ *      orthogonalised updates (the paper's layers end in linear maps and non-linearities on the embeddings, Fig. 2(a);
+ *      which norm, which grouping and which optimiser it leaves open) ----
+ * dtype: EGNN_F32, EGNN_F16 (IEEE half precision) or EGNN_BF16: the type of x, y, dx, dy and of the matrices W of the grouped
+ *   linear map.  Sums, statistics, gamma, beta, bias and the gradients of weights are fp32 whatever the dtype (partial sums over rows
+ *   fp64 where the comment of the kernel says so); results in fewer bits are rounded to nearest even once.
+ * *_stride: elements from one row to the next (>= the row's length), so that a plane of a larger tensor can be read and written in
+ *   place.  Rows of any alignment are taken; rows aligned to 16 bytes (or 8) are read in wider pieces.
+ * ws: 256-byte aligned, of the size its *_workspace_bytes call gives (host arithmetic on sizes alone); contents need not be kept
+ *   from one call to the next.
+ *
+ * egnn_group_norm: rows ptr[s] .. ptr[s+1] - 1 of segment s (a structure) and the channels / groups channels of a group are
+ *   normalised together: y = SiLU(gamma_c (x - mean) rstd + beta_c), rstd = 1 / sqrt(var + eps), var the mean squared distance
+ *   from the mean.  ptr (device, [n_segments + 1], from 0 to n_rows, never descending; out-of-range values are clamped to
+ *   0 .. n_rows, rows of no segment are left unwritten); NULL: one segment of all rows.  mean and rstd [n_segments][groups] are
+ *   outputs (0 for a segment without rows).  channels in 1..1024, groups divides channels.  y may be x (same stride).
+ * egnn_group_norm_backward: dx, dgamma [channels] and dbeta [channels] (all overwritten) from dy and what the forward call was
+ *   given and returned.  dx may be dy or x (same stride).
+ *
+ * egnn_group_rows: rows in groups.  key [n] (clamped to 0 .. n_groups - 1): with lmax = -1 row i goes to group key[i]; with lmax >= 0
+ *   atom i has (lmax + 1)^2 rows, row i (lmax + 1)^2 + l*l + l + m goes to group key[i] (lmax + 1) + l.  Groups are numbered
+ *   0 .. G - 1, G = n_groups (lmax < 0) or n_groups (lmax + 1).  perm [rows]: the rows group by group, ascending inside a group;
+ *   ptr [G + 1] (both device, int32).  n_groups in 1..1024.
+ * egnn_grouped_linear: y_r = W_g x_r + bias_g for every row r = perm[k], ptr[g] <= k < ptr[g+1].  W [n_groups][n_out][n_in] of the
+ *   dtype, bias [n_groups][n_out] fp32 or NULL; perm NULL: row k itself (rows already lie group by group).  Groups may be empty.
+ *   Values of ptr and perm outside 0 .. n_rows (- 1) are clamped; rows in no group are left unwritten.
+ * egnn_grouped_linear_backward: dx_r = W_g^T dy_r, dW_g = sum_r dy_r x_r^T (fp32), db_g = sum_r dy_r (fp32); each of dx, dW, db may
+ *   be NULL (not computed), all are overwritten (zeros for a group without rows).  x is read for dW only, W for dx only.
+ *
+ * egnn_orthogonalise: y_b = q(g_b) for each of batch matrices [rows][cols]: x = g / (|g|_F + 1e-7), then `steps` times
+ *   x <- 3.4445 x - 4.7750 (x x^T) x + 2.0315 (x x^T)^2 x (Newton-Schulz products with the coefficients published with the Muon
+ *   optimiser; they bring the singular values near 1, not to it).  steps in 1..32.  y may be g.
+ * egnn_muon_step: m' = beta m + g, u = g + beta m', W' = (1 - lr weight_decay) W - lr sqrt(max(1, rows / cols)) q(u), all fp32;
+ *   m_out may be m, W_out may be W. */
+#define EGNN_F32 0
+#define EGNN_F16 1
+#define EGNN_BF16 2
+int egnn_group_norm_workspace_bytes(const egnn_ctx* ctx, int64_t n_rows, int32_t n_segments, int32_t channels, int32_t groups,
+                                    size_t* bytes);
+int egnn_group_norm(egnn_ctx* ctx, int32_t dtype, const void* x, int64_t x_stride, int64_t n_rows, int32_t channels,
+                    int32_t groups, const int32_t* ptr, int32_t n_segments, const float* gamma, const float* beta, float eps,
+                    void* y, int64_t y_stride, float* mean, float* rstd, void* ws, size_t ws_bytes, void* stream);
+int egnn_group_norm_backward(egnn_ctx* ctx, int32_t dtype, const void* x, int64_t x_stride, const void* dy, int64_t dy_stride,
+                             const float* mean, const float* rstd, int64_t n_rows, int32_t channels, int32_t groups,
+                             const int32_t* ptr, int32_t n_segments, const float* gamma, const float* beta, void* dx,
+                             int64_t dx_stride, float* dgamma, float* dbeta, void* ws, size_t ws_bytes, void* stream);
+int egnn_group_rows_workspace_bytes(const egnn_ctx* ctx, int64_t n, int32_t n_groups, size_t* bytes);
+int egnn_group_rows(egnn_ctx* ctx, const int32_t* key, int64_t n, int32_t n_groups, int32_t lmax, int32_t* ptr, int32_t* perm,
+                    void* ws, size_t ws_bytes, void* stream);
+int egnn_grouped_linear_workspace_bytes(const egnn_ctx* ctx, int64_t n_rows, int32_t n_groups, int32_t n_in, int32_t n_out,
+                                        size_t* bytes);
+int egnn_grouped_linear(egnn_ctx* ctx, int32_t dtype, const void* x, int64_t x_stride, int64_t n_rows, int32_t n_in,
+                        int32_t n_out, const void* W, const float* bias, const int32_t* ptr, const int32_t* perm,
+                        int32_t n_groups, void* y, int64_t y_stride, void* stream);
+int egnn_grouped_linear_backward(egnn_ctx* ctx, int32_t dtype, const void* x, int64_t x_stride, const void* W, const void* dy,
+                                 int64_t dy_stride, int64_t n_rows, int32_t n_in, int32_t n_out, const int32_t* ptr,
+                                 const int32_t* perm, int32_t n_groups, void* dx, int64_t dx_stride, float* dW, float* db,
+                                 void* ws, size_t ws_bytes, void* stream);
+int egnn_orthogonalise_workspace_bytes(const egnn_ctx* ctx, int32_t batch, int32_t rows, int32_t cols, size_t* bytes);
+int egnn_orthogonalise(egnn_ctx* ctx, int32_t dtype, const void* g, int32_t batch, int32_t rows, int32_t cols, int32_t steps,
+                       void* y, void* ws, size_t ws_bytes, void* stream);
+int egnn_muon_step(egnn_ctx* ctx, const float* W, const float* g, const float* m, int32_t batch, int32_t rows, int32_t cols,
+                   float lr, float beta, float weight_decay, int32_t steps, float* W_out, float* m_out, void* ws,
+                   size_t ws_bytes, void* stream);
+
 /* ---- stage timing (measurement aid; follows the paper's protocol of timing the blocks of the forward
  *      pass separately, Sec. 4.4 / Fig. 6(c)) ----
  * egnn_timing_enable(ctx, max_calls > 0) creates HIP events; from then on every egnn_layer_forward /

@@ -33,7 +33,28 @@ SYMBOLS = [
     "egnn_layer_forward_save", "egnn_readout_hij_save", "egnn_layer_backward_saved", "egnn_readout_backward_saved",
     "egnn_radial_weights_static", "egnn_edge_pairs_workspace_bytes", "egnn_edge_pairs",
     "egnn_length_bins_workspace_bytes", "egnn_length_bins",
+    "egnn_group_norm_workspace_bytes", "egnn_group_norm", "egnn_group_norm_backward", "egnn_group_rows_workspace_bytes", "egnn_group_rows",
+    "egnn_grouped_linear_workspace_bytes", "egnn_grouped_linear", "egnn_grouped_linear_backward",
+    "egnn_orthogonalise_workspace_bytes", "egnn_orthogonalise", "egnn_muon_step",
 ]
+
+DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}   # EGNN_F32, EGNN_F16, EGNN_BF16
+# Argument types of the calls that are short enough for their marshalling to show: plain Python numbers are passed.
+# p pointer, i int32, l int64, f float, z size_t
+_SIGNATURES = {
+    "egnn_group_norm_workspace_bytes": "pliiip",
+    "egnn_group_norm": "piplliipippfplpppzp",
+    "egnn_group_norm_backward": "piplplppliipippplpppzp",
+    "egnn_group_rows_workspace_bytes": "plip",
+    "egnn_group_rows": "ppliipppzp",
+    "egnn_grouped_linear_workspace_bytes": "pliiip",
+    "egnn_grouped_linear": "piplliippppiplp",
+    "egnn_grouped_linear_backward": "piplpplliippiplpppzp",
+    "egnn_orthogonalise_workspace_bytes": "piiip",
+    "egnn_orthogonalise": "pipiiiippzp",
+    "egnn_muon_step": "ppppiiifffipppzp",
+}
+_LETTERS = {"p": C.c_void_p, "i": C.c_int32, "l": C.c_int64, "f": C.c_float, "z": C.c_size_t}
 
 
 class ModelDesc(C.Structure):
@@ -69,6 +90,8 @@ def load_library():
         lib.egnn_last_error.argtypes = [C.c_void_p]
         lib.egnn_destroy.restype = None
         lib.egnn_destroy.argtypes = [C.c_void_p]
+        for name, letters in _SIGNATURES.items():
+            getattr(lib, name).argtypes = [_LETTERS[c] for c in letters]
         _lib = lib
     return _lib
 
@@ -78,6 +101,25 @@ def _ptr(t):
         return C.c_void_p(0)
     assert t.is_cuda and t.is_contiguous(), "device-resident contiguous tensor required"
     return C.c_void_p(t.data_ptr())
+
+
+def _at(t, shape, dtype=torch.float32):
+    """Address of a contiguous device tensor of this shape and type; None for None."""
+    if t is None:
+        return None
+    if not (t.is_cuda and t.dtype == dtype and t.shape == shape and t.is_contiguous()):
+        raise ValueError(f"contiguous {dtype} device tensor of shape {tuple(shape)} required, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _rows(t, n, length, dtype):
+    """(address, row stride) of a device tensor of n rows of this length, contiguous inside a row."""
+    if not (t.is_cuda and t.dtype == dtype and t.dim() == 2 and t.shape[0] == n and t.shape[1] == length):
+        raise ValueError(f"{dtype} device tensor of {n} rows of {length} required, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    row, one = t.stride()
+    if one != 1 and length > 1 or row < length and n > 1:
+        raise ValueError(f"rows must be contiguous and must not overlap, not of strides {(row, one)}")
+    return t.data_ptr(), max(row, length)
 
 
 def _f3(a):
@@ -645,6 +687,116 @@ class Egnn:
             _ptr(grads["W_t"]), _ptr(grads["W_r1"]), _ptr(grads["W_r2"]), _ptr(grads["V"]), _ptr(ws),
             C.c_size_t(ws.numel()), _stream()))
         return dx, grads
+
+    # ---- a trained block beside the message passing: group norm with SiLU, grouped linear maps, orthogonalised updates
+    def _bytes(self, call, *sizes):
+        out = C.c_size_t()
+        self._check(call(self.ctx, *sizes, C.addressof(out)))
+        return out.value
+
+    def _room(self, ws, call, *sizes):
+        """(workspace to keep alive, address, bytes); allocated where the caller brings none."""
+        if ws is None:
+            ws = torch.empty(max(256, self._bytes(call, *sizes)), dtype=torch.uint8, device="cuda")
+        elif not (ws.is_cuda and ws.dtype == torch.uint8 and ws.is_contiguous()):
+            raise ValueError("the workspace must be a contiguous uint8 device tensor")
+        return ws, ws.data_ptr(), ws.numel()
+
+    @staticmethod
+    def _dtype(t):
+        if t.dtype not in DTYPES:
+            raise ValueError(f"float32, float16 or bfloat16 required, not {t.dtype}")
+        return DTYPES[t.dtype]
+
+    def egnn_group_norm_workspace_bytes(self, n_rows, n_segments, channels, groups):
+        return self._bytes(self.lib.egnn_group_norm_workspace_bytes, n_rows, n_segments, channels, groups)
+
+    def egnn_group_norm(self, x, groups, gamma, beta, ptr=None, eps=1e-5, y=None, mean=None, rstd=None, ws=None):
+        """y = SiLU(group norm of x) with x [n][channels] (rows may lie in a larger tensor); returns (y, mean, rstd)."""
+        code, (n, c), segments = self._dtype(x), x.shape, 1 if ptr is None else ptr.numel() - 1
+        y = torch.empty((n, c), dtype=x.dtype, device=x.device) if y is None else y
+        mean = torch.empty((segments, groups), dtype=torch.float32, device=x.device) if mean is None else mean
+        rstd = torch.empty((segments, groups), dtype=torch.float32, device=x.device) if rstd is None else rstd
+        ws, at, size = self._room(ws, self.lib.egnn_group_norm_workspace_bytes, n, segments, c, groups)
+        self._check(self.lib.egnn_group_norm(
+            self.ctx, code, *_rows(x, n, c, x.dtype), n, c, groups, _at(ptr, (segments + 1,), torch.int32), segments, _at(gamma, (c,)),
+            _at(beta, (c,)), eps, *_rows(y, n, c, x.dtype), _at(mean, (segments, groups)), _at(rstd, (segments, groups)), at, size,
+            _stream()))
+        return y, mean, rstd
+
+    def egnn_group_norm_backward(self, x, dy, mean, rstd, groups, gamma, beta, ptr=None, dx=None, dgamma=None, dbeta=None, ws=None):
+        """Adjoint of egnn_group_norm with the statistics it returned; returns (dx, dgamma, dbeta)."""
+        code, (n, c), segments = self._dtype(x), x.shape, 1 if ptr is None else ptr.numel() - 1
+        dx = torch.empty((n, c), dtype=x.dtype, device=x.device) if dx is None else dx
+        dgamma = torch.empty_like(gamma) if dgamma is None else dgamma
+        dbeta = torch.empty_like(beta) if dbeta is None else dbeta
+        ws, at, size = self._room(ws, self.lib.egnn_group_norm_workspace_bytes, n, segments, c, groups)
+        self._check(self.lib.egnn_group_norm_backward(
+            self.ctx, code, *_rows(x, n, c, x.dtype), *_rows(dy, n, c, x.dtype), _at(mean, (segments, groups)),
+            _at(rstd, (segments, groups)), n, c, groups, _at(ptr, (segments + 1,), torch.int32), segments, _at(gamma, (c,)), _at(beta, (c,)),
+            *_rows(dx, n, c, x.dtype), _at(dgamma, (c,)), _at(dbeta, (c,)), at, size, _stream()))
+        return dx, dgamma, dbeta
+
+    def egnn_group_rows_workspace_bytes(self, n, n_groups):
+        return self._bytes(self.lib.egnn_group_rows_workspace_bytes, n, n_groups)
+
+    def egnn_group_rows(self, key, n_groups, lmax=-1, ptr=None, perm=None, ws=None):
+        """Rows grouped by key (lmax < 0), or the (lmax + 1)^2 rows of every atom by (key, degree); returns (ptr, perm)."""
+        n, degrees = key.numel(), max(1, lmax + 1)
+        ptr = torch.empty(n_groups * degrees + 1, dtype=torch.int32, device=key.device) if ptr is None else ptr
+        perm = torch.empty(n * degrees * degrees, dtype=torch.int32, device=key.device) if perm is None else perm
+        ws, at, size = self._room(ws, self.lib.egnn_group_rows_workspace_bytes, n, n_groups)
+        self._check(self.lib.egnn_group_rows(
+            self.ctx, _at(key, (n,), torch.int32), n, n_groups, lmax, _at(ptr, (n_groups * degrees + 1,), torch.int32),
+            _at(perm, (n * degrees * degrees,), torch.int32), at, size, _stream()))
+        return ptr, perm
+
+    def egnn_grouped_linear_workspace_bytes(self, n_rows, n_groups, n_in, n_out):
+        return self._bytes(self.lib.egnn_grouped_linear_workspace_bytes, n_rows, n_groups, n_in, n_out)
+
+    def egnn_grouped_linear(self, x, W, ptr, perm=None, bias=None, y=None):
+        """y = W_g x + bias_g for the rows of every group; x [n][n_in], W [groups][n_out][n_in]."""
+        code, n, (groups, n_out, n_in) = self._dtype(x), x.shape[0], W.shape
+        y = torch.empty((n, n_out), dtype=x.dtype, device=x.device) if y is None else y
+        self._check(self.lib.egnn_grouped_linear(
+            self.ctx, code, *_rows(x, n, n_in, x.dtype), n, n_in, n_out, _at(W, W.shape, x.dtype), _at(bias, (groups, n_out)),
+            _at(ptr, (groups + 1,), torch.int32), _at(perm, (n,), torch.int32), groups, *_rows(y, n, n_out, x.dtype), _stream()))
+        return y
+
+    def egnn_grouped_linear_backward(self, x, W, dy, ptr, perm=None, dx=None, dW=None, db=None, ws=None):
+        """Adjoint of egnn_grouped_linear; returns (dx, dW, db), dW and db in fp32."""
+        code, n, (groups, n_out, n_in) = self._dtype(x), x.shape[0], W.shape
+        dx = torch.empty((n, n_in), dtype=x.dtype, device=x.device) if dx is None else dx
+        dW = torch.empty((groups, n_out, n_in), dtype=torch.float32, device=x.device) if dW is None else dW
+        db = torch.empty((groups, n_out), dtype=torch.float32, device=x.device) if db is None else db
+        ws, at, size = self._room(ws, self.lib.egnn_grouped_linear_workspace_bytes, n, groups, n_in, n_out)
+        self._check(self.lib.egnn_grouped_linear_backward(
+            self.ctx, code, *_rows(x, n, n_in, x.dtype), _at(W, W.shape, x.dtype), *_rows(dy, n, n_out, x.dtype), n, n_in, n_out,
+            _at(ptr, (groups + 1,), torch.int32), _at(perm, (n,), torch.int32), groups, *_rows(dx, n, n_in, x.dtype), _at(dW, W.shape),
+            _at(db, (groups, n_out)), at, size, _stream()))
+        return dx, dW, db
+
+    def egnn_orthogonalise_workspace_bytes(self, batch, rows, cols):
+        return self._bytes(self.lib.egnn_orthogonalise_workspace_bytes, batch, rows, cols)
+
+    def egnn_orthogonalise(self, g, steps=5, y=None, ws=None):
+        """Newton-Schulz products on each matrix of g [batch][rows][cols]."""
+        code, (batch, rows, cols) = self._dtype(g), g.shape
+        y = torch.empty_like(g) if y is None else y
+        ws, at, size = self._room(ws, self.lib.egnn_orthogonalise_workspace_bytes, batch, rows, cols)
+        self._check(self.lib.egnn_orthogonalise(self.ctx, code, _at(g, g.shape, g.dtype), batch, rows, cols, steps,
+                                                _at(y, g.shape, g.dtype), at, size, _stream()))
+        return y
+
+    def egnn_muon_step(self, W, g, momentum, lr, beta=0.95, weight_decay=0.0, steps=5, W_out=None, momentum_out=None, ws=None):
+        """One step of the optimiser for weights [batch][rows][cols]; in place unless outputs are given; returns (W, momentum)."""
+        batch, rows, cols = W.shape
+        W_out, momentum_out = W if W_out is None else W_out, momentum if momentum_out is None else momentum_out
+        ws, at, size = self._room(ws, self.lib.egnn_orthogonalise_workspace_bytes, batch, rows, cols)
+        self._check(self.lib.egnn_muon_step(
+            self.ctx, _at(W, W.shape), _at(g, W.shape), _at(momentum, W.shape), batch, rows, cols, lr, beta, weight_decay, steps,
+            _at(W_out, W.shape), _at(momentum_out, W.shape), at, size, _stream()))
+        return W_out, momentum_out
 
     # ---- stage timing
     def egnn_timing_enable(self, max_calls):

@@ -1,0 +1,491 @@
+// Group norm with SiLU over the rows of a structure (or of each of several), channels last, and its adjoint.
+//
+// Rows of one segment s (a structure) and the channels of one group g are normalised together:
+//   mean = sum x / n, var = sum (x - mean)^2 / n, rstd = 1 / sqrt(var + eps), n = rows of s times channels of g,
+//   xhat = (x - mean) rstd, z = gamma_c xhat + beta_c, y = z / (1 + exp(-z)).
+// Adjoint, with dz = dy sig (1 + z (1 - sig)), sig = 1 / (1 + exp(-z)):
+//   dgamma_c = sum_rows dz xhat, dbeta_c = sum_rows dz, dx = rstd (gamma_c dz - mean_g(gamma dz) - xhat mean_g(gamma dz xhat)).
+// Both directions are a pass that sums and a pass that writes, one launch each.  What bounds them is memory: x (and dy) are
+// read twice, because the sums of all rows of a segment come before its first result.
+//
+// The rows are cut into equal chunks, one workgroup each; segments are ragged and may be shorter or longer than a chunk.
+// A chunk c and a segment s that share rows own the slot c + s of the partial sums: walking along the rows either c or s
+// goes up by one, so no two pairs share a slot, the slots of a segment are contiguous, and their number is at most chunks +
+// segments.  The second pass adds the slots of its segments itself, in ascending order (no atomics).
+#include "row_types.h"
+
+namespace {
+
+constexpr int GN_CHUNKS = 512;        // two workgroups per compute unit; the second pass reads all partial sums of a segment
+constexpr int GN_CHUNK_BYTES = 16384; // a chunk holds at least this much of x: below it the launch is longer than the reading
+
+struct GnShape {
+  long n;               // rows
+  int C, G, S;          // channels, groups, segments
+  int chunks;
+  long rows;            // rows per chunk
+  const int* ptr;       // [S + 1] or NULL: one segment of all rows
+};
+
+__host__ __device__ inline long gn_clamp(long v, long n) { return v < 0 ? 0 : v > n ? n : v; }
+__device__ __forceinline__ long gn_begin(const GnShape& p, int s) { return p.ptr ? gn_clamp(p.ptr[s], p.n) : s ? p.n : 0; }
+
+// first segment that ends behind `row`
+__device__ __forceinline__ int gn_first_segment(const GnShape& p, long row) {
+  int lo = 0, hi = p.S;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (gn_begin(p, mid + 1) > row) hi = mid; else lo = mid + 1;
+  }
+  return lo;
+}
+
+// The sums are of x - x', x' the first value of the segment and group, and fp64: sum (x - x')^2 / n - (sum (x - x') / n)^2 then loses
+// nothing to a mean far from zero, and a first value far from all others costs n 2^-53.
+// ---- forward ---------------------------------------------------------------------------------------------------------
+template <class T, int V>
+__global__ __launch_bounds__(1024) void gn_sums_kernel(GnShape p, const T* x, long x_stride, double2* part, float* first_of) {
+  extern __shared__ double2 smem[];   // [row slots][C]
+  const int L = p.C / V, slots = blockDim.x / L, l = threadIdx.x % L, rr = threadIdx.x / L;
+  const long r0 = (long)blockIdx.x * p.rows, r1 = min(r0 + p.rows, p.n);
+  const int size = p.C / p.G;
+  for (int s = gn_first_segment(p, r0); s < p.S; ++s) {
+    const long b = max(gn_begin(p, s), r0), e = min(gn_begin(p, s + 1), r1);
+    if (gn_begin(p, s) >= r1) break;
+    if (b >= e) continue;
+    double a1[V], a2[V], from[V];
+    const T* first = x + gn_begin(p, s) * x_stride;
+#pragma unroll
+    for (int q = 0; q < V; ++q) {
+      a1[q] = a2[q] = 0.0;
+      from[q] = (double)(float)first[rr < slots ? (l * V + q) / size * size : 0];
+    }
+    if (rr < slots) {
+#pragma unroll 4
+      for (long r = b + rr; r < e; r += slots) {
+        float v[V];
+        rt_load<T, V>(x + r * x_stride + l * V, v);
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+          const double d = (double)v[q] - from[q];
+          a1[q] += d;
+          a2[q] += d * d;
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < V; ++q) smem[rr * p.C + l * V + q] = make_double2(a1[q], a2[q]);
+    }
+    __syncthreads();
+    for (int g = threadIdx.x; g < p.G; g += blockDim.x) {
+      double t1 = 0.0, t2 = 0.0;
+      for (int r = 0; r < slots; ++r)
+        for (int c = g * size; c < (g + 1) * size; ++c) {
+          t1 += smem[r * p.C + c].x;
+          t2 += smem[r * p.C + c].y;
+        }
+      part[(size_t)(blockIdx.x + s) * p.G + g] = make_double2(t1, t2);
+      if (b == gn_begin(p, s)) first_of[(size_t)s * p.G + g] = (float)first[g * size];   // (y may be x: kept apart)
+    }
+    __syncthreads();
+  }
+}
+
+// sums of the slots of segment s, to out[G] in LDS; scratch [blockDim]
+__device__ __forceinline__ void gn_segment_sums(const GnShape& p, const double2* part, int s, double2* out, double2* scratch) {
+  const long b = gn_begin(p, s), e = gn_begin(p, s + 1);
+  const int c0 = (int)(b / p.rows), c1 = (int)((e - 1) / p.rows);
+  const int per = max(1, (int)blockDim.x / p.G), k = threadIdx.x / p.G;
+  for (int g0 = 0; g0 < p.G; g0 += blockDim.x) {
+    const int g = g0 + threadIdx.x % p.G;
+    double2 t = make_double2(0.0, 0.0);
+    if (k < per && g < p.G)
+      for (int c = c0 + k; c <= c1; c += per) {
+        const double2 v = part[(size_t)(c + s) * p.G + g];
+        t.x += v.x;
+        t.y += v.y;
+      }
+    scratch[threadIdx.x] = t;
+    __syncthreads();
+    if (k == 0 && g < p.G) {
+      for (int j = 1; j < per; ++j) {
+        t.x += scratch[j * p.G + threadIdx.x].x;
+        t.y += scratch[j * p.G + threadIdx.x].y;
+      }
+      out[g] = t;
+    }
+    __syncthreads();
+  }
+}
+
+__device__ __forceinline__ float gn_sigmoid(float z) { return 1.0f / (1.0f + __expf(-z)); }
+
+template <class T, int V>
+__global__ __launch_bounds__(1024) void gn_write_kernel(GnShape p, const T* x, long x_stride, const float* gamma, const float* beta,
+                                                        float eps, T* y, long y_stride, float* mean, float* rstd,
+                                                        const double2* part, const float* first) {
+  __shared__ double2 sums[1024], scratch[1024];
+  __shared__ float s_mean[1024], s_rstd[1024];
+  const int L = p.C / V, slots = blockDim.x / L, l = threadIdx.x % L, rr = threadIdx.x / L;
+  const long r0 = (long)blockIdx.x * p.rows, r1 = min(r0 + p.rows, p.n);
+  const int size = p.C / p.G;
+  // segments without rows: the first workgroup writes their zeros
+  if (blockIdx.x == 0)
+    for (int s = threadIdx.x; s < p.S; s += blockDim.x)
+      if (gn_begin(p, s) >= gn_begin(p, s + 1))
+        for (int g = 0; g < p.G; ++g) mean[(size_t)s * p.G + g] = rstd[(size_t)s * p.G + g] = 0.0f;
+  float ga[V], be[V];
+#pragma unroll
+  for (int q = 0; q < V; ++q) {
+    ga[q] = gamma[l * V + q];
+    be[q] = beta[l * V + q];
+  }
+  for (int s = gn_first_segment(p, r0); s < p.S; ++s) {
+    const long sb = gn_begin(p, s), se = gn_begin(p, s + 1);
+    const long b = max(sb, r0), e = min(se, r1);
+    if (sb >= r1) break;
+    if (b >= e) continue;
+    gn_segment_sums(p, part, s, sums, scratch);
+    for (int g = threadIdx.x; g < p.G; g += blockDim.x) {
+      const double n = (double)(se - sb) * size, mu = sums[g].x / n;
+      const double var = sums[g].y / n - mu * mu;
+      s_mean[g] = (float)((double)first[(size_t)s * p.G + g] + mu);
+      s_rstd[g] = (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)eps));   // (a NaN stays one)
+      if (b == sb) {
+        mean[(size_t)s * p.G + g] = s_mean[g];
+        rstd[(size_t)s * p.G + g] = s_rstd[g];
+      }
+    }
+    __syncthreads();
+    if (rr < slots) {
+      float mu[V], rs[V];
+#pragma unroll
+      for (int q = 0; q < V; ++q) {
+        const int g = (l * V + q) / size;
+        mu[q] = s_mean[g];
+        rs[q] = s_rstd[g];
+      }
+      for (long r = b + rr; r < e; r += slots) {
+        float v[V];
+        rt_load<T, V>(x + r * x_stride + l * V, v);
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+          const float z = (v[q] - mu[q]) * rs[q] * ga[q] + be[q];
+          v[q] = z * gn_sigmoid(z);
+        }
+        rt_store<T, V>(y + r * y_stride + l * V, v);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// ---- adjoint ---------------------------------------------------------------------------------------------------------
+struct GnAdjoint {
+  const float *mean, *rstd, *gamma, *beta;
+};
+
+template <class T, int V>
+__global__ __launch_bounds__(1024) void gn_adjoint_sums_kernel(GnShape p, GnAdjoint w, const T* x, long x_stride, const T* dy,
+                                                               long dy_stride, double2* part, float2* channel_part) {
+  extern __shared__ float2 srow[];    // [row slots][C], then [C] totals of the chunk
+  const int L = p.C / V, slots = blockDim.x / L, l = threadIdx.x % L, rr = threadIdx.x / L;
+  float2* total = srow + (size_t)slots * p.C;
+  const long r0 = (long)blockIdx.x * p.rows, r1 = min(r0 + p.rows, p.n);
+  const int size = p.C / p.G;
+  float ga[V], be[V];
+#pragma unroll
+  for (int q = 0; q < V; ++q) {
+    ga[q] = w.gamma[l * V + q];
+    be[q] = w.beta[l * V + q];
+  }
+  for (int c = threadIdx.x; c < p.C; c += blockDim.x) total[c] = make_float2(0.0f, 0.0f);
+  for (int s = gn_first_segment(p, r0); s < p.S; ++s) {
+    const long b = max(gn_begin(p, s), r0), e = min(gn_begin(p, s + 1), r1);
+    if (gn_begin(p, s) >= r1) break;
+    if (b >= e) continue;
+    if (rr < slots) {
+      float mu[V], rs[V], a1[V], a2[V];
+#pragma unroll
+      for (int q = 0; q < V; ++q) {
+        const size_t at = (size_t)s * p.G + (l * V + q) / size;
+        mu[q] = w.mean[at];
+        rs[q] = w.rstd[at];
+        a1[q] = a2[q] = 0.0f;
+      }
+      for (long r = b + rr; r < e; r += slots) {
+        float v[V], d[V];
+        rt_load<T, V>(x + r * x_stride + l * V, v);
+        rt_load<T, V>(dy + r * dy_stride + l * V, d);
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+          const float h = (v[q] - mu[q]) * rs[q], z = h * ga[q] + be[q], sig = gn_sigmoid(z);
+          const float dz = d[q] * sig * (1.0f + z * (1.0f - sig));
+          a1[q] += dz;
+          a2[q] += dz * h;
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < V; ++q) srow[rr * p.C + l * V + q] = make_float2(a1[q], a2[q]);
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.C; c += blockDim.x) {
+      float2 t = srow[c];
+      for (int r = 1; r < slots; ++r) {
+        t.x += srow[r * p.C + c].x;
+        t.y += srow[r * p.C + c].y;
+      }
+      srow[c] = t;
+      total[c].x += t.x;
+      total[c].y += t.y;
+    }
+    __syncthreads();
+    for (int g = threadIdx.x; g < p.G; g += blockDim.x) {
+      double t1 = 0.0, t2 = 0.0;
+      for (int c = g * size; c < (g + 1) * size; ++c) {
+        t1 += (double)w.gamma[c] * srow[c].x;
+        t2 += (double)w.gamma[c] * srow[c].y;
+      }
+      part[(size_t)(blockIdx.x + s) * p.G + g] = make_double2(t1, t2);
+    }
+    __syncthreads();
+  }
+  for (int c = threadIdx.x; c < p.C; c += blockDim.x) channel_part[(size_t)blockIdx.x * p.C + c] = total[c];
+}
+
+template <class T, int V>
+__global__ __launch_bounds__(1024) void gn_adjoint_write_kernel(GnShape p, GnAdjoint w, const T* x, long x_stride, const T* dy,
+                                                                long dy_stride, T* dx, long dx_stride, float* dgamma,
+                                                                float* dbeta, const double2* part, const float2* channel_part) {
+  __shared__ double2 sums[1024], scratch[1024];
+  if ((int)blockIdx.x >= p.chunks) {   // the last workgroups add the channels' sums over the chunks, 16 channels each
+    const int c = ((int)blockIdx.x - p.chunks) * 16 + threadIdx.x % 16, per = blockDim.x / 16;
+    double2 t = make_double2(0.0, 0.0);
+    if (c < p.C)
+      for (int k = threadIdx.x / 16; k < p.chunks; k += per) {
+        const float2 v = channel_part[(size_t)k * p.C + c];
+        t.x += v.x;
+        t.y += v.y;
+      }
+    scratch[threadIdx.x] = t;
+    __syncthreads();
+    if (threadIdx.x < 16 && c < p.C) {
+      for (int j = 1; j < per; ++j) {
+        t.x += scratch[j * 16 + threadIdx.x].x;
+        t.y += scratch[j * 16 + threadIdx.x].y;
+      }
+      dbeta[c] = (float)t.x;
+      dgamma[c] = (float)t.y;
+    }
+    return;
+  }
+  const int L = p.C / V, slots = blockDim.x / L, l = threadIdx.x % L, rr = threadIdx.x / L;
+  const long r0 = (long)blockIdx.x * p.rows, r1 = min(r0 + p.rows, p.n);
+  const int size = p.C / p.G;
+  float ga[V], be[V];
+#pragma unroll
+  for (int q = 0; q < V; ++q) {
+    ga[q] = w.gamma[l * V + q];
+    be[q] = w.beta[l * V + q];
+  }
+  for (int s = gn_first_segment(p, r0); s < p.S; ++s) {
+    const long sb = gn_begin(p, s), se = gn_begin(p, s + 1);
+    const long b = max(sb, r0), e = min(se, r1);
+    if (sb >= r1) break;
+    if (b >= e) continue;
+    gn_segment_sums(p, part, s, sums, scratch);
+    if (rr < slots) {
+      float mu[V], rs[V], m1[V], m2[V];
+      const double inv = 1.0 / ((double)(se - sb) * size);
+#pragma unroll
+      for (int q = 0; q < V; ++q) {
+        const int g = (l * V + q) / size;
+        const size_t at = (size_t)s * p.G + g;
+        mu[q] = w.mean[at];
+        rs[q] = w.rstd[at];
+        m1[q] = (float)(sums[g].x * inv);
+        m2[q] = (float)(sums[g].y * inv);
+      }
+      for (long r = b + rr; r < e; r += slots) {
+        float v[V], d[V];
+        rt_load<T, V>(x + r * x_stride + l * V, v);
+        rt_load<T, V>(dy + r * dy_stride + l * V, d);
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+          const float h = (v[q] - mu[q]) * rs[q], z = h * ga[q] + be[q], sig = gn_sigmoid(z);
+          const float dz = d[q] * sig * (1.0f + z * (1.0f - sig));
+          v[q] = rs[q] * (ga[q] * dz - m1[q] - h * m2[q]);
+        }
+        rt_store<T, V>(dx + r * dx_stride + l * V, v);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+__global__ void gn_no_rows_kernel(float* a, long na, float* b, long nb) {
+  for (long i = threadIdx.x; i < na; i += blockDim.x) a[i] = 0.0f;
+  for (long i = threadIdx.x; i < nb; i += blockDim.x) b[i] = 0.0f;
+}
+
+size_t gn_align(size_t n) { return (n + 255) & ~(size_t)255; }
+
+GnShape gn_shape(int64_t n, int32_t C, int32_t G, int32_t S, const int32_t* ptr, int element) {
+  GnShape p;
+  p.n = n; p.C = C; p.G = G; p.S = S; p.ptr = ptr;
+  const long least = (GN_CHUNK_BYTES + (long)C * element - 1) / ((long)C * element);
+  p.rows = (n + GN_CHUNKS - 1) / GN_CHUNKS;
+  if (p.rows < least) p.rows = least;
+  p.chunks = (int)((n + p.rows - 1) / p.rows);
+  return p;
+}
+
+// partial sums per slot, channel sums per chunk (element = 4: the most chunks any type gives)
+size_t gn_part_bytes(const GnShape& p) { return gn_align((size_t)(p.chunks + p.S) * p.G * sizeof(double2)); }
+size_t gn_first_bytes(const GnShape& p) { return gn_align((size_t)p.S * p.G * sizeof(float)); }
+size_t gn_channel_bytes(const GnShape& p) { return gn_align((size_t)p.chunks * p.C * sizeof(float2)); }
+
+int gn_check(egnn_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32_t C, int32_t G, const int32_t* ptr, int32_t S) {
+  const std::string at(who);
+  if (!rt_size(dtype)) return egnn_fail(ctx, EGNN_EINVAL, at + ": dtype must be EGNN_F32, EGNN_F16 or EGNN_BF16");
+  if (n < 0 || n > 0x7fffffff) return egnn_fail(ctx, EGNN_EINVAL, at + ": n_rows must be in 0..2^31-1");
+  if (C < 1 || C > 1024) return egnn_fail(ctx, EGNN_EINVAL, at + ": channels must be in 1..1024");
+  if (G < 1 || C % G) return egnn_fail(ctx, EGNN_EINVAL, at + ": groups must divide the channels");
+  if (S < 1 || (!ptr && S != 1)) return egnn_fail(ctx, EGNN_EINVAL, at + ": n_segments must be at least 1, and 1 without ptr");
+  return EGNN_OK;
+}
+
+// vector width for which all rows are aligned
+template <class T>
+int gn_width(int32_t C, std::initializer_list<const void*> at, std::initializer_list<int64_t> strides) {
+  for (int v = 16 / (int)sizeof(T); v > 1; v /= 2) {
+    if (v == 2) continue;
+    bool fits = C % v == 0;
+    for (const void* a : at) fits = fits && (uintptr_t)a % (v * sizeof(T)) == 0;
+    for (int64_t s : strides) fits = fits && s % v == 0;
+    if (fits) return v;
+  }
+  return 1;
+}
+
+struct GnLaunch { int threads, slots; };
+GnLaunch gn_launch(int C, int V) {
+  const int L = C / V, threads = L <= 256 ? 256 : 1024;
+  return {threads, threads / L};
+}
+
+template <class T, int V>
+int gn_forward(egnn_ctx* ctx, const GnShape& p, const void* x, int64_t xs, const float* gamma, const float* beta, float eps, void* y,
+               int64_t ys, float* mean, float* rstd, void* ws, hipStream_t st) {
+  const GnLaunch at = gn_launch(p.C, V);
+  double2* part = (double2*)ws;
+  float* first = (float*)((char*)ws + gn_part_bytes(p));
+  hipLaunchKernelGGL((gn_sums_kernel<T, V>), dim3(p.chunks), dim3(at.threads), (size_t)at.slots * p.C * sizeof(double2), st, p,
+                     (const T*)x, (long)xs, part, first);
+  hipLaunchKernelGGL((gn_write_kernel<T, V>), dim3(p.chunks), dim3(at.threads), 0, st, p, (const T*)x, (long)xs, gamma, beta, eps,
+                     (T*)y, (long)ys, mean, rstd, (const double2*)part, (const float*)first);
+  EGNN_LAUNCH_CHECK(ctx, "group_norm");
+  return EGNN_OK;
+}
+
+template <class T, int V>
+int gn_backward(egnn_ctx* ctx, const GnShape& p, const GnAdjoint& w, const void* x, int64_t xs, const void* dy, int64_t dys, void* dx,
+                int64_t dxs, float* dgamma, float* dbeta, void* ws, hipStream_t st) {
+  const GnLaunch at = gn_launch(p.C, V);
+  double2* part = (double2*)ws;
+  float2* channel_part = (float2*)((char*)ws + gn_part_bytes(p));
+  hipLaunchKernelGGL((gn_adjoint_sums_kernel<T, V>), dim3(p.chunks), dim3(at.threads), (size_t)(at.slots + 1) * p.C * sizeof(float2),
+                     st, p, w, (const T*)x, (long)xs, (const T*)dy, (long)dys, part, channel_part);
+  hipLaunchKernelGGL((gn_adjoint_write_kernel<T, V>), dim3(p.chunks + (p.C + 15) / 16), dim3(at.threads), 0, st, p, w, (const T*)x,
+                     (long)xs, (const T*)dy, (long)dys, (T*)dx, (long)dxs, dgamma, dbeta, (const double2*)part,
+                     (const float2*)channel_part);
+  EGNN_LAUNCH_CHECK(ctx, "group_norm_backward");
+  return EGNN_OK;
+}
+
+}  // namespace
+
+extern "C" int egnn_group_norm_workspace_bytes(const egnn_ctx* ctx, int64_t n_rows, int32_t n_segments, int32_t channels,
+                                               int32_t groups, size_t* bytes) {
+  if (!ctx || !bytes || n_rows < 0 || n_rows > 0x7fffffff || n_segments < 1 || channels < 1 || channels > 1024 || groups < 1 ||
+      channels % groups)
+    return egnn_fail(const_cast<egnn_ctx*>(ctx), EGNN_EINVAL, "group_norm_workspace_bytes: bad argument");
+  const GnShape p = gn_shape(n_rows, channels, groups, n_segments, nullptr, 4);
+  const size_t forward = gn_part_bytes(p) + gn_first_bytes(p), backward = gn_part_bytes(p) + gn_channel_bytes(p);
+  *bytes = forward > backward ? forward : backward;
+  return EGNN_OK;
+}
+
+extern "C" int egnn_group_norm(egnn_ctx* ctx, int32_t dtype, const void* x, int64_t x_stride, int64_t n_rows, int32_t channels,
+                               int32_t groups, const int32_t* ptr, int32_t n_segments, const float* gamma, const float* beta,
+                               float eps, void* y, int64_t y_stride, float* mean, float* rstd, void* ws, size_t ws_bytes,
+                               void* stream) {
+  if (!ctx) return EGNN_EINVAL;
+  if (int rc = gn_check(ctx, "group_norm", dtype, n_rows, channels, groups, ptr, n_segments)) return rc;
+  if (!gamma || !beta || !mean || !rstd || (n_rows > 0 && (!x || !y)))
+    return egnn_fail(ctx, EGNN_EINVAL, "group_norm: null pointer");
+  if (x_stride < channels || y_stride < channels) return egnn_fail(ctx, EGNN_EINVAL, "group_norm: a row stride below the channels");
+  if (!(eps > 0.0f)) return egnn_fail(ctx, EGNN_EINVAL, "group_norm: eps must be > 0");
+  hipStream_t st = (hipStream_t)stream;
+  const GnShape p = gn_shape(n_rows, channels, groups, n_segments, ptr, rt_size(dtype));
+  if (n_rows == 0) {
+    const long k = (long)n_segments * groups;
+    hipLaunchKernelGGL(gn_no_rows_kernel, dim3(1), dim3(256), 0, st, mean, k, rstd, k);
+    EGNN_LAUNCH_CHECK(ctx, "group_norm");
+    return EGNN_OK;
+  }
+  if (!ws || (uintptr_t)ws % 256 || ws_bytes < gn_part_bytes(p) + gn_first_bytes(p))
+    return egnn_fail(ctx, EGNN_EWS, "group_norm: workspace too small or not 256-byte aligned");
+#define GN_CALL(T, V) return gn_forward<T, V>(ctx, p, x, x_stride, gamma, beta, eps, y, y_stride, mean, rstd, ws, st)
+  if (dtype == EGNN_F32) {
+    if (gn_width<float>(channels, {x, y}, {x_stride, y_stride}) == 4) GN_CALL(float, 4);
+    GN_CALL(float, 1);
+  }
+  const int v = gn_width<_Float16>(channels, {x, y}, {x_stride, y_stride});
+  if (dtype == EGNN_F16) {
+    if (v == 8) GN_CALL(_Float16, 8);
+    if (v == 4) GN_CALL(_Float16, 4);
+    GN_CALL(_Float16, 1);
+  }
+  if (v == 8) GN_CALL(__bf16, 8);
+  if (v == 4) GN_CALL(__bf16, 4);
+  GN_CALL(__bf16, 1);
+#undef GN_CALL
+}
+
+extern "C" int egnn_group_norm_backward(egnn_ctx* ctx, int32_t dtype, const void* x, int64_t x_stride, const void* dy,
+                                        int64_t dy_stride, const float* mean, const float* rstd, int64_t n_rows, int32_t channels,
+                                        int32_t groups, const int32_t* ptr, int32_t n_segments, const float* gamma,
+                                        const float* beta, void* dx, int64_t dx_stride, float* dgamma, float* dbeta, void* ws,
+                                        size_t ws_bytes, void* stream) {
+  if (!ctx) return EGNN_EINVAL;
+  if (int rc = gn_check(ctx, "group_norm_backward", dtype, n_rows, channels, groups, ptr, n_segments)) return rc;
+  if (!gamma || !beta || !mean || !rstd || !dgamma || !dbeta || (n_rows > 0 && (!x || !dy || !dx)))
+    return egnn_fail(ctx, EGNN_EINVAL, "group_norm_backward: null pointer");
+  if (x_stride < channels || dy_stride < channels || dx_stride < channels)
+    return egnn_fail(ctx, EGNN_EINVAL, "group_norm_backward: a row stride below the channels");
+  hipStream_t st = (hipStream_t)stream;
+  const GnShape p = gn_shape(n_rows, channels, groups, n_segments, ptr, rt_size(dtype));
+  if (n_rows == 0) {
+    hipLaunchKernelGGL(gn_no_rows_kernel, dim3(1), dim3(256), 0, st, dgamma, (long)channels, dbeta, (long)channels);
+    EGNN_LAUNCH_CHECK(ctx, "group_norm_backward");
+    return EGNN_OK;
+  }
+  if (!ws || (uintptr_t)ws % 256 || ws_bytes < gn_part_bytes(p) + gn_channel_bytes(p))
+    return egnn_fail(ctx, EGNN_EWS, "group_norm_backward: workspace too small or not 256-byte aligned");
+  const GnAdjoint w{mean, rstd, gamma, beta};
+#define GN_CALL(T, V) return gn_backward<T, V>(ctx, p, w, x, x_stride, dy, dy_stride, dx, dx_stride, dgamma, dbeta, ws, st)
+  if (dtype == EGNN_F32) {
+    if (gn_width<float>(channels, {x, dy, dx}, {x_stride, dy_stride, dx_stride}) == 4) GN_CALL(float, 4);
+    GN_CALL(float, 1);
+  }
+  const int v = gn_width<_Float16>(channels, {x, dy, dx}, {x_stride, dy_stride, dx_stride});
+  if (dtype == EGNN_F16) {
+    if (v == 8) GN_CALL(_Float16, 8);
+    if (v == 4) GN_CALL(_Float16, 4);
+    GN_CALL(_Float16, 1);
+  }
+  if (v == 8) GN_CALL(__bf16, 8);
+  if (v == 4) GN_CALL(__bf16, 4);
+  GN_CALL(__bf16, 1);
+#undef GN_CALL
+}
