@@ -25,7 +25,6 @@ constexpr int OU_PARTS = 512;       // partial sums of squares per matrix, at mo
 constexpr int OU_ONE_PIECE = 256;
 
 typedef _Float16 ou_h8 __attribute__((ext_vector_type(8)));
-typedef _Float16 ou_h4 __attribute__((ext_vector_type(4)));
 typedef float ou_f16v __attribute__((ext_vector_type(16)));
 
 struct OuShape {
@@ -124,7 +123,7 @@ __global__ __launch_bounds__(256) void ou_pieces_kernel(OuShape p, OuInput<T> in
 enum OuProduct { OU_GRAM, OU_POLY, OU_UPDATE, OU_LAST };
 
 template <class T>
-struct OuOut { T* y; const float* W; float keep, scale; };   // of the last product: y = q, or keep W - scale q
+struct OuOut { T* y; const float* W; float keep, scale; bool eights; };   // y = q, or keep W - scale q; rows of y in aligned eights
 
 struct OuOperands {
   const _Float16 *A, *B;   // per matrix [P pieces][I][K], [P pieces][J][K]; x^T always has two pieces
@@ -134,16 +133,6 @@ struct OuOperands {
 
 typedef const __attribute__((address_space(1))) void* ou_gp;
 typedef __attribute__((address_space(3))) void* ou_lp;
-
-// 4 x 4 halves across a quad of lanes: lane q holds column q of rows 0..3, and gets row q
-__device__ __forceinline__ uint2 ou_turn(uint2 v, int lane) {
-  const uint32_t pa = __builtin_amdgcn_mov_dpp(v.x, 0xB1, 0xf, 0xf, true), pb = __builtin_amdgcn_mov_dpp(v.y, 0xB1, 0xf, 0xf, true);
-  const bool odd = lane & 1, upper = lane & 2;
-  const uint32_t a = odd ? __builtin_amdgcn_perm(v.x, pa, 0x07060302) : __builtin_amdgcn_perm(pa, v.x, 0x05040100);
-  const uint32_t b = odd ? __builtin_amdgcn_perm(v.y, pb, 0x07060302) : __builtin_amdgcn_perm(pb, v.y, 0x05040100);
-  const uint32_t qa = __builtin_amdgcn_mov_dpp(a, 0x4E, 0xf, 0xf, true), qb = __builtin_amdgcn_mov_dpp(b, 0x4E, 0xf, 0xf, true);
-  return upper ? make_uint2(qb, b) : make_uint2(a, qa);
-}
 
 // waits until at most N loads of this wave are under way (loads return in order), then for the other waves
 template <int N>
@@ -249,324 +238,472 @@ __global__ __launch_bounds__(256) void ou_product_kernel(OuShape p, OuOperands o
   }
   ou_loads_then_barrier<0>();      // (no load to LDS outlives the workgroup)
 
-  // a lane holds column j = lane & 31 of its blocks and four times four neighbouring rows i
+  // Results go through LDS, so that whole lines are read and written: a lane holds column j = lane & 31 of its blocks and four times
+  // four neighbouring rows i; row j of the tile in LDS, its pieces of four values exchanged by j.
   constexpr float unscale = WHAT == OU_GRAM ? 1.0f / (OU_SX * OU_SX) : WHAT == OU_POLY ? 1.0f / (OU_SG * OU_SG) : 1.0f / (OU_SP * OU_SX);
   constexpr float scale = WHAT == OU_GRAM ? OU_SG : WHAT == OU_POLY ? OU_SP : OU_SX;
-  const size_t plane_c = (size_t)o.I * o.J;
+  constexpr int SLOTS = TILE / 4;
+  float4* tile = (float4*)smem;                      // [j][SLOTS]
+  auto slot = [](int j, int i4) { return j * SLOTS + (i4 ^ (j & (SLOTS - 1))); };
 #pragma unroll
   for (int x = 0; x < B; ++x)
 #pragma unroll
     for (int y = 0; y < B; ++y)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int i = i0 + wi + 32 * x + 8 * r + 4 * hh, j = j0 + wj + 32 * y + r32;
-        float v[4];
+      for (int r = 0; r < 4; ++r)
+        tile[slot(wj + 32 * y + r32, (wi + 32 * x + 8 * r + 4 * hh) >> 2)] =
+            make_float4(acc[x][y][4 * r], acc[x][y][4 * r + 1], acc[x][y][4 * r + 2], acc[x][y][4 * r + 3]);
+  __syncthreads();
+  const size_t plane_c = (size_t)o.I * o.J;
+  constexpr int ACROSS = TILE / 8;                   // threads along a row, eight values each
+  for (int e = tid; e < TILE * ACROSS; e += 256) {
+    const int jl = e / ACROSS, il = (e % ACROSS) * 8, i = i0 + il, j = j0 + jl;
+    if (i >= o.I || j >= o.J) continue;
+    const float4 lo4 = tile[slot(jl, il >> 2)], hi4 = tile[slot(jl, (il >> 2) + 1)];
+    float v[8] = {lo4.x, lo4.y, lo4.z, lo4.w, hi4.x, hi4.y, hi4.z, hi4.w};
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = acc[x][y][4 * r + q] * unscale;
-        if (STEP && P == 1 && i < o.I && j < o.J) {
-          const _Float16* old = Bm + (size_t)j * o.I + i;
-          const ou_h4 xh = *(const ou_h4*)old, xl = *(const ou_h4*)(old + plane_b);
+    for (int q = 0; q < 8; ++q) v[q] *= unscale;
+    const size_t at = (size_t)j * o.I + i;
+    if (WHAT == OU_POLY || (STEP && P == 1)) {       // + b g, or + a x
+      const _Float16* old = (STEP ? Bm : A) + at;
+      const ou_h8 oh = *(const ou_h8*)old;
+      ou_h8 ol = {};
+      if (PB == 2) ol = *(const ou_h8*)(old + plane_c);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) v[q] += OU_A * (((float)xh[q] + (float)xl[q]) * (1.0f / OU_SX));
-        }
-        if (WHAT == OU_LAST) {
-          const int n = p.n, m = p.m;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            if (i + q >= n || j >= m) continue;
-            const size_t at = z * n * m + (p.tall ? (size_t)j * n + i + q : (size_t)(i + q) * m + j);
-            out.y[at] = (T)(out.W ? out.keep * out.W[at] - out.scale * v[q] : v[q]);
-          }
-          continue;
-        }
-        if (i >= o.I || j >= o.J) continue;           // (a tile of 128 over sides that are multiples of 64: whole quads of lanes)
-        const size_t at = (size_t)j * o.I + i;
-        if (WHAT == OU_POLY) {
-          const _Float16* g = A + at;
-          ou_h4 gh = *(const ou_h4*)g, gl;
-          if (P == 2) gl = *(const ou_h4*)(g + plane_a);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const float gv = ((float)gh[q] + (P == 2 ? (float)gl[q] : 0.0f)) * (1.0f / OU_SG);
-            v[q] = OU_C * v[q] + OU_B * gv + (P == 2 && i + q == j && j < p.n ? OU_A : 0.0f);
-          }
-        }
-        ou_h4 hi, lo;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          _Float16 h, l;
-          ou_cut(v[q] * scale, h, l);
-          hi[q] = h; lo[q] = l;
-        }
-        _Float16* c = o.C + z * (STEP ? 2 : P) * plane_c + at;
-        *(ou_h4*)c = hi;
-        if (STEP || P == 2) *(ou_h4*)(c + plane_c) = lo;
-        if (WHAT == OU_UPDATE) {
-          _Float16* ct = o.Ct + z * P * plane_c + (size_t)(i + (lane & 3)) * o.J + (j & ~3);
-          *(uint2*)ct = ou_turn(__builtin_bit_cast(uint2, hi), lane);
-          if (P == 2) *(uint2*)(ct + plane_c) = ou_turn(__builtin_bit_cast(uint2, lo), lane);
+      for (int q = 0; q < 8; ++q) {
+        const float g = (float)oh[q] + (float)ol[q];
+        if (STEP) {
+          v[q] += (OU_A / OU_SX) * g;
+        } else {
+          v[q] = OU_C * v[q] + (OU_B / OU_SG) * g;
+          if (P == 2 && i + q == j && j < p.n) v[q] += OU_A;
         }
       }
+    }
+    if (WHAT == OU_LAST) {
+      const int n = p.n, m = p.m;
+      if (!p.tall) {                                 // rows of the result run along j: below
+        tile[slot(jl, il >> 2)] = make_float4(v[0], v[1], v[2], v[3]);
+        tile[slot(jl, (il >> 2) + 1)] = make_float4(v[4], v[5], v[6], v[7]);
+      } else if (j < m && i < n) {
+        const size_t to = z * n * m + (size_t)j * n + i;
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          if (out.W && i + q < n) v[q] = out.keep * out.W[to + q] - out.scale * v[q];
+        if (out.eights) {
+          rt_store<T, 8>(out.y + to, v);
+        } else {
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            if (i + q < n) out.y[to + q] = (T)v[q];
+        }
+      }
+      continue;
+    }
+    ou_h8 hi, lo;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      _Float16 h, l;
+      ou_cut(v[q] * scale, h, l);
+      hi[q] = h; lo[q] = l;
+    }
+    _Float16* c = o.C + z * (STEP ? 2 : P) * plane_c + at;
+    *(ou_h8*)c = hi;
+    if (STEP || P == 2) *(ou_h8*)(c + plane_c) = lo;
+    if (WHAT == OU_UPDATE && P == 1) {
+      tile[slot(jl, il >> 2)] = make_float4(v[0], v[1], v[2], v[3]);
+      tile[slot(jl, (il >> 2) + 1)] = make_float4(v[4], v[5], v[6], v[7]);
+    }
+  }
+  if (WHAT == OU_UPDATE || (WHAT == OU_LAST && !p.tall)) {    // the same along j
+    const float one = WHAT == OU_UPDATE && P == 2 ? unscale : 1.0f;
+    __syncthreads();
+    const float* flat = (const float*)smem;
+    for (int e = tid; e < TILE * ACROSS; e += 256) {
+      const int il = e / ACROSS, jl = (e % ACROSS) * 8, i = i0 + il, j = j0 + jl;
+      if (i >= o.I || j >= o.J) continue;
+      float v[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] = flat[4 * slot(jl + q, il >> 2) + (il & 3)] * one;
+      if (WHAT == OU_LAST) {
+        const int n = p.n, m = p.m;
+        if (i >= n) continue;
+        const size_t to = z * n * m + (size_t)i * m + j;
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          if (out.W && j + q < m) v[q] = out.keep * out.W[to + q] - out.scale * v[q];
+        if (out.eights) {
+          if (j < m) rt_store<T, 8>(out.y + to, v);
+        } else {
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            if (j + q < m) out.y[to + q] = (T)v[q];
+        }
+        continue;
+      }
+      ou_h8 hi, lo;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        _Float16 h, l;
+        ou_cut(v[q] * scale, h, l);
+        hi[q] = h; lo[q] = l;
+      }
+      _Float16* ct = o.Ct + z * P * plane_c + (size_t)i * o.J + j;
+      *(ou_h8*)ct = hi;
+      if (P == 2) *(ou_h8*)(ct + plane_c) = lo;
+    }
+  }
 }
 
 // ---- n <= 64: all of g and p in one workgroup ----------------------------------------------------------------------------------
-// The long side is cut into slabs of 128 columns of x (rows of x^T).  A launch takes the parts of g = x x^T of all slabs, and every
-// workgroup adds them (16 KB a slab, always in the same order), makes p for itself, takes its slab one step further and leaves
-// the slab's part of the next g.  So a step is one launch; with up to 128 columns in all (ALONE) everything is one.
+// The long side is cut into slabs of up to 256 columns of x (rows of x^T), 32 to a wave.  A launch takes the parts of g = x x^T of all
+// slabs, and every workgroup adds them (always in the same order), makes p for itself, takes its slab one step further and leaves
+// the slab's part of the next g.  So a step is one launch; where one slab holds everything (ALONE) all steps are one.
 //
-// x^T p lands in the accumulators with a lane holding column j and rows k of x^T four by four; that is also how the next product, g =
-// sum_k x^T[k][i] x^T[k][j], wants both its operands if the same order of k is taken for both, which any order may be.  Only the next
-// step's x^T has to change lanes (through memory, each wave its own rows).  Step 0 takes p = I, which is exact in pieces.
-constexpr int OS_ROWS = 128;                 // of a slab: 32 a wave
-constexpr int OS_SLABS = 64;                 // more columns than this many slabs: a workgroup takes several
-constexpr int OS_X = 2 * OS_ROWS * 8;        // LDS, in uint4: x^T pieces; then g and p pieces, and over them the waves' parts of g
-constexpr size_t OS_LDS = (size_t)OS_X * 16 + 4 * 64 * 64 * 4;
+// Everything stays in the order in which 32 x 32 products land in the accumulators: a lane holds one column and sixteen rows, eight and
+// eight (fragment t = 0, 1).  Read as an operand, the lane's column is the operand's row and the sixteen rows are contraction indices, in an
+// order that does not matter as long as both operands share it.  So the fragments of g serve as both operands of g g (g and p are
+// symmetric), those of x^T (lane = column j, registers = rows k) as both operands of g, and those of x (lane = k, registers = i) with p's
+// make the next x^T and, with the operands exchanged, the next x: twice the products, but no value ever changes lanes.
+// Until step 1 a slab is scaled by its own norm: the sums of squares of the others come with their parts of g, no pass for |u| alone.
+//
+// What bounds it: the chain of dependent products, conversions and barriers of a step, and the reading of the parts (16 KB a slab from L2).
+constexpr int OS_ROWS = 256, OS_WAVES = OS_ROWS / 32;
+constexpr int OS_SLABS = 64;                 // more columns than this many slabs: a workgroup takes several turns
 
 struct OsPlace {
-  _Float16* xt;           // [batch][slabs * turns * 128][2 pieces][64]
-  const float* part_in;   // [batch][slabs][64 * 64]: parts of g of this step
-  float* part_out;        // of the next one
-  const double* squares;  // sums of squares (not ALONE)
-  int n_squares, slabs, turns;
+  uint4* x;               // [batch][slabs * turns][8 waves][NB blocks][2 fragments][2 pieces][64 lanes] between two launches
+  const float4* part_in;  // [batch][slabs][NB^2 blocks][4][64 lanes]: parts of g of this step
+  float4* part_out;       // of the next one
+  double* squares;        // [batch][slabs]: sums of squares of the slabs
+  int slabs, turns;
 };
 
-// place of element (r, c) of a 64-wide tile of halves: 16-byte pieces exchanged by row, as in the products above
-__device__ __forceinline__ int os_at(int r, int c) { return r * 64 + (((c >> 3) ^ (r & 7)) << 3) + (c & 7); }
+template <int NB>
+struct OsLds {
+  static constexpr int FRAGMENTS = NB * NB * 2 * 2 * 64;                // uint4: g or p, [rows block][columns block][t][piece][lane]
+  static constexpr int PARTS = NB * NB * 4 * 64;                        // float4: one wave's part of g
+  static size_t bytes(int waves) { return (size_t)(2 * FRAGMENTS + waves * PARTS) * 16; }
+};
 
-template <class T, bool ALONE>
-__global__ __launch_bounds__(256) void ou_slab_kernel(OuShape p, OuInput<T> in, const float* m_old, float* m_new, OsPlace w, int step,
+// Eight values times `scale` -> hi and lo.  scale has to be a power of two: the compiler may round the product to 11 bits in one step or in
+// two, hi and the remainder each in its own way, which is the same only where the product is exact.
+__device__ __forceinline__ void os_cut(const float (&v)[8], float scale, ou_h8& hi, ou_h8& lo) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    const _Float16 h = (_Float16)(v[q] * scale);
+    hi[q] = h;
+    lo[q] = (_Float16)__builtin_fmaf(v[q], scale, -(float)h);
+  }
+}
+
+__device__ __forceinline__ ou_f16v os_product(const ou_h8 (&a)[2], const ou_h8 (&b)[2], ou_f16v acc) {   // [0] = hi, [1] = lo
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[1], b[0], acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0], b[1], acc, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a[0], b[0], acc, 0, 0, 0);
+}
+
+__device__ __forceinline__ ou_f16v os_zero() {
+  ou_f16v v;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+  return v;
+}
+
+// sum over the workgroup, in every thread
+__device__ __forceinline__ double os_sum(double t, double* s) {
+  for (int h = 32; h; h >>= 1) t += __shfl_xor(t, h);
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = t;
+  __syncthreads();
+  t = 0.0;
+  for (int w = 0; w < (int)blockDim.x >> 6; ++w) t += s[w];
+  __syncthreads();
+  return t;
+}
+
+template <class T, int NB, bool ALONE>
+__global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, const float* m_old, float* m_new, OsPlace w, int step,
                                                       int steps, OuOut<T> out) {
   extern __shared__ uint4 smem[];
-  _Float16* sx = (_Float16*)smem;                        // [2][128][64]
-  _Float16* sg = (_Float16*)(smem + OS_X);               // [2][64][64]
-  _Float16* sp = sg + 2 * 64 * 64;                       // [2][64][64]
-  float4* sums = (float4*)(smem + OS_X);                 // [4 waves][64][16], over sg and sp
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int r32 = lane & 31, hh = lane >> 5, slab = blockIdx.x;
-  const size_t z = blockIdx.y, size = (size_t)p.rows * p.cols, at0 = z * size;
-  double inv;
-  if (ALONE) {
-    double t = 0.0;
-    for (int i = tid; i < (int)size; i += 256) {
-      float v = (float)in.u[at0 + i];
-      if (m_old) {
-        const float mm = in.beta * m_old[at0 + i] + v;
-        m_new[at0 + i] = mm;
-        v = v + in.beta * mm;
+  typedef OsLds<NB> Lds;
+  uint4* sg = smem;
+  uint4* sp = smem + Lds::FRAGMENTS;
+  float4* sums = (float4*)(smem + 2 * Lds::FRAGMENTS);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+  const int r32 = lane & 31, hh = lane >> 5, slab = blockIdx.x, turns = ALONE ? 1 : w.turns;
+  const size_t z = blockIdx.y, at0 = z * p.rows * p.cols;
+  auto fragment = [&](const uint4* from, int a, int b, int t, ou_h8 (&v)[2]) {
+    const uint4* f = from + ((a * NB + b) * 2 + t) * 128 + lane;
+    v[0] = __builtin_bit_cast(ou_h8, f[0]);
+    v[1] = __builtin_bit_cast(ou_h8, f[64]);
+  };
+  // element of the caller's matrix for register q of block b of fragments of x; -1 past the edges
+  auto place = [&](int first, int b, int q) -> long {
+    const int i = 32 * b + 8 * (q >> 2) + 4 * hh + (q & 3), c = first + r32;
+    return i < p.n && c < p.m ? (long)(at0 + (p.tall ? (size_t)c * p.cols + i : (size_t)i * p.cols + c)) : -1;
+  };
+  // u of one turn's rows; the new momentum on the way
+  auto input = [&](int first, bool write, float (&u)[NB][16]) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) {
+        const long at = place(first, b, q);
+        float v = 0.0f;
+        if (at >= 0) {
+          v = (float)in.u[at];
+          if (m_old && write) {
+            const float mm = in.beta * m_old[at] + v;
+            m_new[at] = mm;
+            v = v + in.beta * mm;
+          } else if (m_old) {
+            v = v + in.beta * m_new[at];
+          }
+        }
+        u[b][q] = v;
       }
-      t += (double)v * (double)v;
-    }
-    for (int h = 32; h; h >>= 1) t += __shfl_xor(t, h);
-    double* s = (double*)smem;
-    if (lane == 0) s[wave] = t;
-    __syncthreads();
-    inv = (double)OU_SX / (sqrt((s[0] + s[1]) + (s[2] + s[3])) + OU_EPS);
-    __syncthreads();
-  } else if (step == 0) {
-    inv = ou_inverse_norm(w.squares + z * OU_PARTS, w.n_squares) * (double)OU_SX;
-  }
+  };
 
-  ou_f16v g[2][2];
-  for (int k = ALONE ? 0 : step; k <= (ALONE ? steps : step); ++k) {
-    // p in pieces
-    if (k == 0) {
-      for (int e = tid; e < 64 * 64; e += 256) {
-        const int r = e >> 6, c = e & 63;
-        sp[os_at(r, c)] = (_Float16)(r == c ? OU_SP : 0.0f);
-        sp[64 * 64 + os_at(r, c)] = (_Float16)0.0f;
-      }
-    } else {
-      float4 v[4];
-      if (ALONE) {
+  ou_h8 x[NB][2][2];           // fragments of x: [block][t][piece]
+  ou_f16v g[NB][NB];
+  auto row_of = [&](int turn) { return (slab * turns + turn) * OS_ROWS + wave * 32; };      // first row of x^T of this wave
+  auto kept = [&](int turn) { return w.x + (((z * w.slabs + slab) * turns + turn) * OS_WAVES + wave) * (NB * 256) + lane; };
+  auto clear = [&]() {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int e = tid + 256 * q;
-          const float4 a = sums[e], b = sums[1024 + e], c = sums[2048 + e], d = sums[3072 + e];
-          v[q] = make_float4((a.x + b.x) + (c.x + d.x), (a.y + b.y) + (c.y + d.y), (a.z + b.z) + (c.z + d.z), (a.w + b.w) + (c.w + d.w));
-        }
-        __syncthreads();
-      } else {
-        const float4* from = (const float4*)w.part_in + z * w.slabs * 1024;
+    for (int a = 0; a < NB; ++a)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = from[tid + 256 * q];
-#pragma unroll 4
-        for (int t = 1; t < w.slabs; ++t)
+      for (int b = 0; b < NB; ++b) g[a][b] = os_zero();
+  };
+  auto load_x = [&](int turn) {
+    const uint4* from = kept(turn);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const float4 a = from[t * 1024 + tid + 256 * q];
-            v[q].x += a.x; v[q].y += a.y; v[q].z += a.z; v[q].w += a.w;
-          }
-      }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int e = tid + 256 * q, r = e >> 4, c = 4 * ((e & 15) ^ (r & 15));
-        const float f[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
-        ou_h4 hi, lo;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          _Float16 h, l;
-          ou_cut(f[i] * OU_SG, h, l);
-          hi[i] = h; lo[i] = l;
-        }
-        *(ou_h4*)(sg + os_at(r, c)) = hi;
-        *(ou_h4*)(sg + 64 * 64 + os_at(r, c)) = lo;
-      }
-      __syncthreads();
-      const int wi = (wave >> 1) * 32, wj = (wave & 1) * 32;
-      ou_f16v acc;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[i] = 0.0f;
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const int c = 16 * s + 8 * hh;
-        const ou_h8 ah = *(const ou_h8*)(sg + os_at(wi + r32, c)), al = *(const ou_h8*)(sg + 64 * 64 + os_at(wi + r32, c));
-        const ou_h8 bh = *(const ou_h8*)(sg + os_at(wj + r32, c)), bl = *(const ou_h8*)(sg + 64 * 64 + os_at(wj + r32, c));
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(al, bh, acc, 0, 0, 0);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bl, acc, 0, 0, 0);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bh, acc, 0, 0, 0);
-      }
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int i = wi + 8 * r + 4 * hh, j = wj + r32;
-        const ou_h4 gh = *(const ou_h4*)(sg + os_at(j, i)), gl = *(const ou_h4*)(sg + 64 * 64 + os_at(j, i));
-        ou_h4 hi, lo;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float gv = ((float)gh[q] + (float)gl[q]) * (1.0f / OU_SG);
-          const float v = OU_C * (acc[4 * r + q] * (1.0f / (OU_SG * OU_SG))) + OU_B * gv + (i + q == j ? OU_A : 0.0f);
-          _Float16 h, l;
-          ou_cut(v * OU_SP, h, l);
-          hi[q] = h; lo[q] = l;
-        }
-        *(ou_h4*)(sp + os_at(j, i)) = hi;
-        *(ou_h4*)(sp + 64 * 64 + os_at(j, i)) = lo;
-      }
-    }
-#pragma unroll
-    for (int a = 0; a < 2; ++a)
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) g[a][b][i] = 0.0f;
-    __syncthreads();       // p is there
-
-    for (int turn = 0; turn < (ALONE ? 1 : w.turns); ++turn) {
-      const int first = (slab * (ALONE ? 1 : w.turns) + turn) * OS_ROWS;      // row of x^T
-      _Float16* mine = ALONE ? nullptr : w.xt + ((z * w.slabs * w.turns + slab * w.turns + turn) * OS_ROWS + wave * 32) * 128;
-      if (k == 0) {       // x_0 = u / |u|, each wave its own rows
-        for (int e = lane; e < 32 * 64; e += 64) {
-          const int row = p.tall ? e >> 6 : e & 31, i = p.tall ? e & 63 : e >> 5;
-          const int c = first + wave * 32 + row;
-          const bool there = i < p.n && c < p.m;
-          const size_t at = at0 + (p.tall ? (size_t)c * p.cols + i : (size_t)i * p.cols + c);
-          const float v = there ? (float)((double)ou_value(in, at) * inv) : 0.0f;
-          _Float16 h, l;
-          ou_cut(v, h, l);
-          sx[os_at(wave * 32 + row, i)] = h;
-          sx[OS_ROWS * 64 + os_at(wave * 32 + row, i)] = l;
-        }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
-      }
-      ou_f16v acc[2];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[0][i] = acc[1][i] = 0.0f;
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const int c = 16 * s + 8 * hh;
-        ou_h8 ah, al;
-        if (ALONE || k == 0) {
-          ah = *(const ou_h8*)(sx + os_at(wave * 32 + r32, c));
-          al = *(const ou_h8*)(sx + OS_ROWS * 64 + os_at(wave * 32 + r32, c));
-        } else {
-          ah = *(const ou_h8*)(mine + r32 * 128 + c);
-          al = *(const ou_h8*)(mine + r32 * 128 + 64 + c);
-        }
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const ou_h8 bh = *(const ou_h8*)(sp + os_at(32 * b + r32, c)), bl = *(const ou_h8*)(sp + 64 * 64 + os_at(32 * b + r32, c));
-          acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(al, bh, acc[b], 0, 0, 0);
-          acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bl, acc[b], 0, 0, 0);
-          acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bh, acc[b], 0, 0, 0);
-        }
-      }
-      if (k == steps) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int j = 32 * b + r32, c = first + wave * 32 + 8 * (i >> 2) + 4 * hh + (i & 3);
-            if (j >= p.n || c >= p.m) continue;
-            const size_t at = at0 + (p.tall ? (size_t)c * p.cols + j : (size_t)j * p.cols + c);
-            const float v = acc[b][i] * (1.0f / (OU_SP * OU_SX));
-            out.y[at] = (T)(out.W ? out.keep * out.W[at] - out.scale * v : v);
-          }
-        continue;
-      }
-      ou_h8 xh[2][2], xl[2][2];        // [column block][16 rows]: the operands of g
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          _Float16 h, l;
-          ou_cut(acc[b][i] * (1.0f / OU_SP), h, l);
-          xh[b][i >> 3][i & 7] = h;
-          xl[b][i >> 3][i & 7] = l;
-        }
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          ou_h4 h, l;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            h[q] = xh[b][r >> 1][4 * (r & 1) + q];
-            l[q] = xl[b][r >> 1][4 * (r & 1) + q];
-          }
-          const uint2 th = ou_turn(__builtin_bit_cast(uint2, h), lane), tl = ou_turn(__builtin_bit_cast(uint2, l), lane);
-          const int row = 8 * r + 4 * hh + (lane & 3), c = 32 * b + (r32 & ~3);
-          if (ALONE) {
-            *(uint2*)(sx + os_at(wave * 32 + row, c)) = th;
-            *(uint2*)(sx + OS_ROWS * 64 + os_at(wave * 32 + row, c)) = tl;
-          } else {
-            *(uint2*)(mine + row * 128 + c) = th;
-            *(uint2*)(mine + row * 128 + 64 + c) = tl;
-          }
-        }
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int a = 0; a < 2; ++a)
+        for (int q = 0; q < 2; ++q) x[b][t][q] = __builtin_bit_cast(ou_h8, from[((b * 2 + t) * 2 + q) * 64]);
+  };
+  auto store_x = [&](int turn) {
+    uint4* to = kept(turn);
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            g[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(xl[a][t], xh[b][t], g[a][b], 0, 0, 0);
-            g[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(xh[a][t], xl[b][t], g[a][b], 0, 0, 0);
-            g[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(xh[a][t], xh[b][t], g[a][b], 0, 0, 0);
-          }
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) to[((b * 2 + t) * 2 + q) * 64] = __builtin_bit_cast(uint4, x[b][t][q]);
+  };
+  auto cut = [&](const ou_f16v& acc, float scale, ou_h8 (&to)[2][2]) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      float v[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] = acc[8 * t + q];
+      os_cut(v, scale, to[t][0], to[t][1]);
     }
-    if (k == steps) return;
-    __syncthreads();       // p is no longer read: the waves' parts of g go over it
+  };
+  auto add_g = [&](const ou_h8 (&xt)[NB][2][2]) {
 #pragma unroll
-    for (int a = 0; a < 2; ++a)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int a = 0; a < NB; ++a)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) g[a][b] = os_product(xt[a][t], xt[b][t], g[a][b]);
+  };
+
+  // step 0: x = u / |u| and its g
+  auto begin = [&]() {
+    float u[NB][16];
+    double t = 0.0;
+    for (int turn = 0; turn < turns; ++turn) {
+      input(row_of(turn), true, u);
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) t += (double)u[b][q] * (double)u[b][q];
+    }
+    t = os_sum(t, (double*)smem);
+    const double inverse = ALONE ? 1.0 / (sqrt(t) + OU_EPS) : t == 0.0 ? 0.0 : 1.0 / sqrt(t);
+    if (!ALONE && tid == 0) w.squares[z * w.slabs + slab] = t;
+    clear();
+    for (int turn = 0; turn < turns; ++turn) {
+      if (turns > 1) input(row_of(turn), false, u);
+      ou_h8 xt[NB][2][2];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        ou_f16v rows = os_zero();      // x^T by a product with the identity: exact, as every value is two pieces
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          float v[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) v[q] = (float)((double)u[b][8 * t + q] * inverse);
+          os_cut(v, OU_SX, x[b][t][0], x[b][t][1]);
+          ou_h8 one;
+#pragma unroll
+          for (int q = 0; q < 8; ++q) one[q] = (_Float16)(16 * t + 8 * (q >> 2) + 4 * hh + (q & 3) == r32 ? 1.0f : 0.0f);
+          rows = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[b][t][1], one, rows, 0, 0, 0);
+          rows = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[b][t][0], one, rows, 0, 0, 0);
+        }
+        cut(rows, 1.0f, xt[b]);
+      }
+      if (!ALONE) store_x(turn);
+      add_g(xt);
+    }
+  };
+
+  // p = a I + b g + c g g in LDS, from the parts of g of all waves or of all slabs; in step 1 times the scale of this slab's x
+  auto make_p = [&](bool first) {
+    double norm = 1.0, factor = 1.0;
+    if (!ALONE && first) {
+      double t = 0.0;
+      for (int i = lane; i < w.slabs; i += 64) t += w.squares[z * w.slabs + i];
+      for (int h = 32; h; h >>= 1) t += __shfl_xor(t, h);
+      norm = 1.0 / (sqrt(t) + OU_EPS);
+      factor = sqrt(w.squares[z * w.slabs + slab]) * norm;
+    }
+    const int parts = ALONE ? waves : w.slabs;
+    const float4* from = ALONE ? sums : w.part_in + z * w.slabs * Lds::PARTS;
+    for (int e = tid; e < NB * NB * 128; e += blockDim.x) {        // the values of one fragment are two float4 of a lane
+      const int at = (e >> 6) * 128 + (e & 63);
+      float v[8] = {};
+#pragma unroll 4
+      for (int t = 0; t < parts; ++t) {
+        const float4 lo = from[t * Lds::PARTS + at], hi = from[t * Lds::PARTS + at + 64];
+        float f = 1.0f;
+        if (!ALONE && first) f = (float)(w.squares[z * w.slabs + t] * norm * norm);
+        v[0] += f * lo.x; v[1] += f * lo.y; v[2] += f * lo.z; v[3] += f * lo.w;
+        v[4] += f * hi.x; v[5] += f * hi.y; v[6] += f * hi.z; v[7] += f * hi.w;
+      }
+      ou_h8 h, l;
+      os_cut(v, OU_SG, h, l);
+      sg[at] = __builtin_bit_cast(uint4, h);
+      sg[at + 64] = __builtin_bit_cast(uint4, l);
+    }
+    __syncthreads();
+    for (int e = wave; e < NB * NB; e += waves) {                  // a block a wave
+      const int a = e / NB, b = e % NB;
+      ou_f16v acc = os_zero();
+#pragma unroll
+      for (int c = 0; c < NB; ++c)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          ou_h8 ga[2], gb[2];
+          fragment(sg, c, a, t, ga);
+          fragment(sg, c, b, t, gb);
+          acc = os_product(ga, gb, acc);
+        }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        ou_h8 ge[2], h, l;
+        fragment(sg, a, b, t, ge);
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const int i = 16 * t + 8 * (q >> 2) + 4 * hh + (q & 3);
+          v[q] = (OU_C / (OU_SG * OU_SG)) * acc[8 * t + q] + (OU_B / OU_SG) * ((float)ge[0][q] + (float)ge[1][q]);
+          v[q] += a == b && i == r32 ? OU_A : 0.0f;
+          v[q] *= (float)factor;
+        }
+        os_cut(v, OU_SP, h, l);
+        uint4* to = sp + (e * 2 + t) * 128 + lane;
+        to[0] = __builtin_bit_cast(uint4, h);
+        to[64] = __builtin_bit_cast(uint4, l);
+      }
+    }
+    __syncthreads();
+  };
+
+  // x^T p (FLIP: p x) of column block b
+  auto times_p = [&](int b, bool flip) {
+    ou_f16v acc = os_zero();
+#pragma unroll
+    for (int c = 0; c < NB; ++c)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        ou_h8 pf[2];
+        fragment(sp, c, b, t, pf);
+        acc = flip ? os_product(pf, x[c][t], acc) : os_product(x[c][t], pf, acc);
+      }
+    return acc;
+  };
+
+  auto advance = [&]() {
+    clear();
+    for (int turn = 0; turn < turns; ++turn) {
+      if (!ALONE) load_x(turn);
+      ou_h8 xt[NB][2][2];
+      ou_f16v next[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        cut(times_p(b, false), 1.0f / OU_SP, xt[b]);
+        next[b] = times_p(b, true);
+      }
+#pragma unroll
+      for (int b = 0; b < NB; ++b) cut(next[b], 1.0f / OU_SP, x[b]);
+      if (!ALONE) store_x(turn);
+      add_g(xt);
+    }
+  };
+
+  auto finish = [&]() {
+    for (int turn = 0; turn < turns; ++turn) {
+      if (!ALONE) load_x(turn);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const ou_f16v last = times_p(b, true);
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+          const long at = place(row_of(turn), b, q);
+          if (at < 0) continue;
+          const float v = last[q] * (1.0f / (OU_SP * OU_SX));
+          out.y[at] = (T)(out.W ? out.keep * out.W[at] - out.scale * v : v);
+        }
+      }
+    }
+  };
+
+  auto publish = [&]() {
+#pragma unroll
+    for (int a = 0; a < NB; ++a)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int i = 32 * a + 8 * r + 4 * hh, j = 32 * b + r32;
-          constexpr float u = 1.0f / (OU_SX * OU_SX);
-          sums[wave * 1024 + j * 16 + ((i >> 2) ^ (j & 15))] =
-              make_float4(g[a][b][4 * r] * u, g[a][b][4 * r + 1] * u, g[a][b][4 * r + 2] * u, g[a][b][4 * r + 3] * u);
+          constexpr float v = 1.0f / (OU_SX * OU_SX);
+          sums[wave * Lds::PARTS + ((a * NB + b) * 4 + r) * 64 + lane] =
+              make_float4(g[a][b][4 * r] * v, g[a][b][4 * r + 1] * v, g[a][b][4 * r + 2] * v, g[a][b][4 * r + 3] * v);
         }
     __syncthreads();
-    if (!ALONE) {
-      float4* to = (float4*)w.part_out + (z * w.slabs + slab) * 1024;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int e = tid + 256 * q;
-        const float4 a = sums[e], b = sums[1024 + e], c = sums[2048 + e], d = sums[3072 + e];
-        to[e] = make_float4((a.x + b.x) + (c.x + d.x), (a.y + b.y) + (c.y + d.y), (a.z + b.z) + (c.z + d.z), (a.w + b.w) + (c.w + d.w));
+    if (ALONE) return;
+    for (int e = tid; e < Lds::PARTS; e += blockDim.x) {
+      float4 t = sums[e];
+      for (int i = 1; i < waves; ++i) {
+        const float4 v = sums[i * Lds::PARTS + e];
+        t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
       }
+      w.part_out[(z * w.slabs + slab) * Lds::PARTS + e] = t;
+    }
+  };
+
+  if (ALONE) {
+    begin();
+    publish();
+    for (int k = 1; k < steps; ++k) {
+      make_p(false);
+      advance();
+      publish();
+    }
+    make_p(false);
+    finish();
+  } else if (step == 0) {
+    begin();
+    publish();
+  } else {
+    make_p(step == 1);
+    if (step < steps) {
+      advance();
+      publish();
+    } else {
+      finish();
     }
   }
 }
@@ -587,43 +724,46 @@ OuShape ou_shape(int32_t batch, int32_t rows, int32_t cols) {
 // 64 x 900 and more below; half precision and fp32 results would lose 2 and 400 times their own accuracy.
 int ou_pieces(const OuShape& p, int32_t dtype) { return dtype == EGNN_BF16 && p.n >= OU_ONE_PIECE ? 1 : 2; }
 
-struct OsSpace { size_t part, xt, g, bytes; int slabs, turns; };
+struct OsSpace { size_t squares, x, g, bytes; int slabs, turns, blocks; };
 OsSpace os_space(const OuShape& p) {
   OsSpace s;
-  const int pieces = (p.m + OS_ROWS - 1) / OS_ROWS;
-  s.turns = (pieces + OS_SLABS - 1) / OS_SLABS;
-  s.slabs = (pieces + s.turns - 1) / s.turns;
-  s.part = 0;
-  s.xt = ou_align((size_t)p.batch * OU_PARTS * sizeof(double));
-  s.g = s.xt + ou_align((size_t)p.batch * s.slabs * s.turns * OS_ROWS * 128 * 2);
-  s.bytes = s.slabs == 1 && s.turns == 1 ? 256 : s.g + 2 * ou_align((size_t)p.batch * s.slabs * 64 * 64 * 4);
+  const int slabs = (p.m + OS_ROWS - 1) / OS_ROWS;
+  s.blocks = p.n <= 32 ? 1 : 2;
+  s.turns = (slabs + OS_SLABS - 1) / OS_SLABS;
+  s.slabs = (slabs + s.turns - 1) / s.turns;
+  s.squares = 0;
+  s.x = ou_align((size_t)p.batch * s.slabs * sizeof(double));
+  s.g = s.x + ou_align((size_t)p.batch * s.slabs * s.turns * OS_WAVES * s.blocks * 256 * sizeof(uint4));
+  s.bytes = slabs == 1 ? 256 : s.g + 2 * ou_align((size_t)p.batch * s.slabs * s.blocks * s.blocks * 256 * sizeof(float4));
   return s;
 }
 
 int ou_parts(size_t size) { return (int)(size > (size_t)OU_PARTS * 4096 ? OU_PARTS : (size + 4095) / 4096); }
 
-template <class T>
+// Side of at most 32: one block of 32 x 32 holds g, otherwise four do (a step of 15 matrices 32 x 32 took OS_32 us with one and OS_64 us with four).
+template <class T, int NB>
 int ou_run_slabs(egnn_ctx* ctx, const OuShape& p, const OuInput<T>& in, const float* m_old, float* m_new, int steps,
                  const OuOut<T>& out, void* ws, hipStream_t st) {
   const OsSpace s = os_space(p);
+  const size_t most = OsLds<NB>::bytes(OS_WAVES);
   static bool ready = false;      // (set again by two threads at once: to the same value)
   if (!ready) {
-    EGNN_HIP(ctx, hipFuncSetAttribute((const void*)ou_slab_kernel<T, true>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)OS_LDS));
-    EGNN_HIP(ctx, hipFuncSetAttribute((const void*)ou_slab_kernel<T, false>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)OS_LDS));
+    EGNN_HIP(ctx, hipFuncSetAttribute((const void*)ou_slab_kernel<T, NB, true>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)most));
+    EGNN_HIP(ctx, hipFuncSetAttribute((const void*)ou_slab_kernel<T, NB, false>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)most));
     ready = true;
   }
-  if (s.slabs == 1 && s.turns == 1) {
-    hipLaunchKernelGGL((ou_slab_kernel<T, true>), dim3(1, p.batch), dim3(256), OS_LDS, st, p, in, m_old, m_new, OsPlace{}, 0, steps, out);
+  if (p.m <= OS_ROWS) {
+    const int waves = (p.m + 31) / 32;
+    hipLaunchKernelGGL((ou_slab_kernel<T, NB, true>), dim3(1, p.batch), dim3(64 * waves), OsLds<NB>::bytes(waves), st, p, in, m_old, m_new,
+                       OsPlace{}, 0, steps, out);
     EGNN_LAUNCH_CHECK(ctx, "orthogonalise");
     return EGNN_OK;
   }
-  double* part = (double*)((char*)ws + s.part);
-  float* g[2] = {(float*)((char*)ws + s.g), (float*)((char*)ws + s.g + (s.bytes - s.g) / 2)};
-  const size_t size = (size_t)p.rows * p.cols;
-  hipLaunchKernelGGL((ou_square_kernel<T>), dim3(ou_parts(size), p.batch), dim3(256), 0, st, in, m_old, m_new, size, part);
+  float4* g[2] = {(float4*)((char*)ws + s.g), (float4*)((char*)ws + s.g + (s.bytes - s.g) / 2)};
   for (int k = 0; k <= steps; ++k) {
-    const OsPlace w{(_Float16*)((char*)ws + s.xt), g[k & 1], g[(k + 1) & 1], part, ou_parts(size), s.slabs, s.turns};
-    hipLaunchKernelGGL((ou_slab_kernel<T, false>), dim3(s.slabs, p.batch), dim3(256), OS_LDS, st, p, in, m_old, m_new, w, k, steps, out);
+    const OsPlace w{(uint4*)((char*)ws + s.x), g[k & 1], g[(k + 1) & 1], (double*)((char*)ws + s.squares), s.slabs, s.turns};
+    hipLaunchKernelGGL((ou_slab_kernel<T, NB, false>), dim3(s.slabs, p.batch), dim3(64 * OS_WAVES), most, st, p, in, m_old, m_new, w, k, steps,
+                       out);
   }
   EGNN_LAUNCH_CHECK(ctx, "orthogonalise");
   return EGNN_OK;
@@ -666,7 +806,8 @@ int ou_product(egnn_ctx* ctx, const OuShape& p, const OuOperands& o, const OuOut
 template <class T, int P>
 int ou_run(egnn_ctx* ctx, const OuShape& p, const OuInput<T>& in, const float* m_old, float* m_new, int steps, const OuOut<T>& out,
            void* ws, hipStream_t st) {
-  if (p.n <= 64) return ou_run_slabs<T>(ctx, p, in, m_old, m_new, steps, out, ws, st);
+  if (p.n <= 32) return ou_run_slabs<T, 1>(ctx, p, in, m_old, m_new, steps, out, ws, st);
+  if (p.n <= 64) return ou_run_slabs<T, 2>(ctx, p, in, m_old, m_new, steps, out, ws, st);
   const OuSpace s = ou_space(p, P);
   double* part = (double*)((char*)ws + s.part);
   _Float16* x = (_Float16*)((char*)ws + s.x);
@@ -701,7 +842,7 @@ int ou_check(egnn_ctx* ctx, const char* who, int32_t batch, int32_t rows, int32_
 template <class T>
 int ou_matrices(egnn_ctx* ctx, int32_t dtype, const OuShape& p, const void* g, int steps, void* y, void* ws, hipStream_t st) {
   const OuInput<T> in{(const T*)g, nullptr, 0.0f};
-  const OuOut<T> out{(T*)y, nullptr, 0.0f, 0.0f};
+  const OuOut<T> out{(T*)y, nullptr, 0.0f, 0.0f, p.cols % 8 == 0 && (uintptr_t)y % 16 == 0};
   if constexpr (std::is_same<T, __bf16>::value)
     if (ou_pieces(p, dtype) == 1) return ou_run<T, 1>(ctx, p, in, nullptr, nullptr, steps, out, ws, st);
   return ou_run<T, 2>(ctx, p, in, nullptr, nullptr, steps, out, ws, st);
@@ -744,6 +885,6 @@ extern "C" int egnn_muon_step(egnn_ctx* ctx, const float* W, const float* g, con
     return egnn_fail(ctx, EGNN_EWS, "muon_step: workspace too small or not 256-byte aligned");
   const float scale = (float)((double)lr * sqrt(rows > cols ? (double)rows / cols : 1.0));
   const float keep = (float)(1.0 - (double)lr * (double)weight_decay);
-  return ou_run<float, 2>(ctx, p, OuInput<float>{g, m_out, beta}, m, m_out, steps, OuOut<float>{W_out, W, keep, scale}, ws,
+  return ou_run<float, 2>(ctx, p, OuInput<float>{g, m_out, beta}, m, m_out, steps, OuOut<float>{W_out, W, keep, scale, cols % 8 == 0 && (uintptr_t)W_out % 16 == 0}, ws,
                           (hipStream_t)stream);
 }
