@@ -4,6 +4,7 @@
 //                rows ascend.  Only the keys are sorted: (l, m) runs through fixed places of an atom's rows.
 //   linear:      y_r = x_r W_g^T + b_g,   dx_r = dy_r W_g,   dW_g = sum_r dy_r^T x_r,   db_g = sum_r dy_r   (r in group g).
 #include "row_types.h"
+#include "stream_gemm.h"
 
 namespace {
 
@@ -105,87 +106,441 @@ __device__ __forceinline__ long gl_row(const GlRows& p, long at) {
   return p.perm ? min(max((long)p.perm[at], 0l), p.n - 1) : at;
 }
 
-constexpr int GL_TILE = 64, GL_K = 16;
+// The types on the matrix cores: fp32 as the three bf16 pieces of split_bf16.h (8 + 8 + 8 bits, exact, and of any magnitude: no scaling,
+// so gradients of any size keep their accuracy), whose six leading products are kept (the dropped ones are 2^-24 of the product);
+// half precision and bfloat16 as they are.
+typedef _Float16 gl_h8 __attribute__((ext_vector_type(8)));
+typedef float gl_f16v __attribute__((ext_vector_type(16)));
+template <class T> struct GlType {
+  static constexpr int PIECES = 1;
+  typedef uint4 Raw;                                     // eight values
+};
+template <> struct GlType<float> {
+  static constexpr int PIECES = 3;
+  struct Raw { uint4 a, b; };
+};
 
-// y rows = x rows times W_g^T (BACK: W_g) + bias; 64 rows of one group by 64 columns
-template <class T, bool BACK>
-__global__ __launch_bounds__(256) void gl_rows_kernel(GlRows p, const T* x, long xs, const T* W, const float* bias, int K, int N, T* y,
-                                                      long ys) {
-  __shared__ float sx[GL_K][GL_TILE + 4], sw[GL_K][GL_TILE + 4];
-  __shared__ int s_g, s_tile;
-  const int tid = threadIdx.x;
-  if (tid == 0) {
-    int left = blockIdx.x, g = 0;
-    for (; g < p.G; ++g) {
-      const int tiles = (int)((max(gl_begin(p, g + 1) - gl_begin(p, g), 0l) + GL_TILE - 1) / GL_TILE);
-      if (left < tiles) break;
-      left -= tiles;
-    }
-    s_g = g;
-    s_tile = left;
+__device__ __forceinline__ gl_f16v gl_mfma(uint4 a, uint4 b, gl_f16v c, __bf16) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
+}
+__device__ __forceinline__ gl_f16v gl_mfma(uint4 a, uint4 b, gl_f16v c, _Float16) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(gl_h8, a), __builtin_bit_cast(gl_h8, b), c, 0, 0, 0);
+}
+template <class T>
+__device__ __forceinline__ gl_f16v gl_product(const uint4 (&a)[1], const uint4 (&b)[1], gl_f16v c) {
+  return gl_mfma(a[0], b[0], c, T());
+}
+template <class T>
+__device__ __forceinline__ gl_f16v gl_product(const uint4 (&a)[3], const uint4 (&b)[3], gl_f16v c) {
+  const __bf16 t = {};
+  c = gl_mfma(a[2], b[0], c, t);
+  c = gl_mfma(a[0], b[2], c, t);
+  c = gl_mfma(a[1], b[1], c, t);
+  c = gl_mfma(a[1], b[0], c, t);
+  c = gl_mfma(a[0], b[1], c, t);
+  return gl_mfma(a[0], b[0], c, t);
+}
+
+// eight values at p (aligned to one value), of which the first `valid` are there; the others are zero
+typedef uint32_t gl_u4 __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ uint4 gl_load16(const void* p) {
+  const gl_u4 v = *reinterpret_cast<const gl_u4*>(p);
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+template <class T>
+__device__ __forceinline__ void gl_load(const T* p, int valid, uint4& r) {
+  r = make_uint4(0, 0, 0, 0);
+  if (valid >= 8) {
+    r = gl_load16(p);
+  } else if (valid > 0) {
+    uint32_t w[4] = {};
+#pragma unroll
+    for (int q = 0; q < 7; ++q)
+      if (q < valid) w[q >> 1] |= (uint32_t) reinterpret_cast<const uint16_t*>(p)[q] << (16 * (q & 1));
+    r = make_uint4(w[0], w[1], w[2], w[3]);
   }
+}
+__device__ __forceinline__ void gl_load(const float* p, int valid, GlType<float>::Raw& r) {
+  r.a = r.b = make_uint4(0, 0, 0, 0);
+  if (valid >= 8) {
+    r.a = gl_load16(p);
+    r.b = gl_load16(p + 4);
+  } else if (valid > 0) {
+    uint32_t w[8] = {};
+#pragma unroll
+    for (int q = 0; q < 7; ++q)
+      if (q < valid) w[q] = __float_as_uint(p[q]);
+    r.a = make_uint4(w[0], w[1], w[2], w[3]);
+    r.b = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+}
+// -> pieces
+__device__ __forceinline__ void gl_cut(uint4 r, uint4 (&to)[1]) { to[0] = r; }
+__device__ __forceinline__ void gl_cut(const GlType<float>::Raw& r, uint4 (&to)[3]) {
+  const uint32_t w[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
+  uint32_t h[4], m[4], l[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const Split3 s0 = split3(__uint_as_float(w[2 * q])), s1 = split3(__uint_as_float(w[2 * q + 1]));
+    h[q] = pack2(s0.hi, s1.hi);
+    m[q] = pack2(s0.mid, s1.mid);
+    l[q] = pack2(s0.lo, s1.lo);
+  }
+  to[0] = make_uint4(h[0], h[1], h[2], h[3]);
+  to[1] = make_uint4(m[0], m[1], m[2], m[3]);
+  to[2] = make_uint4(l[0], l[1], l[2], l[3]);
+}
+template <class T>
+__device__ __forceinline__ void gl_add(uint4 r, float (&to)[8]) {
+  typedef T vec __attribute__((ext_vector_type(8)));
+  const vec v = __builtin_bit_cast(vec, r);
+#pragma unroll
+  for (int q = 0; q < 8; ++q) to[q] += (float)v[q];
+}
+template <class T>
+__device__ __forceinline__ void gl_add(const GlType<float>::Raw& r, float (&to)[8]) {
+  const uint32_t w[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
+#pragma unroll
+  for (int q = 0; q < 8; ++q) to[q] += __uint_as_float(w[q]);
+}
+
+// One tile of a product in LDS, as pieces, 16 bits a value, in one of two layouts:
+//   along the contraction  [SIDE][KS]: rows of 2 KS + 16 bytes, so that eight rows read at one place meet different banks;
+//   across it              [KS][SIDE]: rows of 2 SIDE + 64 bytes; the operand's eight contraction indices come out of two transposing reads
+//                          of four rows each (ds_read_b64_tr_b16: lane i of sixteen gets column i of the four rows that its lanes point to).
+template <int SIDE, int KS, bool ACROSS>
+struct GlTile {
+  static constexpr int ROW = ACROSS ? 2 * SIDE + 64 : 2 * KS + 16;           // bytes
+  static constexpr int ROWS = ACROSS ? KS : SIDE, PLANE = ROW * ROWS;
+  static constexpr int EIGHTS = (ACROSS ? SIDE : KS) / 8;                     // of a row
+  static constexpr int CHUNKS = ROWS * EIGHTS / 256;                          // a thread stages so many pieces of eight values
+  static_assert(ROWS * EIGHTS % 256 == 0, "whole rounds");
+  __device__ static int row(int c) { return (threadIdx.x + 256 * c) / EIGHTS; }
+  __device__ static int col(int c) { return (threadIdx.x + 256 * c) % EIGHTS * 8; }
+  __device__ static int at(int c) { return row(c) * ROW + col(c) * 2; }
+  // operand of 32 rows from `side` on, contraction indices 16 s ..
+  __device__ static uint4 operand(const char* plane, int side, int s) {
+    const int lane = threadIdx.x & 63, hh = lane >> 5;
+    if (!ACROSS) return *reinterpret_cast<const uint4*>(plane + (side + (lane & 31)) * ROW + (16 * s + 8 * hh) * 2);
+    typedef short s4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s4* lp;
+    const char* p = plane + (16 * s + 8 * hh + ((lane & 15) >> 2)) * ROW + (side + (lane & 16) + 4 * (lane & 3)) * 2;
+    const uint2 u = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)p));
+    const uint2 v = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(p + 4 * ROW)));
+    return make_uint4(u.x, u.y, v.x, v.y);
+  }
+};
+
+enum GlKind { GL_FORWARD, GL_INPUT, GL_WEIGHTS };      // y = x W^T + b;  dx = dy W;  dW = dy^T x, db
+
+template <class T>
+struct GlArgs {
+  GlRows rows;
+  const T *a, *b;                 // GL_FORWARD: x, W;  GL_INPUT: dy, W;  GL_WEIGHTS: dy, x
+  long a_stride, b_stride;
+  int I, J, K;                    // result columns n of the output (GL_WEIGHTS: n_out x n_in); K: contraction (unused by GL_WEIGHTS)
+  T* y;
+  long y_stride;
+  const float* bias;
+  float *dW, *db;                 // GL_WEIGHTS: per slot [I][J] and [I]
+  int tiles_j;                    // column tiles
+  long chunk;                     // GL_WEIGHTS: rows of a slot at most
+};
+
+// Tile `t` of the rows: group and first row; false past the end.  The tiles of a group start at its first row.
+__device__ __forceinline__ bool gl_find(const GlRows& p, long t, int size, int& group, long& r0, long& r1) {
+  __shared__ long s_sum[4], s_found[3];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (tid == 0) s_found[0] = -1;
+  for (int g0 = 0; g0 < p.G; g0 += 256) {
+    const int g = g0 + tid;
+    long b = 0, e = 0;
+    if (g < p.G) {
+      b = gl_begin(p, g);
+      e = gl_begin(p, g + 1);
+    }
+    const long mine = e > b ? (e - b + size - 1) / size : 0;
+    long sum = mine;
+    for (int h = 1; h < 64; h <<= 1) {
+      const long v = __shfl_up(sum, h);
+      if (lane >= h) sum += v;
+    }
+    __syncthreads();
+    if (lane == 63) s_sum[wave] = sum;
+    __syncthreads();
+    long before = 0, all = 0;
+    for (int w = 0; w < 4; ++w) {
+      before += w < wave ? s_sum[w] : 0;
+      all += s_sum[w];
+    }
+    if (t < all) {
+      const long first = before + sum - mine;
+      if (t >= first && t < first + mine) {
+        s_found[0] = g;
+        s_found[1] = b + (t - first) * size;
+        s_found[2] = min(b + (t - first + 1) * size, e);
+      }
+      __syncthreads();
+      break;
+    }
+    t -= all;
+  }
+  if (s_found[0] < 0) return false;
+  group = (int)s_found[0];
+  r0 = s_found[1];
+  r1 = s_found[2];
+  return true;
+}
+
+// Slot `t` of the rows cut into equal chunks: chunk c and group g that share rows own slot c + g (either goes up by one from slot to slot, so
+// no two pairs share one).  With one chunk the slot is the group.
+__device__ __forceinline__ bool gl_slot(const GlRows& p, long chunk, int t, int& group, long& r0, long& r1) {
+  int lo = 0, hi = p.G - 1;                       // the last group whose first slot is not behind t
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (gl_begin(p, mid) / chunk + mid <= t) lo = mid; else hi = mid - 1;
+  }
+  group = lo;
+  const long b = gl_begin(p, lo), e = gl_begin(p, lo + 1), c = t - lo;
+  r0 = max(b, c * chunk);
+  r1 = min(e, (c + 1) * chunk);
+  return c >= 0 && r0 < r1;
+}
+
+// 256 threads, four waves, each a quarter of the BM x BN tile in 32 x 32 blocks.  Tiles go from memory to registers a turn ahead, are cut into
+// pieces on the way to one of two LDS buffers, and are contracted from the other.
+template <class T, GlKind KIND, int BM, int BN, int KS>
+__global__ __launch_bounds__(256) void gl_tile_kernel(GlArgs<T> g) {
+  extern __shared__ __align__(16) char smem[];
+  constexpr int NP = GlType<T>::PIECES, MB = BM / 64, NB = BN / 64;
+  typedef typename GlType<T>::Raw Raw;
+  typedef GlTile<BM, KS, KIND == GL_WEIGHTS> TA;
+  typedef GlTile<BN, KS, KIND != GL_FORWARD> TB;
+  constexpr int STAGE = NP * (TA::PLANE + TB::PLANE);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r32 = lane & 31, hh = lane >> 5;
+
+  // Neighbouring tiles to the same XCD (workgroups go round the eight of them in turn), the columns of a tile of rows one after the other.
+  const long per = ((long)gridDim.x + 7) >> 3, tile = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if ((blockIdx.x >> 3) >= per) return;
+  int group;
+  long r0, r1;
+  const long rt = tile / g.tiles_j;
+  const int ct = (int)(tile - rt * g.tiles_j);
+  int i0 = 0, j0 = ct * BN;
+  if (KIND == GL_WEIGHTS) {
+    const int across = g.dW ? (g.J + BN - 1) / BN : 1;
+    i0 = ct / across * BM;
+    j0 = ct % across * BN;
+    const bool there = rt < 0x7fffffff && gl_slot(g.rows, g.chunk, (int)rt, group, r0, r1);
+    if (!there && (g.chunk < g.rows.n || rt >= g.rows.G)) return;
+    if (!there) r0 = r1 = 0;                          // one chunk: a group without rows gets its zeros here
+  } else if (!gl_find(g.rows, rt, BM, group, r0, r1)) {
+    return;
+  }
+
+  // what this thread stages
+  const T *pa[TA::CHUNKS], *pb[TB::CHUNKS];
+  int na[TA::CHUNKS], nb[TB::CHUNKS];                 // GL_FORWARD, GL_INPUT: values to the end of the row (or the column), 0: no row
+  long ra[TA::CHUNKS], rb[TB::CHUNKS];                // GL_WEIGHTS: the rows of the next turn to be fetched, -1: none
+  const long weights = KIND == GL_WEIGHTS ? 0 : (long)group * g.J * g.K;
+#pragma unroll
+  for (int c = 0; c < TA::CHUNKS; ++c) {
+    if (KIND == GL_WEIGHTS) {
+      pa[c] = g.a + i0 + TA::col(c);
+      na[c] = g.I - i0 - TA::col(c);
+      const long r = r0 + TA::row(c);
+      ra[c] = r < r1 ? gl_row(g.rows, r) : -1;
+    } else {
+      const long r = r0 + TA::row(c);
+      pa[c] = g.a + (r < r1 ? gl_row(g.rows, r) * g.a_stride : 0) + TA::col(c);
+      na[c] = r < r1 ? g.K - TA::col(c) : 0;
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < TB::CHUNKS; ++c) {
+    if (KIND == GL_WEIGHTS) {
+      pb[c] = g.b + j0 + TB::col(c);
+      nb[c] = g.J - j0 - TB::col(c);
+      const long r = r0 + TB::row(c);
+      rb[c] = r < r1 ? gl_row(g.rows, r) : -1;
+    } else if (KIND == GL_INPUT) {                    // W[k][j]
+      pb[c] = g.b + weights + (long)TB::row(c) * g.J + j0 + TB::col(c);
+      nb[c] = g.J - j0 - TB::col(c);
+    } else {                                          // W[j][k]
+      pb[c] = g.b + weights + (long)(j0 + TB::row(c)) * g.K + TB::col(c);
+      nb[c] = j0 + TB::row(c) < g.J ? g.K - TB::col(c) : 0;
+    }
+  }
+  Raw a[TA::CHUNKS], b[TB::CHUNKS];
+  auto fetch = [&](int turn) {
+#pragma unroll
+    for (int c = 0; c < TA::CHUNKS; ++c) {
+      if (KIND == GL_WEIGHTS) {
+        gl_load(pa[c] + (ra[c] < 0 ? 0 : ra[c]) * g.a_stride, ra[c] < 0 ? 0 : na[c], a[c]);
+        const long r = r0 + (long)(turn + 1) * KS + TA::row(c);
+        ra[c] = r < r1 ? gl_row(g.rows, r) : -1;
+      } else {
+        gl_load(pa[c], na[c], a[c]);
+        pa[c] += KS;
+        na[c] -= KS;
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < TB::CHUNKS; ++c) {
+      if (KIND == GL_WEIGHTS) {
+        gl_load(pb[c] + (rb[c] < 0 ? 0 : rb[c]) * g.b_stride, rb[c] < 0 ? 0 : nb[c], b[c]);
+        const long r = r0 + (long)(turn + 1) * KS + TB::row(c);
+        rb[c] = r < r1 ? gl_row(g.rows, r) : -1;
+      } else if (KIND == GL_INPUT) {
+        gl_load(pb[c], turn * KS + TB::row(c) < g.K ? nb[c] : 0, b[c]);
+        pb[c] += (long)KS * g.J;
+      } else {
+        gl_load(pb[c], nb[c], b[c]);
+        pb[c] += KS;
+        nb[c] -= KS;
+      }
+    }
+  };
+  float turn_sum[8];
+  double col_sum[8] = {};
+  const bool sums = KIND == GL_WEIGHTS && g.db && j0 == 0;
+  auto stage = [&](int at) {
+    char* to = smem + at * STAGE;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) turn_sum[q] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < TA::CHUNKS; ++c) {
+      uint4 v[NP];
+      gl_cut(a[c], v);
+      if (sums) gl_add<T>(a[c], turn_sum);
+#pragma unroll
+      for (int q = 0; q < NP; ++q) *reinterpret_cast<uint4*>(to + q * TA::PLANE + TA::at(c)) = v[q];
+    }
+#pragma unroll
+    for (int c = 0; c < TB::CHUNKS; ++c) {
+      uint4 v[NP];
+      gl_cut(b[c], v);
+#pragma unroll
+      for (int q = 0; q < NP; ++q) *reinterpret_cast<uint4*>(to + NP * TA::PLANE + q * TB::PLANE + TB::at(c)) = v[q];
+    }
+    if (sums)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) col_sum[q] += (double)turn_sum[q];
+  };
+
+  gl_f16v acc[MB][NB];
+#pragma unroll
+  for (int x = 0; x < MB; ++x)
+#pragma unroll
+    for (int y = 0; y < NB; ++y)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[x][y][i] = 0.0f;
+  const int wi = (wave >> 1) * (BM / 2), wj = (wave & 1) * (BN / 2);
+  const int turns = (int)(KIND == GL_WEIGHTS ? (r1 - r0 + KS - 1) / KS : (g.K + KS - 1) / KS);
+  if (turns > 0) {
+    fetch(0);
+    stage(0);
+    if (turns > 1) fetch(1);
+  }
+  for (int k = 0; k < turns; ++k) {
+    rb_release_barrier();        // (only LDS is waited for: the next turn's loads stay under way)
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    const char* from = smem + (k & 1) * STAGE;
+#pragma unroll
+    for (int s = 0; s < KS / 16; ++s) {
+      uint4 fa[MB][NP], fb[NB][NP];
+#pragma unroll
+      for (int x = 0; x < MB; ++x)
+#pragma unroll
+        for (int q = 0; q < NP; ++q) fa[x][q] = TA::operand(from + q * TA::PLANE, wi + 32 * x, s);
+#pragma unroll
+      for (int y = 0; y < NB; ++y)
+#pragma unroll
+        for (int q = 0; q < NP; ++q) fb[y][q] = TB::operand(from + NP * TA::PLANE + q * TB::PLANE, wj + 32 * y, s);
+#pragma unroll
+      for (int x = 0; x < MB; ++x)
+#pragma unroll
+        for (int y = 0; y < NB; ++y) acc[x][y] = gl_product<T>(fa[x], fb[y], acc[x][y]);
+    }
+    if (k + 1 < turns) {
+      stage((k + 1) & 1);
+      if (k + 2 < turns) fetch(k + 2);
+    }
+  }
+
+  // a lane holds column j = lane & 31 of its blocks and four times four neighbouring rows i
+  if (KIND == GL_WEIGHTS) {
+    float* to = g.dW ? g.dW + (size_t)rt * g.I * g.J : nullptr;
+#pragma unroll
+    for (int x = 0; x < MB; ++x)
+#pragma unroll
+      for (int y = 0; y < NB; ++y)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+          const int i = i0 + wi + 32 * x + 8 * (q >> 2) + 4 * hh + (q & 3), j = j0 + wj + 32 * y + r32;
+          if (to && i < g.I && j < g.J) to[(size_t)i * g.J + j] = acc[x][y][q];
+        }
+    if (sums) {                  // the threads of a column of pieces
+      __syncthreads();
+      double* s = reinterpret_cast<double*>(smem);
+      constexpr int E = TA::EIGHTS, R = 256 / E;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) s[(tid / E) * BM + tid % E * 8 + q] = col_sum[q];
+      __syncthreads();
+      if (tid < BM && i0 + tid < g.I) {
+        double t = 0.0;
+        for (int r = 0; r < R; ++r) t += s[r * BM + tid];
+        g.db[(size_t)rt * g.I + i0 + tid] = (float)t;
+      }
+    }
+    return;
+  }
+  // rows of results go through LDS, to be written eight values a thread
   __syncthreads();
-  const int g = s_g;
-  if (g >= p.G) return;
-  const long r0 = gl_begin(p, g) + (long)s_tile * GL_TILE, r1 = min(r0 + GL_TILE, gl_begin(p, g + 1));
-  const int n0 = blockIdx.y * GL_TILE;
-  const T* Wg = W + (size_t)g * K * N;
-  float acc[4][4] = {};
-  const int ti = (tid >> 4) * 4, tj = (tid & 15) * 4;
-  const long row = r0 + (tid >> 2) < r1 ? gl_row(p, r0 + (tid >> 2)) : -1;
-  for (int k0 = 0; k0 < K; k0 += GL_K) {
-    for (int q = 0; q < 4; ++q) {
-      const int k = (tid & 3) * 4 + q, n = tid >> 2;
-      sx[k][tid >> 2] = row >= 0 && k0 + k < K ? (float)x[row * xs + k0 + k] : 0.0f;
-      const bool in = n0 + n < N && k0 + k < K;
-      sw[k][n] = !in ? 0.0f : BACK ? (float)Wg[(size_t)(k0 + k) * N + n0 + n] : (float)Wg[(size_t)(n0 + n) * K + k0 + k];
+  float* tile_out = reinterpret_cast<float*>(smem);
+  constexpr int LD = BN + 4;
+#pragma unroll
+  for (int x = 0; x < MB; ++x)
+#pragma unroll
+    for (int y = 0; y < NB; ++y)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) tile_out[(wi + 32 * x + 8 * (q >> 2) + 4 * hh + (q & 3)) * LD + wj + 32 * y + r32] = acc[x][y][q];
+  __syncthreads();
+  const bool wide = ((uintptr_t)g.y | (g.y_stride * sizeof(T))) % 16 == 0;
+  for (int e = tid; e < BM * (BN / 8); e += 256) {
+    const int i = e / (BN / 8), jl = e % (BN / 8) * 8, j = j0 + jl;
+    if (r0 + i >= r1 || j >= g.J) continue;
+    T* to = g.y + gl_row(g.rows, r0 + i) * g.y_stride + j;
+    float v[8];
+    *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(tile_out + i * LD + jl);
+    *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(tile_out + i * LD + jl + 4);
+    const int valid = g.J - j;
+    if (KIND == GL_FORWARD && g.bias)
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        if (q < valid) v[q] += g.bias[(size_t)group * g.J + j + q];
+    if (wide && valid >= 8) {
+      rt_store<T, 8>(to, v);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        if (q < valid) to[q] = (T)v[q];
     }
-    __syncthreads();
-    for (int k = 0; k < GL_K; ++k)
-      for (int a = 0; a < 4; ++a)
-        for (int b = 0; b < 4; ++b) acc[a][b] += sx[k][ti + a] * sw[k][tj + b];
-    __syncthreads();
-  }
-  for (int a = 0; a < 4; ++a) {
-    if (r0 + ti + a >= r1) continue;
-    const long r = gl_row(p, r0 + ti + a);
-    for (int b = 0; b < 4; ++b)
-      if (n0 + tj + b < N) y[r * ys + n0 + tj + b] = (T)(acc[a][b] + (bias ? bias[(size_t)g * N + n0 + tj + b] : 0.0f));
   }
 }
 
-// dW_g: 64 outputs by 64 inputs, over all rows of the group; db_g by the first column of workgroups
-template <class T>
-__global__ __launch_bounds__(256) void gl_weights_kernel(GlRows p, const T* x, long xs, const T* dy, long dys, int K, int N, float* dW,
-                                                         float* db) {
-  __shared__ float sx[GL_K][GL_TILE + 4], sd[GL_K][GL_TILE + 4];
-  const int tid = threadIdx.x, g = blockIdx.z;
-  const long r0 = gl_begin(p, g), r1 = gl_begin(p, g + 1);
-  const int k0 = blockIdx.x * GL_TILE, n0 = blockIdx.y * GL_TILE;
-  float acc[4][4] = {}, sum[4] = {};
-  const int ti = (tid >> 4) * 4, tj = (tid & 15) * 4;
-  for (long r = r0; r < r1; r += GL_K) {
-    const int k = tid >> 4;
-    const long row = r + k < r1 ? gl_row(p, r + k) : -1;
-    for (int q = 0; q < 4; ++q) {
-      const int c = (tid & 15) * 4 + q;
-      sx[k][c] = row >= 0 && k0 + c < K ? (float)x[row * xs + k0 + c] : 0.0f;
-      sd[k][c] = row >= 0 && n0 + c < N ? (float)dy[row * dys + n0 + c] : 0.0f;
-    }
-    __syncthreads();
-    for (int j = 0; j < GL_K; ++j)
-      for (int a = 0; a < 4; ++a) {
-        sum[a] += sd[j][ti + a];
-        for (int b = 0; b < 4; ++b) acc[a][b] += sd[j][ti + a] * sx[j][tj + b];
-      }
-    __syncthreads();
-  }
-  for (int a = 0; a < 4; ++a) {
-    if (n0 + ti + a >= N) continue;
-    for (int b = 0; b < 4; ++b)
-      if (dW && k0 + tj + b < K) dW[((size_t)g * N + n0 + ti + a) * K + k0 + tj + b] = acc[a][b];
-    if (db && k0 == 0 && tj == 0) db[(size_t)g * N + n0 + ti + a] = sum[a];
-  }
+// sums of the slots of every group; n values a slot
+__global__ __launch_bounds__(256) void gl_join_kernel(GlRows p, long chunk, const float* part, float* out, long n) {
+  const int g = blockIdx.y;
+  const long i = (long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const long b = gl_begin(p, g), e = gl_begin(p, g + 1);
+  float t = 0.0f;
+  if (b < e)
+#pragma unroll 4
+    for (long c = b / chunk; c <= (e - 1) / chunk; ++c) t += part[(size_t)(c + g) * n + i];
+  out[(size_t)g * n + i] = t;
 }
 
 int gl_check(egnn_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32_t K, int32_t N, int32_t G, const int32_t* ptr) {
@@ -198,28 +553,100 @@ int gl_check(egnn_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32_t K
   return EGNN_OK;
 }
 
-template <class T>
-int gl_forward(egnn_ctx* ctx, const GlRows& p, const void* x, int64_t xs, const void* W, const float* bias, int K, int N, void* y,
-               int64_t ys, hipStream_t st) {
-  const dim3 grid((unsigned)((p.n + GL_TILE - 1) / GL_TILE + p.G), (N + GL_TILE - 1) / GL_TILE);
-  hipLaunchKernelGGL((gl_rows_kernel<T, false>), grid, dim3(256), 0, st, p, (const T*)x, (long)xs, (const T*)W, bias, K, N, (T*)y,
-                     (long)ys);
+size_t gl_align(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// Rows of one slot of the weight gradient: enough slots that the launch fills the compute units three times, of at least 256 rows
+// (below that a slot's partial result is longer than what it reads).
+struct GlSplit { long chunk; int slots; size_t weights, bytes; };
+GlSplit gl_split(int64_t n, int G, int K, int N) {
+  GlSplit s;
+  const long tiles = (long)((N + 63) / 64) * ((K + 63) / 64);
+  long chunks = (3 * EGNN_CUS + tiles - 1) / tiles - G;
+  if (chunks > n / 256) chunks = n / 256;
+  if (chunks < 1) chunks = 1;
+  s.chunk = n ? (n + chunks - 1) / chunks : 1;
+  s.slots = chunks > 1 ? (int)((n + s.chunk - 1) / s.chunk) + G : G;
+  s.weights = gl_align((size_t)s.slots * N * K * sizeof(float));
+  s.bytes = chunks > 1 ? s.weights + gl_align((size_t)s.slots * N * sizeof(float)) : 256;
+  return s;
+}
+
+template <class T, GlKind KIND, int BM, int BN, int KS>
+int gl_launch(egnn_ctx* ctx, const GlArgs<T>& g, long tiles, hipStream_t st) {
+  constexpr size_t stage = GlType<T>::PIECES * (GlTile<BM, KS, KIND == GL_WEIGHTS>::PLANE + GlTile<BN, KS, KIND != GL_FORWARD>::PLANE);
+  constexpr size_t out = KIND == GL_WEIGHTS ? (size_t)256 * 8 * sizeof(double) : (size_t)BM * (BN + 4) * sizeof(float);
+  constexpr size_t lds = 2 * stage > out ? 2 * stage : out;
+  static bool ready = false;      // (set again by two threads at once: to the same value)
+  if (!ready && lds > 65536) {
+    EGNN_HIP(ctx, hipFuncSetAttribute((const void*)gl_tile_kernel<T, KIND, BM, BN, KS>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    ready = true;
+  }
+  hipLaunchKernelGGL((gl_tile_kernel<T, KIND, BM, BN, KS>), dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(256), lds, st, g);
   EGNN_LAUNCH_CHECK(ctx, "grouped_linear");
   return EGNN_OK;
 }
 
+template <class T, GlKind KIND>
+int gl_rows(egnn_ctx* ctx, GlArgs<T> g, hipStream_t st) {
+  constexpr int KS = GlType<T>::PIECES == 1 ? 64 : 32;
+  auto tiles = [&](int bm, int bn) {
+    g.tiles_j = (g.J + bn - 1) / bn;
+    return ((g.rows.n + bm - 1) / bm + g.rows.G) * (long)g.tiles_j;
+  };
+  if constexpr (GlType<T>::PIECES == 1) {
+    const long wide = tiles(128, 128);
+    if (g.J > 64 && wide >= EGNN_CUS) return gl_launch<T, KIND, 128, 128, KS>(ctx, g, wide, st);
+  }
+  const long tall = tiles(128, 64);
+  if (tall >= EGNN_CUS) return gl_launch<T, KIND, 128, 64, KS>(ctx, g, tall, st);
+  const long small = tiles(64, 64);
+  return gl_launch<T, KIND, 64, 64, KS>(ctx, g, small, st);
+}
+
+template <class T>
+int gl_forward(egnn_ctx* ctx, const GlRows& p, const void* x, int64_t xs, const void* W, const float* bias, int K, int N, void* y,
+               int64_t ys, hipStream_t st) {
+  GlArgs<T> g{p, (const T*)x, (const T*)W, xs, 0, 0, N, K, (T*)y, ys, bias, nullptr, nullptr, 0, 0};
+  return gl_rows<T, GL_FORWARD>(ctx, g, st);
+}
+
 template <class T>
 int gl_backward(egnn_ctx* ctx, const GlRows& p, const void* x, int64_t xs, const void* W, const void* dy, int64_t dys, int K, int N,
-                void* dx, int64_t dxs, float* dW, float* db, hipStream_t st) {
+                void* dx, int64_t dxs, float* dW, float* db, void* ws, hipStream_t st) {
   if (dx && p.n) {
-    const dim3 grid((unsigned)((p.n + GL_TILE - 1) / GL_TILE + p.G), (K + GL_TILE - 1) / GL_TILE);
-    hipLaunchKernelGGL((gl_rows_kernel<T, true>), grid, dim3(256), 0, st, p, (const T*)dy, (long)dys, (const T*)W, (const float*)nullptr,
-                       N, K, (T*)dx, (long)dxs);
-    EGNN_LAUNCH_CHECK(ctx, "grouped_linear_backward");
+    GlArgs<T> g{p, (const T*)dy, (const T*)W, dys, 0, 0, K, N, (T*)dx, dxs, nullptr, nullptr, nullptr, 0, 0};
+    if (int rc = gl_rows<T, GL_INPUT>(ctx, g, st)) return rc;
   }
-  if (dW || db) {
-    const dim3 grid((K + GL_TILE - 1) / GL_TILE, (N + GL_TILE - 1) / GL_TILE, p.G);
-    hipLaunchKernelGGL((gl_weights_kernel<T>), grid, dim3(256), 0, st, p, (const T*)x, (long)xs, (const T*)dy, (long)dys, K, N, dW, db);
+  if (!dW && !db) return EGNN_OK;
+  const GlSplit s = gl_split(p.n, p.G, K, N);
+  const bool join = s.slots > p.G;
+  float *pw = dW, *pb = db;
+  if (join) {
+    pw = dW ? (float*)ws : nullptr;
+    pb = db ? (float*)((char*)ws + s.weights) : nullptr;
+  }
+  GlArgs<T> g{p, (const T*)dy, (const T*)x, dys, xs, N, K, 0, nullptr, 0, nullptr, pw, pb, 0, s.chunk};
+  constexpr int KS = GlType<T>::PIECES == 1 ? 32 : 16;
+  auto tiles = [&](int bm, int bn) {
+    g.tiles_j = ((N + bm - 1) / bm) * (dW ? (K + bn - 1) / bn : 1);      // db alone: the first column of tiles
+    return (long)s.slots * g.tiles_j;
+  };
+  bool done = false;
+  if constexpr (GlType<T>::PIECES == 1) {
+    const long wide = tiles(128, 128);
+    if (N > 64 && K > 64 && wide >= EGNN_CUS) {
+      if (int rc = gl_launch<T, GL_WEIGHTS, 128, 128, KS>(ctx, g, wide, st)) return rc;
+      done = true;
+    }
+  }
+  if (!done) {
+    const long small = tiles(64, 64);
+    if (int rc = gl_launch<T, GL_WEIGHTS, 64, 64, 2 * KS>(ctx, g, small, st)) return rc;
+  }
+  if (join) {
+    const long n = (long)N * K;
+    if (dW) hipLaunchKernelGGL(gl_join_kernel, dim3((unsigned)((n + 255) / 256), p.G), dim3(256), 0, st, p, s.chunk, pw, dW, n);
+    if (db) hipLaunchKernelGGL(gl_join_kernel, dim3((N + 255) / 256, p.G), dim3(256), 0, st, p, s.chunk, pb, db, (long)N);
     EGNN_LAUNCH_CHECK(ctx, "grouped_linear_backward");
   }
   return EGNN_OK;
@@ -260,7 +687,7 @@ extern "C" int egnn_grouped_linear_workspace_bytes(const egnn_ctx* ctx, int64_t 
   if (!ctx || !bytes || n_rows < 0 || n_rows > 0x7fffffff || n_groups < 1 || n_groups > 65535 || n_in < 1 || n_in > 65536 || n_out < 1 ||
       n_out > 65536)
     return egnn_fail(const_cast<egnn_ctx*>(ctx), EGNN_EINVAL, "grouped_linear_workspace_bytes: bad argument");
-  *bytes = 256;
+  *bytes = gl_split(n_rows, n_groups, n_in, n_out).bytes;
   return EGNN_OK;
 }
 
@@ -294,7 +721,7 @@ extern "C" int egnn_grouped_linear_backward(egnn_ctx* ctx, int32_t dtype, const 
     return egnn_fail(ctx, EGNN_EWS, "grouped_linear_backward: workspace too small or not 256-byte aligned");
   const GlRows p{n_rows, n_groups, ptr, perm};
   hipStream_t st = (hipStream_t)stream;
-  if (dtype == EGNN_F32) return gl_backward<float>(ctx, p, x, x_stride, W, dy, dy_stride, n_in, n_out, dx, dx_stride, dW, db, st);
-  if (dtype == EGNN_F16) return gl_backward<_Float16>(ctx, p, x, x_stride, W, dy, dy_stride, n_in, n_out, dx, dx_stride, dW, db, st);
-  return gl_backward<__bf16>(ctx, p, x, x_stride, W, dy, dy_stride, n_in, n_out, dx, dx_stride, dW, db, st);
+  if (dtype == EGNN_F32) return gl_backward<float>(ctx, p, x, x_stride, W, dy, dy_stride, n_in, n_out, dx, dx_stride, dW, db, ws, st);
+  if (dtype == EGNN_F16) return gl_backward<_Float16>(ctx, p, x, x_stride, W, dy, dy_stride, n_in, n_out, dx, dx_stride, dW, db, ws, st);
+  return gl_backward<__bf16>(ctx, p, x, x_stride, W, dy, dy_stride, n_in, n_out, dx, dx_stride, dW, db, ws, st);
 }
