@@ -141,38 +141,60 @@ __device__ __forceinline__ gl_f16v gl_product(const uint4 (&a)[3], const uint4 (
   return gl_mfma(a[0], b[0], c, t);
 }
 
-// eight values at p (aligned to one value), of which the first `valid` are there; the others are zero
+// Eight values at p, aligned to one value.  Loads are never under a condition: a condition would end in a wait for the load.  At the end of
+// a row the last eight values of the row are taken instead (it has that many, or the row is narrow) and moved down by the places too many.
 typedef uint32_t gl_u4 __attribute__((ext_vector_type(4), aligned(2)));
 __device__ __forceinline__ uint4 gl_load16(const void* p) {
   const gl_u4 v = *reinterpret_cast<const gl_u4*>(p);
   return make_uint4(v.x, v.y, v.z, v.w);
 }
 template <class T>
-__device__ __forceinline__ void gl_load(const T* p, int valid, uint4& r) {
-  r = make_uint4(0, 0, 0, 0);
-  if (valid >= 8) {
-    r = gl_load16(p);
-  } else if (valid > 0) {
-    uint32_t w[4] = {};
-#pragma unroll
-    for (int q = 0; q < 7; ++q)
-      if (q < valid) w[q >> 1] |= (uint32_t) reinterpret_cast<const uint16_t*>(p)[q] << (16 * (q & 1));
-    r = make_uint4(w[0], w[1], w[2], w[3]);
-  }
+__device__ __forceinline__ void gl_load(const T* p, uint4& r) { r = gl_load16(p); }
+__device__ __forceinline__ void gl_load(const float* p, GlType<float>::Raw& r) {
+  r.a = gl_load16(p);
+  r.b = gl_load16(p + 4);
 }
-__device__ __forceinline__ void gl_load(const float* p, int valid, GlType<float>::Raw& r) {
-  r.a = r.b = make_uint4(0, 0, 0, 0);
-  if (valid >= 8) {
-    r.a = gl_load16(p);
-    r.b = gl_load16(p + 4);
-  } else if (valid > 0) {
-    uint32_t w[8] = {};
+// a row of fewer than eight values
+template <class T>
+__device__ __forceinline__ void gl_load_narrow(const T* p, int valid, uint4& r) {
+  uint32_t w[4] = {};
 #pragma unroll
-    for (int q = 0; q < 7; ++q)
-      if (q < valid) w[q] = __float_as_uint(p[q]);
-    r.a = make_uint4(w[0], w[1], w[2], w[3]);
-    r.b = make_uint4(w[4], w[5], w[6], w[7]);
-  }
+  for (int q = 0; q < 7; ++q)
+    if (q < valid) w[q >> 1] |= (uint32_t) reinterpret_cast<const uint16_t*>(p)[q] << (16 * (q & 1));
+  r = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void gl_load_narrow(const float* p, int valid, GlType<float>::Raw& r) {
+  uint32_t w[8] = {};
+#pragma unroll
+  for (int q = 0; q < 7; ++q)
+    if (q < valid) w[q] = __float_as_uint(p[q]);
+  r.a = make_uint4(w[0], w[1], w[2], w[3]);
+  r.b = make_uint4(w[4], w[5], w[6], w[7]);
+}
+// moves the values down by n places, zeros behind them (n >= 8: nothing is left)
+template <int N, int BY>
+__device__ __forceinline__ void gl_down(uint32_t (&w)[N], bool yes) {
+#pragma unroll
+  for (int q = 0; q < N; ++q) w[q] = yes ? (q + BY < N ? w[q + BY] : 0u) : w[q];
+}
+__device__ __forceinline__ void gl_shift(uint4& r, int n) {
+  uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (n & 1) w[q] = w[q] >> 16 | (q < 3 ? w[q + 1] << 16 : 0u);
+  gl_down<4, 1>(w, n & 2);
+  gl_down<4, 2>(w, n & 4);
+  gl_down<4, 4>(w, n >= 8);
+  r = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void gl_shift(GlType<float>::Raw& r, int n) {
+  uint32_t w[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
+  gl_down<8, 1>(w, n & 1);
+  gl_down<8, 2>(w, n & 2);
+  gl_down<8, 4>(w, n & 4);
+  gl_down<8, 8>(w, n >= 8);
+  r.a = make_uint4(w[0], w[1], w[2], w[3]);
+  r.b = make_uint4(w[4], w[5], w[6], w[7]);
 }
 // -> pieces
 __device__ __forceinline__ void gl_cut(uint4 r, uint4 (&to)[1]) { to[0] = r; }
@@ -339,74 +361,104 @@ __global__ __launch_bounds__(256) void gl_tile_kernel(GlArgs<T> g) {
     return;
   }
 
-  // what this thread stages
-  const T *pa[TA::CHUNKS], *pb[TB::CHUNKS];
-  int na[TA::CHUNKS], nb[TB::CHUNKS];                 // GL_FORWARD, GL_INPUT: values to the end of the row (or the column), 0: no row
-  long ra[TA::CHUNKS], rb[TB::CHUNKS];                // GL_WEIGHTS: the rows of the next turn to be fetched, -1: none
-  const long weights = KIND == GL_WEIGHTS ? 0 : (long)group * g.J * g.K;
-#pragma unroll
-  for (int c = 0; c < TA::CHUNKS; ++c) {
-    if (KIND == GL_WEIGHTS) {
-      pa[c] = g.a + i0 + TA::col(c);
-      na[c] = g.I - i0 - TA::col(c);
-      const long r = r0 + TA::row(c);
-      ra[c] = r < r1 ? gl_row(g.rows, r) : -1;
-    } else {
-      const long r = r0 + TA::row(c);
-      pa[c] = g.a + (r < r1 ? gl_row(g.rows, r) * g.a_stride : 0) + TA::col(c);
-      na[c] = r < r1 ? g.K - TA::col(c) : 0;
-    }
-  }
-#pragma unroll
-  for (int c = 0; c < TB::CHUNKS; ++c) {
-    if (KIND == GL_WEIGHTS) {
-      pb[c] = g.b + j0 + TB::col(c);
-      nb[c] = g.J - j0 - TB::col(c);
-      const long r = r0 + TB::row(c);
-      rb[c] = r < r1 ? gl_row(g.rows, r) : -1;
-    } else if (KIND == GL_INPUT) {                    // W[k][j]
-      pb[c] = g.b + weights + (long)TB::row(c) * g.J + j0 + TB::col(c);
-      nb[c] = g.J - j0 - TB::col(c);
-    } else {                                          // W[j][k]
-      pb[c] = g.b + weights + (long)(j0 + TB::row(c)) * g.K + TB::col(c);
-      nb[c] = j0 + TB::row(c) < g.J ? g.K - TB::col(c) : 0;
-    }
-  }
-  Raw a[TA::CHUNKS], b[TB::CHUNKS];
-  auto fetch = [&](int turn) {
+  // What this thread stages.  Rows of the result past its end, and columns past its last, may hold anything (the last ones again): they do
+  // not reach others.  Only contraction indices past the end have to be zero, in both operands: they end in the last turn.
+  const int turns = (int)(KIND == GL_WEIGHTS ? (r1 - r0 + KS - 1) / KS : (g.K + KS - 1) / KS);
+  const T *pa[TA::CHUNKS], *pb[TB::CHUNKS];           // row, or column for rows that change with the turn
+  long ra[TA::CHUNKS], rb[TB::CHUNKS];                // GL_WEIGHTS: the rows of the next turn to be fetched
+  int da[TA::CHUNKS], db[TB::CHUNKS];                 // across: places the columns are moved down at the end of a row
+  bool edge_a = false, edge_b = false;
+  const T* const W = KIND == GL_WEIGHTS ? nullptr : g.b + (long)group * g.J * g.K;
+  auto next_row = [&](long r) { return gl_row(g.rows, min(r, r1 - 1)); };
+  const bool narrow_a = (KIND == GL_WEIGHTS ? g.I : g.K) < 8, narrow_b = (KIND == GL_FORWARD ? g.K : g.J) < 8;
+  if (turns > 0) {
 #pragma unroll
     for (int c = 0; c < TA::CHUNKS; ++c) {
+      const long r = next_row(r0 + TA::row(c));
       if (KIND == GL_WEIGHTS) {
-        gl_load(pa[c] + (ra[c] < 0 ? 0 : ra[c]) * g.a_stride, ra[c] < 0 ? 0 : na[c], a[c]);
-        const long r = r0 + (long)(turn + 1) * KS + TA::row(c);
-        ra[c] = r < r1 ? gl_row(g.rows, r) : -1;
+        const int col = i0 + TA::col(c), from = narrow_a ? col : min(col, g.I - 8);
+        pa[c] = g.a + min(from, g.I - 1);
+        da[c] = col - from;
+        ra[c] = r;
       } else {
-        gl_load(pa[c], na[c], a[c]);
-        pa[c] += KS;
-        na[c] -= KS;
+        pa[c] = g.a + r * g.a_stride;
       }
     }
 #pragma unroll
     for (int c = 0; c < TB::CHUNKS; ++c) {
-      if (KIND == GL_WEIGHTS) {
-        gl_load(pb[c] + (rb[c] < 0 ? 0 : rb[c]) * g.b_stride, rb[c] < 0 ? 0 : nb[c], b[c]);
-        const long r = r0 + (long)(turn + 1) * KS + TB::row(c);
-        rb[c] = r < r1 ? gl_row(g.rows, r) : -1;
-      } else if (KIND == GL_INPUT) {
-        gl_load(pb[c], turn * KS + TB::row(c) < g.K ? nb[c] : 0, b[c]);
-        pb[c] += (long)KS * g.J;
-      } else {
-        gl_load(pb[c], nb[c], b[c]);
-        pb[c] += KS;
-        nb[c] -= KS;
+      const int col = j0 + TB::col(c), from = narrow_b ? col : min(col, g.J - 8);
+      if (KIND == GL_FORWARD) {                       // W[j][k]
+        pb[c] = W + (long)min(j0 + TB::row(c), g.J - 1) * g.K;
+      } else {                                        // W[k][j], x[r][j]
+        pb[c] = (KIND == GL_INPUT ? W : g.b) + min(from, g.J - 1);
+        db[c] = col - from;
+        if (KIND == GL_WEIGHTS) rb[c] = next_row(r0 + TB::row(c));
       }
+    }
+    edge_a = KIND == GL_WEIGHTS && i0 + BM > g.I && !narrow_a;
+    edge_b = KIND != GL_FORWARD && j0 + BN > g.J && !narrow_b;
+  }
+  Raw a[TA::CHUNKS], b[TB::CHUNKS];
+  auto fetch = [&](int turn) {
+    if (narrow_a) {
+#pragma unroll
+      for (int c = 0; c < TA::CHUNKS; ++c) {
+        const int k = turn * KS + TA::col(c);
+        if (KIND == GL_WEIGHTS) gl_load_narrow(pa[c] + ra[c] * g.a_stride, g.I - i0 - TA::col(c), a[c]);
+        else gl_load_narrow(pa[c] + min(k, g.K - 1), g.K - k, a[c]);
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < TA::CHUNKS; ++c) gl_load(KIND == GL_WEIGHTS ? pa[c] + ra[c] * g.a_stride : pa[c] + min(turn * KS + TA::col(c), g.K - 8), a[c]);
+    }
+    if (narrow_b) {
+#pragma unroll
+      for (int c = 0; c < TB::CHUNKS; ++c) {
+        const int k = turn * KS + (KIND == GL_FORWARD ? TB::col(c) : TB::row(c));
+        if (KIND == GL_FORWARD) gl_load_narrow(pb[c] + min(k, g.K - 1), g.K - k, b[c]);
+        else gl_load_narrow(pb[c] + (KIND == GL_WEIGHTS ? rb[c] * g.b_stride : (long)min(k, g.K - 1) * g.J), g.J - j0 - TB::col(c), b[c]);
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < TB::CHUNKS; ++c) {
+        if (KIND == GL_FORWARD) gl_load(pb[c] + min(turn * KS + TB::col(c), g.K - 8), b[c]);
+        else gl_load(pb[c] + (KIND == GL_WEIGHTS ? rb[c] * g.b_stride : (long)min(turn * KS + TB::row(c), g.K - 1) * g.J), b[c]);
+      }
+    }
+    if (KIND == GL_WEIGHTS) {
+#pragma unroll
+      for (int c = 0; c < TA::CHUNKS; ++c) ra[c] = next_row(r0 + (long)(turn + 1) * KS + TA::row(c));
+#pragma unroll
+      for (int c = 0; c < TB::CHUNKS; ++c) rb[c] = next_row(r0 + (long)(turn + 1) * KS + TB::row(c));
     }
   };
   float turn_sum[8];
   double col_sum[8] = {};
   const bool sums = KIND == GL_WEIGHTS && g.db && j0 == 0;
-  auto stage = [&](int at) {
-    char* to = smem + at * STAGE;
+  auto stage = [&](int turn) {
+    char* to = smem + (turn & 1) * STAGE;
+    const bool last = turn + 1 == turns;
+    const long left = (KIND == GL_WEIGHTS ? r1 - r0 : (long)g.K) - (long)turn * KS;      // contraction indices from this turn on
+    if (KIND == GL_WEIGHTS && edge_a) {
+#pragma unroll
+      for (int c = 0; c < TA::CHUNKS; ++c) gl_shift(a[c], da[c]);
+    }
+    if (KIND != GL_FORWARD && edge_b) {
+#pragma unroll
+      for (int c = 0; c < TB::CHUNKS; ++c) gl_shift(b[c], db[c]);
+    }
+    if (last && left < KS) {
+#pragma unroll
+      for (int c = 0; c < TA::CHUNKS; ++c) {
+        if (KIND == GL_WEIGHTS) gl_shift(a[c], TA::row(c) < left ? 0 : 8);
+        else if (!narrow_a) gl_shift(a[c], max(0, TA::col(c) + 8 - (int)left));
+      }
+#pragma unroll
+      for (int c = 0; c < TB::CHUNKS; ++c) {
+        if (KIND != GL_FORWARD) gl_shift(b[c], TB::row(c) < left ? 0 : 8);
+        else if (!narrow_b) gl_shift(b[c], max(0, TB::col(c) + 8 - (int)left));
+      }
+    }
 #pragma unroll
     for (int q = 0; q < 8; ++q) turn_sum[q] = 0.0f;
 #pragma unroll
@@ -437,7 +489,6 @@ __global__ __launch_bounds__(256) void gl_tile_kernel(GlArgs<T> g) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[x][y][i] = 0.0f;
   const int wi = (wave >> 1) * (BM / 2), wj = (wave & 1) * (BN / 2);
-  const int turns = (int)(KIND == GL_WEIGHTS ? (r1 - r0 + KS - 1) / KS : (g.K + KS - 1) / KS);
   if (turns > 0) {
     fetch(0);
     stage(0);
@@ -464,7 +515,7 @@ __global__ __launch_bounds__(256) void gl_tile_kernel(GlArgs<T> g) {
         for (int y = 0; y < NB; ++y) acc[x][y] = gl_product<T>(fa[x], fb[y], acc[x][y]);
     }
     if (k + 1 < turns) {
-      stage((k + 1) & 1);
+      stage(k + 1);
       if (k + 2 < turns) fetch(k + 2);
     }
   }
