@@ -547,30 +547,38 @@ __global__ __launch_bounds__(256) void gl_tile_kernel(GlArgs<T> g) {
     }
     return;
   }
-  // rows of results go through LDS, to be written eight values a thread
-  __syncthreads();
+  // Rows of results go through LDS, to be written eight values a thread.  Whatever has to be loaded is loaded before the first of them is
+  // stored: loads and stores return in order, and a load behind a store would wait for it.
+  constexpr int LD = BN + 4, ACROSS = BN / 8, ITEMS = BM * ACROSS / 256;
+  const int jl = tid % ACROSS * 8, j = j0 + jl, valid = g.J - j;
+  long row[ITEMS];
+  float bias[8];
+#pragma unroll
+  for (int e = 0; e < ITEMS; ++e) row[e] = gl_row(g.rows, min(r0 + tid / ACROSS + e * (256 / ACROSS), r1 - 1));
+#pragma unroll
+  for (int q = 0; q < 8; ++q) bias[q] = KIND == GL_FORWARD && g.bias ? g.bias[(size_t)group * g.J + min(j + q, g.J - 1)] : 0.0f;
+  rb_release_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
   float* tile_out = reinterpret_cast<float*>(smem);
-  constexpr int LD = BN + 4;
 #pragma unroll
   for (int x = 0; x < MB; ++x)
 #pragma unroll
     for (int y = 0; y < NB; ++y)
 #pragma unroll
       for (int q = 0; q < 16; ++q) tile_out[(wi + 32 * x + 8 * (q >> 2) + 4 * hh + (q & 3)) * LD + wj + 32 * y + r32] = acc[x][y][q];
-  __syncthreads();
+  rb_release_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
   const bool wide = ((uintptr_t)g.y | (g.y_stride * sizeof(T))) % 16 == 0;
-  for (int e = tid; e < BM * (BN / 8); e += 256) {
-    const int i = e / (BN / 8), jl = e % (BN / 8) * 8, j = j0 + jl;
-    if (r0 + i >= r1 || j >= g.J) continue;
-    T* to = g.y + gl_row(g.rows, r0 + i) * g.y_stride + j;
+#pragma unroll
+  for (int e = 0; e < ITEMS; ++e) {
+    const int i = tid / ACROSS + e * (256 / ACROSS);
     float v[8];
     *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(tile_out + i * LD + jl);
     *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(tile_out + i * LD + jl + 4);
-    const int valid = g.J - j;
-    if (KIND == GL_FORWARD && g.bias)
 #pragma unroll
-      for (int q = 0; q < 8; ++q)
-        if (q < valid) v[q] += g.bias[(size_t)group * g.J + j + q];
+    for (int q = 0; q < 8; ++q) v[q] += bias[q];
+    if (r0 + i >= r1 || valid <= 0) continue;
+    T* to = g.y + row[e] * g.y_stride + j;
     if (wide && valid >= 8) {
       rt_store<T, 8>(to, v);
     } else {

@@ -12,6 +12,7 @@
 // Results in bfloat16 of wide updates (both sides at least OU_ONE_PIECE) need no lo in the products: see ou_pieces().  The largest term
 // of a step, a x, then stays out of them: x^T keeps both pieces, and p is b g + c g^2 alone.
 #include "row_types.h"
+#include "stream_gemm.h"
 #include <math.h>
 #include <type_traits>
 
@@ -144,6 +145,12 @@ __device__ __forceinline__ void ou_loads_then_barrier() {
   asm volatile("" ::: "memory");
 }
 
+// waits for LDS alone, not for stores to memory
+__device__ __forceinline__ void ou_lds_barrier() {
+  rb_release_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // C = A B^T of one tile TILE x TILE: four waves, each a quarter (TILE / 2 squared) in 32 x 32 blocks.  64 contraction indices a
 // turn, brought straight into one of STAGES LDS buffers, STAGES - 1 turns ahead: with one wave per SIMD nothing else hides the way to
 // memory.  A row of 128 bytes lies in LDS as eight pieces of 16 bytes, piece c at place c ^ (row & 7): eight lanes that read the same
@@ -253,51 +260,79 @@ __global__ __launch_bounds__(256) void ou_product_kernel(OuShape p, OuOperands o
       for (int r = 0; r < 4; ++r)
         tile[slot(wj + 32 * y + r32, (wi + 32 * x + 8 * r + 4 * hh) >> 2)] =
             make_float4(acc[x][y][4 * r], acc[x][y][4 * r + 1], acc[x][y][4 * r + 2], acc[x][y][4 * r + 3]);
-  __syncthreads();
+  // Whatever has to be loaded is loaded before the first result is stored: loads and stores return in order, and a load behind a store
+  // would wait for it (so did barriers that wait for stores).
   const size_t plane_c = (size_t)o.I * o.J;
-  constexpr int ACROSS = TILE / 8;                   // threads along a row, eight values each
-  for (int e = tid; e < TILE * ACROSS; e += 256) {
-    const int jl = e / ACROSS, il = (e % ACROSS) * 8, i = i0 + il, j = j0 + jl;
-    if (i >= o.I || j >= o.J) continue;
-    const float4 lo4 = tile[slot(jl, il >> 2)], hi4 = tile[slot(jl, (il >> 2) + 1)];
+  constexpr int ACROSS = TILE / 8, ITEMS = TILE * ACROSS / 256;   // threads along a row, eight values each
+  constexpr bool OLD = WHAT == OU_POLY || (STEP && P == 1);       // + b g, or + a x
+  const int n = p.n, m = p.m, across = tid % ACROSS * 8;
+  ou_h8 oh[OLD ? ITEMS : 1], ol[OLD && PB == 2 ? ITEMS : 1];
+  auto along_i = [&](int e, int& i, int& j, int& jl) {            // eight i of one j
+    jl = tid / ACROSS + e * (256 / ACROSS);
+    i = i0 + across;
+    j = j0 + jl;
+    return i < o.I && j < o.J;
+  };
+  if (OLD)
+#pragma unroll
+    for (int e = 0; e < ITEMS; ++e) {
+      int i, j, jl;
+      along_i(e, i, j, jl);
+      const _Float16* old = (STEP ? Bm : A) + (size_t)min(j, o.J - 1) * o.I + min(i, o.I - 8);
+      oh[e] = *(const ou_h8*)old;
+      if (PB == 2) ol[e] = *(const ou_h8*)(old + plane_c);
+    }
+  const bool flip = WHAT == OU_UPDATE || (WHAT == OU_LAST && !p.tall);     // rows of (another) result run along j
+  float keep[WHAT == OU_LAST ? ITEMS : 1][8];
+  if (WHAT == OU_LAST && out.W)
+#pragma unroll
+    for (int e = 0; e < ITEMS; ++e) {
+      const int r = (flip ? i0 : j0) + tid / ACROSS + e * (256 / ACROSS), c = (flip ? j0 : i0) + across;
+      const float* w = out.W + z * n * m + (size_t)min(r, (flip ? n : m) - 1) * p.cols;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) keep[e][q] = out.keep * w[min(c + q, p.cols - 1)];
+    }
+  // (r, c) of the caller's matrix
+  auto write_last = [&](int e, int r, int c, float (&v)[8]) {
+    if (r >= p.rows || c >= p.cols) return;
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (out.W) v[q] = keep[e][q] - out.scale * v[q];
+    T* to = out.y + z * n * m + (size_t)r * p.cols + c;
+    if (out.eights) {
+      rt_store<T, 8>(to, v);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        if (c + q < p.cols) to[q] = (T)v[q];
+    }
+  };
+  ou_lds_barrier();
+#pragma unroll
+  for (int e = 0; e < ITEMS; ++e) {
+    int i, j, jl;
+    if (!along_i(e, i, j, jl)) continue;
+    const float4 lo4 = tile[slot(jl, across >> 2)], hi4 = tile[slot(jl, (across >> 2) + 1)];
     float v[8] = {lo4.x, lo4.y, lo4.z, lo4.w, hi4.x, hi4.y, hi4.z, hi4.w};
 #pragma unroll
     for (int q = 0; q < 8; ++q) v[q] *= unscale;
-    const size_t at = (size_t)j * o.I + i;
-    if (WHAT == OU_POLY || (STEP && P == 1)) {       // + b g, or + a x
-      const _Float16* old = (STEP ? Bm : A) + at;
-      const ou_h8 oh = *(const ou_h8*)old;
-      ou_h8 ol = {};
-      if (PB == 2) ol = *(const ou_h8*)(old + plane_c);
+    if (OLD)
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        const float g = (float)oh[q] + (float)ol[q];
+        const float g = (float)oh[e][q] + (PB == 2 ? (float)ol[e][q] : 0.0f);
         if (STEP) {
           v[q] += (OU_A / OU_SX) * g;
         } else {
           v[q] = OU_C * v[q] + (OU_B / OU_SG) * g;
-          if (P == 2 && i + q == j && j < p.n) v[q] += OU_A;
+          if (P == 2 && i + q == j && j < n) v[q] += OU_A;
         }
       }
+    if (flip) {
+      tile[slot(jl, across >> 2)] = make_float4(v[0], v[1], v[2], v[3]);
+      tile[slot(jl, (across >> 2) + 1)] = make_float4(v[4], v[5], v[6], v[7]);
     }
     if (WHAT == OU_LAST) {
-      const int n = p.n, m = p.m;
-      if (!p.tall) {                                 // rows of the result run along j: below
-        tile[slot(jl, il >> 2)] = make_float4(v[0], v[1], v[2], v[3]);
-        tile[slot(jl, (il >> 2) + 1)] = make_float4(v[4], v[5], v[6], v[7]);
-      } else if (j < m && i < n) {
-        const size_t to = z * n * m + (size_t)j * n + i;
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-          if (out.W && i + q < n) v[q] = out.keep * out.W[to + q] - out.scale * v[q];
-        if (out.eights) {
-          rt_store<T, 8>(out.y + to, v);
-        } else {
-#pragma unroll
-          for (int q = 0; q < 8; ++q)
-            if (i + q < n) out.y[to + q] = (T)v[q];
-        }
-      }
+      if (!flip) write_last(e, j, i, v);
       continue;
     }
     ou_h8 hi, lo;
@@ -307,51 +342,34 @@ __global__ __launch_bounds__(256) void ou_product_kernel(OuShape p, OuOperands o
       ou_cut(v[q] * scale, h, l);
       hi[q] = h; lo[q] = l;
     }
-    _Float16* c = o.C + z * (STEP ? 2 : P) * plane_c + at;
+    _Float16* c = o.C + z * (STEP ? 2 : P) * plane_c + (size_t)j * o.I + i;
     *(ou_h8*)c = hi;
     if (STEP || P == 2) *(ou_h8*)(c + plane_c) = lo;
-    if (WHAT == OU_UPDATE && P == 1) {
-      tile[slot(jl, il >> 2)] = make_float4(v[0], v[1], v[2], v[3]);
-      tile[slot(jl, (il >> 2) + 1)] = make_float4(v[4], v[5], v[6], v[7]);
-    }
   }
-  if (WHAT == OU_UPDATE || (WHAT == OU_LAST && !p.tall)) {    // the same along j
-    const float one = WHAT == OU_UPDATE && P == 2 ? unscale : 1.0f;
-    __syncthreads();
-    const float* flat = (const float*)smem;
-    for (int e = tid; e < TILE * ACROSS; e += 256) {
-      const int il = e / ACROSS, jl = (e % ACROSS) * 8, i = i0 + il, j = j0 + jl;
-      if (i >= o.I || j >= o.J) continue;
-      float v[8];
+  if (!flip) return;
+  ou_lds_barrier();
+  const float* flat = (const float*)smem;
 #pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] = flat[4 * slot(jl + q, il >> 2) + (il & 3)] * one;
-      if (WHAT == OU_LAST) {
-        const int n = p.n, m = p.m;
-        if (i >= n) continue;
-        const size_t to = z * n * m + (size_t)i * m + j;
+  for (int e = 0; e < ITEMS; ++e) {                                // eight j of one i
+    const int il = tid / ACROSS + e * (256 / ACROSS), i = i0 + il, j = j0 + across;
+    if (i >= o.I || j >= o.J) continue;
+    float v[8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
-          if (out.W && j + q < m) v[q] = out.keep * out.W[to + q] - out.scale * v[q];
-        if (out.eights) {
-          if (j < m) rt_store<T, 8>(out.y + to, v);
-        } else {
-#pragma unroll
-          for (int q = 0; q < 8; ++q)
-            if (j + q < m) out.y[to + q] = (T)v[q];
-        }
-        continue;
-      }
-      ou_h8 hi, lo;
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        _Float16 h, l;
-        ou_cut(v[q] * scale, h, l);
-        hi[q] = h; lo[q] = l;
-      }
-      _Float16* ct = o.Ct + z * P * plane_c + (size_t)i * o.J + j;
-      *(ou_h8*)ct = hi;
-      if (P == 2) *(ou_h8*)(ct + plane_c) = lo;
+    for (int q = 0; q < 8; ++q) v[q] = flat[4 * slot(across + q, il >> 2) + (il & 3)];
+    if (WHAT == OU_LAST) {
+      write_last(e, i, j, v);
+      continue;
     }
+    ou_h8 hi, lo;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      _Float16 h, l;
+      ou_cut(v[q] * scale, h, l);
+      hi[q] = h; lo[q] = l;
+    }
+    _Float16* ct = o.Ct + z * P * plane_c + (size_t)i * o.J + j;
+    *(ou_h8*)ct = hi;
+    if (P == 2) *(ou_h8*)(ct + plane_c) = lo;
   }
 }
 
