@@ -589,17 +589,264 @@ __global__ __launch_bounds__(256) void gl_tile_kernel(GlArgs<T> g) {
   }
 }
 
-// sums of the slots of every group; n values a slot
-__global__ __launch_bounds__(256) void gl_join_kernel(GlRows p, long chunk, const float* part, float* out, long n) {
-  const int g = blockIdx.y;
-  const long i = (long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
+// ---- n_in and n_out of at most 64: the group's matrix stays in registers ------------------------------------------------------
+// A wave takes an equal share of the rows, group by group, 32 at a time, and nothing is shared between waves: no LDS tile, no barrier.  The
+// product is y^T = W x^T, so that a lane holds one row and writes its values four neighbouring ones at a time.  The next rows are under way
+// while the matrix cores work on these; what is left is the memory.
+// KB: contraction steps of 16, NB: output blocks of 32; 16 KB >= K, 32 NB >= J.
+template <class T, GlKind KIND, int KB, int NB>
+__global__ __launch_bounds__(256, 2) void gl_lean_rows_kernel(GlArgs<T> g, long share) {
+  constexpr int NP = GlType<T>::PIECES;
+  typedef typename GlType<T>::Raw Raw;
+  __shared__ __align__(16) float s_bias[4][32 * NB];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r32 = lane & 31, hh = lane >> 5;
+  const long first = ((long)blockIdx.x * 4 + wave) * share, end = min(first + share, g.rows.n);
+  int lo = 0, hi = g.rows.G - 1;                     // the last group that does not begin behind the first row
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (gl_begin(g.rows, mid) <= first) lo = mid; else hi = mid - 1;
+  }
+  const bool narrow = g.K < 8;
+  auto raw = [&](const T* row, int s, Raw& to) {      // eight values of a row from 16 s + 8 hh on, the row's last ones past its end
+    const int k = 16 * s + 8 * hh;
+    if (narrow) gl_load_narrow(row + min(k, g.K - 1), g.K - k, to);
+    else gl_load(row + min(k, g.K - 8), to);
+  };
+  auto edge = [&](int s, Raw& r) {
+    if (!narrow && 16 * KB > g.K) gl_shift(r, max(0, 16 * s + 8 * hh + 8 - g.K));
+  };
+  const bool wide = ((uintptr_t)g.y | (g.y_stride * sizeof(T))) % (4 * sizeof(T)) == 0;
+  for (int group = lo; group < g.rows.G; ++group) {
+    const long b = max(gl_begin(g.rows, group), first), e = min(gl_begin(g.rows, group + 1), end);
+    if (b >= end) break;
+    if (b >= e) continue;
+    // rows of the next tile first: their way to memory passes while the matrix is prepared
+    auto row_at = [&](long r) { return gl_row(g.rows, min(r + r32, e - 1)); };
+    long here = row_at(b), next = row_at(b + 32);
+    Raw x[KB];
+#pragma unroll
+    for (int s = 0; s < KB; ++s) raw(g.a + here * g.a_stride, s, x[s]);
+    uint4 w[KB][NB][NP];
+    const T* W = g.b + (size_t)group * g.J * g.K;
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      const int j = 32 * n + r32;
+#pragma unroll
+      for (int s = 0; s < KB; ++s) {
+        Raw r;
+        if (KIND == GL_FORWARD) {                     // W[j][k]
+          raw(W + (size_t)min(j, g.J - 1) * g.K, s, r);
+          edge(s, r);
+        } else {                                      // W[k][j]
+          T v[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            const int k = 16 * s + 8 * hh + q;
+            v[q] = W[(size_t)min(k, g.K - 1) * g.J + min(j, g.J - 1)];
+            if (k >= g.K) v[q] = (T)0.0f;
+          }
+          __builtin_memcpy(&r, v, sizeof(Raw));
+        }
+        gl_cut(r, w[s][n]);
+      }
+    }
+    if (KIND == GL_FORWARD) {
+      if (lane < 32 * NB) s_bias[wave][lane] = g.bias ? g.bias[(size_t)group * g.J + min(lane, g.J - 1)] : 0.0f;
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+    }
+    for (long r = b; r < e; r += 32) {
+      uint4 v[KB][NP];
+#pragma unroll
+      for (int s = 0; s < KB; ++s) {
+        edge(s, x[s]);
+        gl_cut(x[s], v[s]);
+      }
+      const long mine = here;
+      here = next;
+      if (r + 32 < e) {
+#pragma unroll
+        for (int s = 0; s < KB; ++s) raw(g.a + here * g.a_stride, s, x[s]);
+        next = row_at(r + 64);
+      }
+      gl_f16v acc[NB];
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float4 t = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          if (KIND == GL_FORWARD) t = *reinterpret_cast<const float4*>(&s_bias[wave][32 * n + 8 * i + 4 * hh]);
+          acc[n][4 * i] = t.x; acc[n][4 * i + 1] = t.y; acc[n][4 * i + 2] = t.z; acc[n][4 * i + 3] = t.w;
+        }
+#pragma unroll
+      for (int s = 0; s < KB; ++s)
+#pragma unroll
+        for (int n = 0; n < NB; ++n) acc[n] = gl_product<T>(w[s][n], v[s], acc[n]);
+      if (r + r32 < e) {
+        T* to = g.y + mine * g.y_stride;
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int j = 32 * n + 8 * i + 4 * hh;
+            const float t[4] = {acc[n][4 * i], acc[n][4 * i + 1], acc[n][4 * i + 2], acc[n][4 * i + 3]};
+            if (wide && j + 4 <= g.J) {
+              rt_store<T, 4>(to + j, t);
+            } else {
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                if (j + q < g.J) to[j + q] = (T)t[q];
+            }
+          }
+      }
+    }
+  }
+}
+
+// dW and db of a slot: each wave its own sixteen rows in turn, operands straight from memory (lane = column, eight rows), the waves' sums
+// joined at the end.  MB, NB: blocks of 32 outputs and inputs.
+template <class T, int MB, int NB>
+__global__ __launch_bounds__(256, 2) void gl_lean_weights_kernel(GlArgs<T> g) {
+  constexpr int NP = GlType<T>::PIECES, PART = MB * NB * 1024;
+  typedef typename GlType<T>::Raw Raw;
+  __shared__ float s_part[4][PART / 2];
+  __shared__ double s_db[8][32 * MB];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, hh = lane >> 5;
+  int group;
+  long r0, r1;
+  const int slot = blockIdx.x;
+  const bool there = gl_slot(g.rows, g.chunk, slot, group, r0, r1);
+  if (!there && (g.chunk < g.rows.n || slot >= g.rows.G)) return;
+  if (!there) r0 = r1 = 0;                             // one chunk: a group without rows gets its zeros here
+  gl_f16v acc[MB][NB];
+#pragma unroll
+  for (int m = 0; m < MB; ++m)
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[m][n][i] = 0.0f;
+  double col_sum[MB] = {};
+  int ci[MB], cj[NB];
+#pragma unroll
+  for (int m = 0; m < MB; ++m) ci[m] = min(32 * m + r32, g.I - 1);
+#pragma unroll
+  for (int n = 0; n < NB; ++n) cj[n] = min(32 * n + r32, g.J - 1);
+  T d[MB][8], x[NB][8];
+  long row = 0;                                        // lane i of sixteen: row i of the unit to be fetched next
+  auto rows_of = [&](long u) { return gl_row(g.rows, min(u + (lane & 15), r1 - 1)); };
+  auto fetch = [&]() {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const long r = __shfl(row, 8 * hh + q);
+      const T* pd = g.a + r * g.a_stride;
+      const T* px = g.b + r * g.b_stride;
+#pragma unroll
+      for (int m = 0; m < MB; ++m) d[m][q] = pd[ci[m]];
+#pragma unroll
+      for (int n = 0; n < NB; ++n) x[n][q] = g.dW ? px[cj[n]] : (T)0.0f;
+    }
+  };
+  const long u0 = r0 + 16 * wave;
+  if (u0 < r1) {
+    row = rows_of(u0);
+    fetch();
+    row = rows_of(u0 + 64);
+  }
+  for (long u = u0; u < r1; u += 64) {
+    uint4 a[MB][NP], b[NB][NP];
+    const bool cut_off = u + 16 > r1;
+#pragma unroll
+    for (int m = 0; m < MB; ++m) {
+      if (cut_off)
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          if (u + 8 * hh + q >= r1) d[m][q] = (T)0.0f;
+      float t = 0.0f;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) t += (float)d[m][q];
+      col_sum[m] += (double)t;
+      Raw r;
+      __builtin_memcpy(&r, d[m], sizeof(Raw));
+      gl_cut(r, a[m]);
+    }
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      if (cut_off)
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          if (u + 8 * hh + q >= r1) x[n][q] = (T)0.0f;
+      Raw r;
+      __builtin_memcpy(&r, x[n], sizeof(Raw));
+      gl_cut(r, b[n]);
+    }
+    if (u + 64 < r1) {
+      fetch();
+      row = rows_of(u + 128);
+    }
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int n = 0; n < NB; ++n) acc[m][n] = gl_product<T>(a[m], b[n], acc[m][n]);
+  }
+  if (g.db) {
+#pragma unroll
+    for (int m = 0; m < MB; ++m) s_db[wave * 2 + hh][32 * m + r32] = col_sum[m];
+    __syncthreads();
+    if (tid < g.I) {
+      double t = 0.0;
+      for (int i = 0; i < 8; ++i) t += s_db[i][tid];
+      g.db[(size_t)slot * g.I + tid] = (float)t;
+    }
+  }
+  if (!g.dW) return;
+  // half of the values at a time: [register][lane] of every wave
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) s_part[wave][((m * NB + n) * 8 + q) * 64 + lane] = acc[m][n][8 * half + q];
+    __syncthreads();
+    for (int e = tid; e < PART / 2; e += 256) {
+      const int l = e & 63, q = (e >> 6) & 7, n = (e >> 9) % NB, m = (e >> 9) / NB;
+      const int i = 32 * m + 8 * (2 * half + (q >> 2)) + 4 * (l >> 5) + (q & 3), j = 32 * n + (l & 31);
+      if (i < g.I && j < g.J)
+        g.dW[((size_t)slot * g.I + i) * g.J + j] = (s_part[0][e] + s_part[1][e]) + (s_part[2][e] + s_part[3][e]);
+    }
+  }
+}
+
+// Sums of the slots of every group, n values a slot for dW and m for db behind them: sixteen values a workgroup, sixteen slots at a time.
+__global__ __launch_bounds__(256) void gl_join_kernel(GlRows p, long chunk, const float* dW_part, const float* db_part, float* dW, float* db,
+                                                      long n, long m) {
+  __shared__ float s[16][68];
+  const int g = blockIdx.y, k = threadIdx.x >> 4;
+  const long n4 = dW ? (n + 63) / 64 * 64 : 0;
+  const long at = (long)blockIdx.x * 64 + (threadIdx.x & 15) * 4;
+  const bool first = at < n4;
+  const float* part = first ? dW_part : db_part;
+  const long i = first ? at : at - n4, size = first ? n : m;
   const long b = gl_begin(p, g), e = gl_begin(p, g + 1);
-  float t = 0.0f;
+  float t[4] = {};
   if (b < e)
 #pragma unroll 4
-    for (long c = b / chunk; c <= (e - 1) / chunk; ++c) t += part[(size_t)(c + g) * n + i];
-  out[(size_t)g * n + i] = t;
+    for (long c = b / chunk + k; c <= (e - 1) / chunk; c += 16)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) t[q] += part[(size_t)(c + g) * size + min(i + q, size - 1)];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) s[k][(threadIdx.x & 15) * 4 + q] = t[q];
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const long v = (long)blockIdx.x * 64 + threadIdx.x, w = v < n4 ? v : v - n4;
+    float sum = 0.0f;
+    for (int r = 0; r < 16; ++r) sum += s[r][threadIdx.x];
+    if (v < n4 && w < n) dW[(size_t)g * n + w] = sum;
+    if (v >= n4 && w < m) db[(size_t)g * m + w] = sum;
+  }
 }
 
 int gl_check(egnn_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32_t K, int32_t N, int32_t G, const int32_t* ptr) {
@@ -652,6 +899,18 @@ int gl_rows(egnn_ctx* ctx, GlArgs<T> g, hipStream_t st) {
     g.tiles_j = (g.J + bn - 1) / bn;
     return ((g.rows.n + bm - 1) / bm + g.rows.G) * (long)g.tiles_j;
   };
+  if (g.J <= 64 && g.K <= 64) {
+    // 2,048 waves, two per SIMD, as long as each gets at least 32 rows
+    long share = (g.rows.n + 2047) / 2048;
+    if (share < 32) share = 32;
+    const unsigned grid = (unsigned)((g.rows.n + 4 * share - 1) / (4 * share));
+    if (g.J <= 32 && g.K <= 32)
+      hipLaunchKernelGGL((gl_lean_rows_kernel<T, KIND, 2, 1>), dim3(grid), dim3(256), 0, st, g, share);
+    else
+      hipLaunchKernelGGL((gl_lean_rows_kernel<T, KIND, 4, 2>), dim3(grid), dim3(256), 0, st, g, share);
+    EGNN_LAUNCH_CHECK(ctx, "grouped_linear");
+    return EGNN_OK;
+  }
   if constexpr (GlType<T>::PIECES == 1) {
     const long wide = tiles(128, 128);
     if (g.J > 64 && wide >= EGNN_CUS) return gl_launch<T, KIND, 128, 128, KS>(ctx, g, wide, st);
@@ -691,7 +950,14 @@ int gl_backward(egnn_ctx* ctx, const GlRows& p, const void* x, int64_t xs, const
     return (long)s.slots * g.tiles_j;
   };
   bool done = false;
-  if constexpr (GlType<T>::PIECES == 1) {
+  if (N <= 64 && K <= 64) {
+    if (N <= 32 && K <= 32)
+      hipLaunchKernelGGL((gl_lean_weights_kernel<T, 1, 1>), dim3(s.slots), dim3(256), 0, st, g);
+    else
+      hipLaunchKernelGGL((gl_lean_weights_kernel<T, 2, 2>), dim3(s.slots), dim3(256), 0, st, g);
+    EGNN_LAUNCH_CHECK(ctx, "grouped_linear_backward");
+    done = true;
+  } else if constexpr (GlType<T>::PIECES == 1) {
     const long wide = tiles(128, 128);
     if (N > 64 && K > 64 && wide >= EGNN_CUS) {
       if (int rc = gl_launch<T, GL_WEIGHTS, 128, 128, KS>(ctx, g, wide, st)) return rc;
@@ -703,9 +969,9 @@ int gl_backward(egnn_ctx* ctx, const GlRows& p, const void* x, int64_t xs, const
     if (int rc = gl_launch<T, GL_WEIGHTS, 64, 64, 2 * KS>(ctx, g, small, st)) return rc;
   }
   if (join) {
-    const long n = (long)N * K;
-    if (dW) hipLaunchKernelGGL(gl_join_kernel, dim3((unsigned)((n + 255) / 256), p.G), dim3(256), 0, st, p, s.chunk, pw, dW, n);
-    if (db) hipLaunchKernelGGL(gl_join_kernel, dim3((N + 255) / 256, p.G), dim3(256), 0, st, p, s.chunk, pb, db, (long)N);
+    const long n = dW ? (long)N * K : 0, m = db ? N : 0;
+    const long blocks = (n + 63) / 64 + (m + 63) / 64;
+    hipLaunchKernelGGL(gl_join_kernel, dim3((unsigned)blocks, p.G), dim3(256), 0, st, p, s.chunk, pw, pb, dW, db, n, m);
     EGNN_LAUNCH_CHECK(ctx, "grouped_linear_backward");
   }
   return EGNN_OK;
