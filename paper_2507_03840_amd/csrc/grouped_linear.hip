@@ -154,19 +154,19 @@ __device__ __forceinline__ void gl_load(const float* p, GlType<float>::Raw& r) {
   r.a = gl_load16(p);
   r.b = gl_load16(p + 4);
 }
-// a row of fewer than eight values
+// the first `valid` of eight values, zeros behind them (rows of fewer than eight)
 template <class T>
 __device__ __forceinline__ void gl_load_narrow(const T* p, int valid, uint4& r) {
   uint32_t w[4] = {};
 #pragma unroll
-  for (int q = 0; q < 7; ++q)
+  for (int q = 0; q < 8; ++q)
     if (q < valid) w[q >> 1] |= (uint32_t) reinterpret_cast<const uint16_t*>(p)[q] << (16 * (q & 1));
   r = make_uint4(w[0], w[1], w[2], w[3]);
 }
 __device__ __forceinline__ void gl_load_narrow(const float* p, int valid, GlType<float>::Raw& r) {
   uint32_t w[8] = {};
 #pragma unroll
-  for (int q = 0; q < 7; ++q)
+  for (int q = 0; q < 8; ++q)
     if (q < valid) w[q] = __float_as_uint(p[q]);
   r.a = make_uint4(w[0], w[1], w[2], w[3]);
   r.b = make_uint4(w[4], w[5], w[6], w[7]);
@@ -329,9 +329,11 @@ __device__ __forceinline__ bool gl_slot(const GlRows& p, long chunk, int t, int&
   return c >= 0 && r0 < r1;
 }
 
-// 256 threads, four waves, each a quarter of the BM x BN tile in 32 x 32 blocks.  Tiles go from memory to registers a turn ahead, are cut into
-// pieces on the way to one of two LDS buffers, and are contracted from the other.
-template <class T, GlKind KIND, int BM, int BN, int KS>
+// 256 threads, four waves, each a quarter of the BM x BN tile in 32 x 32 blocks.  Tiles go from memory to registers DEPTH turns ahead, are cut
+// into pieces on the way to one of two LDS buffers, and are contracted from the other.
+// NARROW: a side that is read along has fewer than eight values.
+constexpr int GL_PIECE = 2048;     // GL_WEIGHTS: row numbers kept in LDS (a row number loaded in turn would have to wait for the rows before it)
+template <class T, GlKind KIND, int BM, int BN, int KS, bool NARROW>
 __global__ __launch_bounds__(256) void gl_tile_kernel(GlArgs<T> g) {
   extern __shared__ __align__(16) char smem[];
   constexpr int NP = GlType<T>::PIECES, MB = BM / 64, NB = BN / 64;
@@ -364,99 +366,81 @@ __global__ __launch_bounds__(256) void gl_tile_kernel(GlArgs<T> g) {
   // What this thread stages.  Rows of the result past its end, and columns past its last, may hold anything (the last ones again): they do
   // not reach others.  Only contraction indices past the end have to be zero, in both operands: they end in the last turn.
   const int turns = (int)(KIND == GL_WEIGHTS ? (r1 - r0 + KS - 1) / KS : (g.K + KS - 1) / KS);
+  constexpr int DEPTH = KIND == GL_WEIGHTS ? 3 : 2;
   const T *pa[TA::CHUNKS], *pb[TB::CHUNKS];           // row, or column for rows that change with the turn
-  long ra[TA::CHUNKS], rb[TB::CHUNKS];                // GL_WEIGHTS: the rows of the next turn to be fetched
   int da[TA::CHUNKS], db[TB::CHUNKS];                 // across: places the columns are moved down at the end of a row
   bool edge_a = false, edge_b = false;
+  __shared__ int s_rows[KIND == GL_WEIGHTS ? GL_PIECE : 1];
   const T* const W = KIND == GL_WEIGHTS ? nullptr : g.b + (long)group * g.J * g.K;
-  auto next_row = [&](long r) { return gl_row(g.rows, min(r, r1 - 1)); };
-  const bool narrow_a = (KIND == GL_WEIGHTS ? g.I : g.K) < 8, narrow_b = (KIND == GL_FORWARD ? g.K : g.J) < 8;
   if (turns > 0) {
 #pragma unroll
     for (int c = 0; c < TA::CHUNKS; ++c) {
-      const long r = next_row(r0 + TA::row(c));
       if (KIND == GL_WEIGHTS) {
-        const int col = i0 + TA::col(c), from = narrow_a ? col : min(col, g.I - 8);
+        const int col = i0 + TA::col(c), from = NARROW ? col : min(col, g.I - 8);
         pa[c] = g.a + min(from, g.I - 1);
         da[c] = col - from;
-        ra[c] = r;
       } else {
-        pa[c] = g.a + r * g.a_stride;
+        pa[c] = g.a + gl_row(g.rows, min(r0 + TA::row(c), r1 - 1)) * g.a_stride;
       }
     }
 #pragma unroll
     for (int c = 0; c < TB::CHUNKS; ++c) {
-      const int col = j0 + TB::col(c), from = narrow_b ? col : min(col, g.J - 8);
+      const int col = j0 + TB::col(c), from = NARROW ? col : min(col, g.J - 8);
       if (KIND == GL_FORWARD) {                       // W[j][k]
         pb[c] = W + (long)min(j0 + TB::row(c), g.J - 1) * g.K;
       } else {                                        // W[k][j], x[r][j]
         pb[c] = (KIND == GL_INPUT ? W : g.b) + min(from, g.J - 1);
         db[c] = col - from;
-        if (KIND == GL_WEIGHTS) rb[c] = next_row(r0 + TB::row(c));
       }
     }
-    edge_a = KIND == GL_WEIGHTS && i0 + BM > g.I && !narrow_a;
-    edge_b = KIND != GL_FORWARD && j0 + BN > g.J && !narrow_b;
+    edge_a = KIND == GL_WEIGHTS && i0 + BM > g.I && !NARROW;
+    edge_b = KIND != GL_FORWARD && j0 + BN > g.J && !NARROW;
   }
-  Raw a[TA::CHUNKS], b[TB::CHUNKS];
-  auto fetch = [&](int turn) {
-    if (narrow_a) {
+  Raw a[DEPTH][TA::CHUNKS], b[DEPTH][TB::CHUNKS];
+  long piece = r0;                                    // GL_WEIGHTS: first row in s_rows
+  auto row_of = [&](int turn, int at) -> long { return s_rows[min((int)(r0 - piece) + turn * KS + at, min(GL_PIECE, (int)(r1 - piece)) - 1)]; };
+  auto fetch = [&](int turn, int to) {
 #pragma unroll
-      for (int c = 0; c < TA::CHUNKS; ++c) {
-        const int k = turn * KS + TA::col(c);
-        if (KIND == GL_WEIGHTS) gl_load_narrow(pa[c] + ra[c] * g.a_stride, g.I - i0 - TA::col(c), a[c]);
-        else gl_load_narrow(pa[c] + min(k, g.K - 1), g.K - k, a[c]);
-      }
-    } else {
-#pragma unroll
-      for (int c = 0; c < TA::CHUNKS; ++c) gl_load(KIND == GL_WEIGHTS ? pa[c] + ra[c] * g.a_stride : pa[c] + min(turn * KS + TA::col(c), g.K - 8), a[c]);
+    for (int c = 0; c < TA::CHUNKS; ++c) {
+      const int k = turn * KS + TA::col(c);
+      const T* p = pa[c] + (KIND == GL_WEIGHTS ? row_of(turn, TA::row(c)) * g.a_stride : (long)min(k, NARROW ? g.K - 1 : g.K - 8));
+      if (NARROW) gl_load_narrow(p, KIND == GL_WEIGHTS ? g.I - i0 - TA::col(c) : g.K - k, a[to][c]);
+      else gl_load(p, a[to][c]);
     }
-    if (narrow_b) {
 #pragma unroll
-      for (int c = 0; c < TB::CHUNKS; ++c) {
-        const int k = turn * KS + (KIND == GL_FORWARD ? TB::col(c) : TB::row(c));
-        if (KIND == GL_FORWARD) gl_load_narrow(pb[c] + min(k, g.K - 1), g.K - k, b[c]);
-        else gl_load_narrow(pb[c] + (KIND == GL_WEIGHTS ? rb[c] * g.b_stride : (long)min(k, g.K - 1) * g.J), g.J - j0 - TB::col(c), b[c]);
-      }
-    } else {
-#pragma unroll
-      for (int c = 0; c < TB::CHUNKS; ++c) {
-        if (KIND == GL_FORWARD) gl_load(pb[c] + min(turn * KS + TB::col(c), g.K - 8), b[c]);
-        else gl_load(pb[c] + (KIND == GL_WEIGHTS ? rb[c] * g.b_stride : (long)min(turn * KS + TB::row(c), g.K - 1) * g.J), b[c]);
-      }
-    }
-    if (KIND == GL_WEIGHTS) {
-#pragma unroll
-      for (int c = 0; c < TA::CHUNKS; ++c) ra[c] = next_row(r0 + (long)(turn + 1) * KS + TA::row(c));
-#pragma unroll
-      for (int c = 0; c < TB::CHUNKS; ++c) rb[c] = next_row(r0 + (long)(turn + 1) * KS + TB::row(c));
+    for (int c = 0; c < TB::CHUNKS; ++c) {
+      const int k = turn * KS + (KIND == GL_FORWARD ? TB::col(c) : TB::row(c));
+      const T* p = pb[c] + (KIND == GL_WEIGHTS ? row_of(turn, TB::row(c)) * g.b_stride
+                            : KIND == GL_INPUT ? (long)min(k, g.K - 1) * g.J : (long)min(k, NARROW ? g.K - 1 : g.K - 8));
+      if (NARROW) gl_load_narrow(p, KIND == GL_FORWARD ? g.K - k : g.J - j0 - TB::col(c), b[to][c]);
+      else gl_load(p, b[to][c]);
     }
   };
   float turn_sum[8];
   double col_sum[8] = {};
   const bool sums = KIND == GL_WEIGHTS && g.db && j0 == 0;
-  auto stage = [&](int turn) {
+  auto stage = [&](int turn, int at) {
     char* to = smem + (turn & 1) * STAGE;
     const bool last = turn + 1 == turns;
     const long left = (KIND == GL_WEIGHTS ? r1 - r0 : (long)g.K) - (long)turn * KS;      // contraction indices from this turn on
     if (KIND == GL_WEIGHTS && edge_a) {
 #pragma unroll
-      for (int c = 0; c < TA::CHUNKS; ++c) gl_shift(a[c], da[c]);
+      for (int c = 0; c < TA::CHUNKS; ++c) gl_shift(a[at][c], da[c]);
     }
     if (KIND != GL_FORWARD && edge_b) {
 #pragma unroll
-      for (int c = 0; c < TB::CHUNKS; ++c) gl_shift(b[c], db[c]);
+      for (int c = 0; c < TB::CHUNKS; ++c) gl_shift(b[at][c], db[c]);
     }
     if (last && left < KS) {
 #pragma unroll
       for (int c = 0; c < TA::CHUNKS; ++c) {
-        if (KIND == GL_WEIGHTS) gl_shift(a[c], TA::row(c) < left ? 0 : 8);
-        else if (!narrow_a) gl_shift(a[c], max(0, TA::col(c) + 8 - (int)left));
+        if (KIND == GL_WEIGHTS) gl_shift(a[at][c], TA::row(c) < left ? 0 : 8);
+        else if (!NARROW) gl_shift(a[at][c], max(0, TA::col(c) + 8 - (int)left));
       }
 #pragma unroll
       for (int c = 0; c < TB::CHUNKS; ++c) {
-        if (KIND != GL_FORWARD) gl_shift(b[c], TB::row(c) < left ? 0 : 8);
-        else if (!narrow_b) gl_shift(b[c], max(0, TB::col(c) + 8 - (int)left));
+        if (KIND != GL_FORWARD) gl_shift(b[at][c], TB::row(c) < left ? 0 : 8);
+        else if (!NARROW) gl_shift(b[at][c], max(0, TB::col(c) + 8 - (int)left));
       }
     }
 #pragma unroll
@@ -464,15 +448,15 @@ __global__ __launch_bounds__(256) void gl_tile_kernel(GlArgs<T> g) {
 #pragma unroll
     for (int c = 0; c < TA::CHUNKS; ++c) {
       uint4 v[NP];
-      gl_cut(a[c], v);
-      if (sums) gl_add<T>(a[c], turn_sum);
+      gl_cut(a[at][c], v);
+      if (sums) gl_add<T>(a[at][c], turn_sum);
 #pragma unroll
       for (int q = 0; q < NP; ++q) *reinterpret_cast<uint4*>(to + q * TA::PLANE + TA::at(c)) = v[q];
     }
 #pragma unroll
     for (int c = 0; c < TB::CHUNKS; ++c) {
       uint4 v[NP];
-      gl_cut(b[c], v);
+      gl_cut(b[at][c], v);
 #pragma unroll
       for (int q = 0; q < NP; ++q) *reinterpret_cast<uint4*>(to + NP * TA::PLANE + q * TB::PLANE + TB::at(c)) = v[q];
     }
@@ -489,13 +473,8 @@ __global__ __launch_bounds__(256) void gl_tile_kernel(GlArgs<T> g) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[x][y][i] = 0.0f;
   const int wi = (wave >> 1) * (BM / 2), wj = (wave & 1) * (BN / 2);
-  if (turns > 0) {
-    fetch(0);
-    stage(0);
-    if (turns > 1) fetch(1);
-  }
-  for (int k = 0; k < turns; ++k) {
-    rb_release_barrier();        // (only LDS is waited for: the next turn's loads stay under way)
+  auto contract = [&](int k) {
+    rb_release_barrier();        // (only LDS is waited for: the next turns' loads stay under way)
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
     const char* from = smem + (k & 1) * STAGE;
 #pragma unroll
@@ -514,10 +493,41 @@ __global__ __launch_bounds__(256) void gl_tile_kernel(GlArgs<T> g) {
 #pragma unroll
         for (int y = 0; y < NB; ++y) acc[x][y] = gl_product<T>(fa[x], fb[y], acc[x][y]);
     }
-    if (k + 1 < turns) {
-      stage(k + 1);
-      if (k + 2 < turns) fetch(k + 2);
+  };
+  // turns k0 .. k1 - 1; their number of loads under way is the same in every turn of the first loop
+  auto run = [&](int k0, int k1) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) fetch(min(k0 + d, k1 - 1), d);
+    stage(k0, 0);
+    fetch(min(k0 + DEPTH, k1 - 1), 0);
+    int k = k0;
+    for (; k + 2 * DEPTH < k1; k += DEPTH)
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) {
+        contract(k + d);
+        stage(k + d + 1, (d + 1) % DEPTH);
+        fetch(k + d + 1 + DEPTH, (d + 1) % DEPTH);
+      }
+#pragma unroll
+    for (int d = 0; d < 2 * DEPTH; ++d)
+      if (k + d < k1) {
+        contract(k + d);
+        if (k + d + 1 < k1) {
+          stage(k + d + 1, (d + 1) % DEPTH);
+          if (d + 1 < DEPTH && k + d + 1 + DEPTH < k1) fetch(k + d + 1 + DEPTH, (d + 1) % DEPTH);
+        }
+      }
+  };
+  if (KIND == GL_WEIGHTS) {
+    for (int k = 0; k < turns; k += GL_PIECE / KS) {
+      piece = r0 + (long)k * KS;
+      __syncthreads();
+      for (int i = tid; i < GL_PIECE; i += 256) s_rows[i] = (int)gl_row(g.rows, min(piece + i, r1 - 1));
+      __syncthreads();
+      run(k, min(turns, k + GL_PIECE / KS));
     }
+  } else {
+    run(0, turns);
   }
 
   // a lane holds column j = lane & 31 of its blocks and four times four neighbouring rows i
@@ -594,7 +604,7 @@ __global__ __launch_bounds__(256) void gl_tile_kernel(GlArgs<T> g) {
 // product is y^T = W x^T, so that a lane holds one row and writes its values four neighbouring ones at a time.  The next rows are under way
 // while the matrix cores work on these; what is left is the memory.
 // KB: contraction steps of 16, NB: output blocks of 32; 16 KB >= K, 32 NB >= J.
-template <class T, GlKind KIND, int KB, int NB>
+template <class T, GlKind KIND, int KB, int NB, bool NARROW>
 __global__ __launch_bounds__(256, 2) void gl_lean_rows_kernel(GlArgs<T> g, long share) {
   constexpr int NP = GlType<T>::PIECES;
   typedef typename GlType<T>::Raw Raw;
@@ -606,14 +616,13 @@ __global__ __launch_bounds__(256, 2) void gl_lean_rows_kernel(GlArgs<T> g, long 
     const int mid = (lo + hi + 1) >> 1;
     if (gl_begin(g.rows, mid) <= first) lo = mid; else hi = mid - 1;
   }
-  const bool narrow = g.K < 8;
   auto raw = [&](const T* row, int s, Raw& to) {      // eight values of a row from 16 s + 8 hh on, the row's last ones past its end
     const int k = 16 * s + 8 * hh;
-    if (narrow) gl_load_narrow(row + min(k, g.K - 1), g.K - k, to);
+    if (NARROW) gl_load_narrow(row + min(k, g.K - 1), g.K - k, to);
     else gl_load(row + min(k, g.K - 8), to);
   };
   auto edge = [&](int s, Raw& r) {
-    if (!narrow && 16 * KB > g.K) gl_shift(r, max(0, 16 * s + 8 * hh + 8 - g.K));
+    if (!NARROW && 16 * KB > g.K) gl_shift(r, max(0, 16 * s + 8 * hh + 8 - g.K));
   };
   const bool wide = ((uintptr_t)g.y | (g.y_stride * sizeof(T))) % (4 * sizeof(T)) == 0;
   for (int group = lo; group < g.rows.G; ++group) {
@@ -877,17 +886,17 @@ GlSplit gl_split(int64_t n, int G, int K, int N) {
   return s;
 }
 
-template <class T, GlKind KIND, int BM, int BN, int KS>
+template <class T, GlKind KIND, int BM, int BN, int KS, bool NARROW = false>
 int gl_launch(egnn_ctx* ctx, const GlArgs<T>& g, long tiles, hipStream_t st) {
   constexpr size_t stage = GlType<T>::PIECES * (GlTile<BM, KS, KIND == GL_WEIGHTS>::PLANE + GlTile<BN, KS, KIND != GL_FORWARD>::PLANE);
   constexpr size_t out = KIND == GL_WEIGHTS ? (size_t)256 * 8 * sizeof(double) : (size_t)BM * (BN + 4) * sizeof(float);
   constexpr size_t lds = 2 * stage > out ? 2 * stage : out;
   static bool ready = false;      // (set again by two threads at once: to the same value)
   if (!ready && lds > 65536) {
-    EGNN_HIP(ctx, hipFuncSetAttribute((const void*)gl_tile_kernel<T, KIND, BM, BN, KS>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    EGNN_HIP(ctx, hipFuncSetAttribute((const void*)gl_tile_kernel<T, KIND, BM, BN, KS, NARROW>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
     ready = true;
   }
-  hipLaunchKernelGGL((gl_tile_kernel<T, KIND, BM, BN, KS>), dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(256), lds, st, g);
+  hipLaunchKernelGGL((gl_tile_kernel<T, KIND, BM, BN, KS, NARROW>), dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(256), lds, st, g);
   EGNN_LAUNCH_CHECK(ctx, "grouped_linear");
   return EGNN_OK;
 }
@@ -904,13 +913,16 @@ int gl_rows(egnn_ctx* ctx, GlArgs<T> g, hipStream_t st) {
     long share = (g.rows.n + 2047) / 2048;
     if (share < 32) share = 32;
     const unsigned grid = (unsigned)((g.rows.n + 4 * share - 1) / (4 * share));
-    if (g.J <= 32 && g.K <= 32)
-      hipLaunchKernelGGL((gl_lean_rows_kernel<T, KIND, 2, 1>), dim3(grid), dim3(256), 0, st, g, share);
+    if (g.K < 8)
+      hipLaunchKernelGGL((gl_lean_rows_kernel<T, KIND, 1, 2, true>), dim3(grid), dim3(256), 0, st, g, share);
+    else if (g.J <= 32 && g.K <= 32)
+      hipLaunchKernelGGL((gl_lean_rows_kernel<T, KIND, 2, 1, false>), dim3(grid), dim3(256), 0, st, g, share);
     else
-      hipLaunchKernelGGL((gl_lean_rows_kernel<T, KIND, 4, 2>), dim3(grid), dim3(256), 0, st, g, share);
+      hipLaunchKernelGGL((gl_lean_rows_kernel<T, KIND, 4, 2, false>), dim3(grid), dim3(256), 0, st, g, share);
     EGNN_LAUNCH_CHECK(ctx, "grouped_linear");
     return EGNN_OK;
   }
+  if (g.K < 8 || (KIND == GL_INPUT && g.J < 8)) return gl_launch<T, KIND, 64, 64, KS, true>(ctx, g, tiles(64, 64), st);
   if constexpr (GlType<T>::PIECES == 1) {
     const long wide = tiles(128, 128);
     if (g.J > 64 && wide >= EGNN_CUS) return gl_launch<T, KIND, 128, 128, KS>(ctx, g, wide, st);
@@ -956,6 +968,10 @@ int gl_backward(egnn_ctx* ctx, const GlRows& p, const void* x, int64_t xs, const
     else
       hipLaunchKernelGGL((gl_lean_weights_kernel<T, 2, 2>), dim3(s.slots), dim3(256), 0, st, g);
     EGNN_LAUNCH_CHECK(ctx, "grouped_linear_backward");
+    done = true;
+  } else if (N < 8 || K < 8) {
+    const long small = tiles(64, 64);
+    if (int rc = gl_launch<T, GL_WEIGHTS, 64, 64, 2 * KS, true>(ctx, g, small, st)) return rc;
     done = true;
   } else if constexpr (GlType<T>::PIECES == 1) {
     const long wide = tiles(128, 128);
