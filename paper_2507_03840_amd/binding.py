@@ -127,7 +127,7 @@ def _f3(a):
 
 
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))   # of the current stream, without an object for it
 
 
 class Graph:

@@ -6,18 +6,22 @@
 // Adjoint, with dz = dy sig (1 + z (1 - sig)), sig = 1 / (1 + exp(-z)):
 //   dgamma_c = sum_rows dz xhat, dbeta_c = sum_rows dz, dx = rstd (gamma_c dz - mean_g(gamma dz) - xhat mean_g(gamma dz xhat)).
 // Both directions are a pass that sums and a pass that writes, one launch each.  What bounds them is memory: x (and dy) are
-// read twice, because the sums of all rows of a segment come before its first result.
+// read twice, because the sums of all rows of a segment come before its first result.  The second pass goes through its rows from the last
+// to the first, so that it begins with what the first pass left in the caches.  Where one workgroup takes all rows the two are one launch.
 //
 // The rows are cut into equal chunks, one workgroup each; segments are ragged and may be shorter or longer than a chunk.
 // A chunk c and a segment s that share rows own the slot c + s of the partial sums: walking along the rows either c or s
 // goes up by one, so no two pairs share a slot, the slots of a segment are contiguous, and their number is at most chunks +
-// segments.  The second pass adds the slots of its segments itself, in ascending order (no atomics).
+// segments.  The second pass adds the slots of its segments itself, in a fixed order (no atomics).
 #include "row_types.h"
 
 namespace {
 
 constexpr int GN_CHUNKS = 512;        // two workgroups per compute unit; the second pass reads all partial sums of a segment
 constexpr int GN_CHUNK_BYTES = 16384; // a chunk holds at least this much of x: below it the launch is longer than the reading
+constexpr int GN_ALONE_BYTES = 65536; // up to this much of x one workgroup takes all rows
+constexpr int GN_THREADS = 512;       // 1,024 where a row has more than 512 pieces
+constexpr int GN_ROWS = 4;            // rows of a thread under way at once
 
 struct GnShape {
   long n;               // rows
@@ -40,92 +44,151 @@ __device__ __forceinline__ int gn_first_segment(const GnShape& p, long row) {
   return lo;
 }
 
-// The sums are of x - x', x' the first value of the segment and group, and fp64: sum (x - x')^2 / n - (sum (x - x') / n)^2 then loses
-// nothing to a mean far from zero, and a first value far from all others costs n 2^-53.
+// ---- sums inside a workgroup -------------------------------------------------------------------------------------------------
+// v[rows][width]: sums over the rows, to row 0
+template <class P>
+__device__ __forceinline__ void gn_sum_over_rows(P* v, int rows, int width) {
+  while (rows > 1) {
+    const int half = (rows + 1) >> 1;
+    __syncthreads();
+    for (int e = threadIdx.x; e < (rows - half) * width; e += blockDim.x) {
+      v[e].x += v[e + half * width].x;
+      v[e].y += v[e + half * width].y;
+    }
+    rows = half;
+  }
+  __syncthreads();
+}
+// v[n]: sums over runs of `size`, to the first of each
+template <class P>
+__device__ __forceinline__ void gn_sum_over_runs(P* v, int n, int size) {
+  for (int left = size; left > 1;) {
+    const int half = (left + 1) >> 1;
+    for (int e = threadIdx.x; e < n; e += blockDim.x) {
+      const int k = e % size;
+      if (k < left - half) {
+        v[e].x += v[e + half].x;
+        v[e].y += v[e + half].y;
+      }
+    }
+    left = half;
+    __syncthreads();
+  }
+}
+
+// calls f(row index of GN_ROWS rows, number of them that are there) for the rows of this thread, the last ones first
+template <class F>
+__device__ __forceinline__ void gn_rows_backwards(long b, long e, int rr, int slots, const F& f) {
+  const long mine = e - b > rr ? (e - b - rr + slots - 1) / slots : 0;      // rows b + rr + k slots
+  for (long k = (mine + GN_ROWS - 1) / GN_ROWS - 1; k >= 0; --k) f(b + rr + k * GN_ROWS * slots, (int)min((long)GN_ROWS, mine - k * GN_ROWS));
+}
+
+struct GnLanes { int L, slots, l, rr; };
+template <int V>
+__device__ __forceinline__ GnLanes gn_lanes(int C) {
+  GnLanes t;
+  t.L = C / V;
+  t.slots = blockDim.x / t.L;
+  t.l = threadIdx.x % t.L;
+  t.rr = threadIdx.x / t.L;
+  return t;
+}
+
 // ---- forward ---------------------------------------------------------------------------------------------------------
+// Sums over the rows b .. e - 1 of one segment, per group, to s[g * run]; returns run.
+// They are of x - x', x' the first value of the segment and group, and fp64: sum (x - x')^2 / n - (sum (x - x') / n)^2 then loses nothing to
+// a mean far from zero, and a first value far from all others costs n 2^-53.
 template <class T, int V>
-__global__ __launch_bounds__(1024) void gn_sums_kernel(GnShape p, const T* x, long x_stride, double2* part, float* first_of) {
-  extern __shared__ double2 smem[];   // [row slots][C]
-  const int L = p.C / V, slots = blockDim.x / L, l = threadIdx.x % L, rr = threadIdx.x / L;
+__device__ __forceinline__ int gn_segment_rows(const GnShape& p, const T* x, long x_stride, const T* first, long b, long e, double2* s) {
+  const GnLanes t = gn_lanes<V>(p.C);
+  const int size = p.C / p.G;
+  const bool whole = size % V == 0;            // all values of a thread are of one group
+  double a1[V], a2[V], from[V];
+#pragma unroll
+  for (int q = 0; q < V; ++q) {
+    a1[q] = a2[q] = 0.0;
+    from[q] = (double)(float)first[(t.l * V + q) / size * size];
+  }
+  if (t.rr < t.slots) {
+    for (long r = b + t.rr; r < e; r += GN_ROWS * t.slots) {
+      float v[GN_ROWS][V];
+#pragma unroll
+      for (int k = 0; k < GN_ROWS; ++k) rt_load<T, V>(x + min(r + (long)k * t.slots, e - 1) * x_stride + t.l * V, v[k]);
+#pragma unroll
+      for (int k = 0; k < GN_ROWS; ++k)
+        if (r + (long)k * t.slots < e)
+#pragma unroll
+          for (int q = 0; q < V; ++q) {
+            const double d = (double)v[k][q] - from[q];
+            a1[q] += d;
+            a2[q] += d * d;
+          }
+    }
+    if (whole) {
+#pragma unroll
+      for (int q = 1; q < V; ++q) {
+        a1[0] += a1[q];
+        a2[0] += a2[q];
+      }
+      s[t.rr * t.L + t.l] = make_double2(a1[0], a2[0]);
+    } else {
+#pragma unroll
+      for (int q = 0; q < V; ++q) s[t.rr * p.C + t.l * V + q] = make_double2(a1[q], a2[q]);
+    }
+  }
+  const int width = whole ? t.L : p.C, run = width / p.G;
+  gn_sum_over_rows(s, t.slots, width);
+  gn_sum_over_runs(s, width, run);
+  return run;
+}
+
+template <class T, int V>
+__global__ __launch_bounds__(V == 1 ? 1024 : GN_THREADS) void gn_sums_kernel(GnShape p, const T* x, long x_stride, double2* part, float* first_of) {
+  extern __shared__ double2 smem[];
   const long r0 = (long)blockIdx.x * p.rows, r1 = min(r0 + p.rows, p.n);
   const int size = p.C / p.G;
   for (int s = gn_first_segment(p, r0); s < p.S; ++s) {
-    const long b = max(gn_begin(p, s), r0), e = min(gn_begin(p, s + 1), r1);
-    if (gn_begin(p, s) >= r1) break;
+    const long sb = gn_begin(p, s), b = max(sb, r0), e = min(gn_begin(p, s + 1), r1);
+    if (sb >= r1) break;
     if (b >= e) continue;
-    double a1[V], a2[V], from[V];
-    const T* first = x + gn_begin(p, s) * x_stride;
-#pragma unroll
-    for (int q = 0; q < V; ++q) {
-      a1[q] = a2[q] = 0.0;
-      from[q] = (double)(float)first[rr < slots ? (l * V + q) / size * size : 0];
-    }
-    if (rr < slots) {
-#pragma unroll 4
-      for (long r = b + rr; r < e; r += slots) {
-        float v[V];
-        rt_load<T, V>(x + r * x_stride + l * V, v);
-#pragma unroll
-        for (int q = 0; q < V; ++q) {
-          const double d = (double)v[q] - from[q];
-          a1[q] += d;
-          a2[q] += d * d;
-        }
-      }
-#pragma unroll
-      for (int q = 0; q < V; ++q) smem[rr * p.C + l * V + q] = make_double2(a1[q], a2[q]);
-    }
-    __syncthreads();
+    const T* first = x + sb * x_stride;
+    const int run = gn_segment_rows<T, V>(p, x, x_stride, first, b, e, smem);
     for (int g = threadIdx.x; g < p.G; g += blockDim.x) {
-      double t1 = 0.0, t2 = 0.0;
-      for (int r = 0; r < slots; ++r)
-        for (int c = g * size; c < (g + 1) * size; ++c) {
-          t1 += smem[r * p.C + c].x;
-          t2 += smem[r * p.C + c].y;
-        }
-      part[(size_t)(blockIdx.x + s) * p.G + g] = make_double2(t1, t2);
-      if (b == gn_begin(p, s)) first_of[(size_t)s * p.G + g] = (float)first[g * size];   // (y may be x: kept apart)
+      part[(size_t)(blockIdx.x + s) * p.G + g] = smem[g * run];
+      if (b == sb) first_of[(size_t)s * p.G + g] = (float)first[g * size];   // (y may be x: kept apart)
     }
     __syncthreads();
   }
 }
 
-// sums of the slots of segment s, to out[G] in LDS; scratch [blockDim]
-__device__ __forceinline__ void gn_segment_sums(const GnShape& p, const double2* part, int s, double2* out, double2* scratch) {
-  const long b = gn_begin(p, s), e = gn_begin(p, s + 1);
-  const int c0 = (int)(b / p.rows), c1 = (int)((e - 1) / p.rows);
-  const int per = max(1, (int)blockDim.x / p.G), k = threadIdx.x / p.G;
-  for (int g0 = 0; g0 < p.G; g0 += blockDim.x) {
-    const int g = g0 + threadIdx.x % p.G;
-    double2 t = make_double2(0.0, 0.0);
-    if (k < per && g < p.G)
-      for (int c = c0 + k; c <= c1; c += per) {
-        const double2 v = part[(size_t)(c + s) * p.G + g];
-        t.x += v.x;
-        t.y += v.y;
+// sums of the slots of segment s, to v[G]; v has room for a value of every thread
+__device__ __forceinline__ void gn_segment_sums(const GnShape& p, const double2* part, int s, double2* v) {
+  const int c0 = (int)(gn_begin(p, s) / p.rows), c1 = (int)((gn_begin(p, s + 1) - 1) / p.rows);
+  const int rows = max(1, (int)blockDim.x / p.G), k = threadIdx.x / p.G;
+  if (k < rows)
+    for (int g = threadIdx.x % p.G; g < p.G; g += blockDim.x) {
+      double2 t = make_double2(0.0, 0.0);
+#pragma unroll 4
+      for (int c = c0 + k; c <= c1; c += rows) {
+        const double2 u = part[(size_t)(c + s) * p.G + g];
+        t.x += u.x;
+        t.y += u.y;
       }
-    scratch[threadIdx.x] = t;
-    __syncthreads();
-    if (k == 0 && g < p.G) {
-      for (int j = 1; j < per; ++j) {
-        t.x += scratch[j * p.G + threadIdx.x].x;
-        t.y += scratch[j * p.G + threadIdx.x].y;
-      }
-      out[g] = t;
+      v[k * p.G + g] = t;
     }
-    __syncthreads();
-  }
+  gn_sum_over_rows(v, min(rows, c1 - c0 + 1), p.G);
 }
 
-__device__ __forceinline__ float gn_sigmoid(float z) { return 1.0f / (1.0f + __expf(-z)); }
+__device__ __forceinline__ float gn_sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 
-template <class T, int V>
-__global__ __launch_bounds__(1024) void gn_write_kernel(GnShape p, const T* x, long x_stride, const float* gamma, const float* beta,
+// ALONE: the only workgroup, which makes the sums itself
+template <class T, int V, bool ALONE>
+__global__ __launch_bounds__(V == 1 ? 1024 : GN_THREADS) void gn_write_kernel(GnShape p, const T* x, long x_stride, const float* gamma, const float* beta,
                                                         float eps, T* y, long y_stride, float* mean, float* rstd,
                                                         const double2* part, const float* first) {
-  __shared__ double2 sums[1024], scratch[1024];
+  extern __shared__ double2 smem[];
   __shared__ float s_mean[1024], s_rstd[1024];
-  const int L = p.C / V, slots = blockDim.x / L, l = threadIdx.x % L, rr = threadIdx.x / L;
+  const GnLanes t = gn_lanes<V>(p.C);
   const long r0 = (long)blockIdx.x * p.rows, r1 = min(r0 + p.rows, p.n);
   const int size = p.C / p.G;
   // segments without rows: the first workgroup writes their zeros
@@ -136,19 +199,23 @@ __global__ __launch_bounds__(1024) void gn_write_kernel(GnShape p, const T* x, l
   float ga[V], be[V];
 #pragma unroll
   for (int q = 0; q < V; ++q) {
-    ga[q] = gamma[l * V + q];
-    be[q] = beta[l * V + q];
+    ga[q] = gamma[t.l * V + q];
+    be[q] = beta[t.l * V + q];
   }
   for (int s = gn_first_segment(p, r0); s < p.S; ++s) {
     const long sb = gn_begin(p, s), se = gn_begin(p, s + 1);
     const long b = max(sb, r0), e = min(se, r1);
     if (sb >= r1) break;
     if (b >= e) continue;
-    gn_segment_sums(p, part, s, sums, scratch);
+    int run = 1;
+    const T* head = x + sb * x_stride;
+    if (ALONE) run = gn_segment_rows<T, V>(p, x, x_stride, head, b, e, smem);
+    else gn_segment_sums(p, part, s, smem);
     for (int g = threadIdx.x; g < p.G; g += blockDim.x) {
-      const double n = (double)(se - sb) * size, mu = sums[g].x / n;
-      const double var = sums[g].y / n - mu * mu;
-      s_mean[g] = (float)((double)first[(size_t)s * p.G + g] + mu);
+      const double n = (double)(se - sb) * size, mu = smem[g * run].x / n;
+      const double var = smem[g * run].y / n - mu * mu;
+      const float from = ALONE ? (float)head[g * size] : first[(size_t)s * p.G + g];
+      s_mean[g] = (float)((double)from + mu);
       s_rstd[g] = (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)eps));   // (a NaN stays one)
       if (b == sb) {
         mean[(size_t)s * p.G + g] = s_mean[g];
@@ -156,24 +223,29 @@ __global__ __launch_bounds__(1024) void gn_write_kernel(GnShape p, const T* x, l
       }
     }
     __syncthreads();
-    if (rr < slots) {
+    if (t.rr < t.slots) {
       float mu[V], rs[V];
 #pragma unroll
       for (int q = 0; q < V; ++q) {
-        const int g = (l * V + q) / size;
+        const int g = (t.l * V + q) / size;
         mu[q] = s_mean[g];
         rs[q] = s_rstd[g];
       }
-      for (long r = b + rr; r < e; r += slots) {
-        float v[V];
-        rt_load<T, V>(x + r * x_stride + l * V, v);
+      gn_rows_backwards(b, e, t.rr, t.slots, [&](long r, int rows) {
+        float v[GN_ROWS][V];
 #pragma unroll
-        for (int q = 0; q < V; ++q) {
-          const float z = (v[q] - mu[q]) * rs[q] * ga[q] + be[q];
-          v[q] = z * gn_sigmoid(z);
+        for (int k = 0; k < GN_ROWS; ++k) rt_load<T, V>(x + (r + (long)min(k, rows - 1) * t.slots) * x_stride + t.l * V, v[k]);
+#pragma unroll
+        for (int k = 0; k < GN_ROWS; ++k) {
+          if (k >= rows) break;
+#pragma unroll
+          for (int q = 0; q < V; ++q) {
+            const float z = (v[k][q] - mu[q]) * rs[q] * ga[q] + be[q];
+            v[k][q] = z * gn_sigmoid(z);
+          }
+          rt_store<T, V>(y + (r + (long)k * t.slots) * y_stride + t.l * V, v[k]);
         }
-        rt_store<T, V>(y + r * y_stride + l * V, v);
-      }
+      });
     }
     __syncthreads();
   }
@@ -183,142 +255,169 @@ __global__ __launch_bounds__(1024) void gn_write_kernel(GnShape p, const T* x, l
 struct GnAdjoint {
   const float *mean, *rstd, *gamma, *beta;
 };
+// LDS of the sums: float2 [slots][C], float2 [C] of the whole chunk, double2 [C]
+__host__ __device__ inline size_t gn_adjoint_lds(int C, int slots) { return (size_t)((slots + 2) & ~1) * C * sizeof(float2) + (size_t)C * sizeof(double2); }
+
+// Sums over the rows b .. e - 1 of segment s: per channel into rows[C] (and added to total[C]), per group with gamma into groups[g * size]
+template <class T, int V>
+__device__ __forceinline__ void gn_adjoint_rows(const GnShape& p, const GnAdjoint& w, const T* x, long x_stride, const T* dy, long dy_stride, int s, long b,
+                                                long e, const float (&ga)[V], const float (&be)[V], float2* rows, float2* total,
+                                                double2* groups) {
+  const GnLanes t = gn_lanes<V>(p.C);
+  const int size = p.C / p.G;
+  if (t.rr < t.slots) {
+    float mu[V], rs[V], a1[V], a2[V];
+#pragma unroll
+    for (int q = 0; q < V; ++q) {
+      const size_t at = (size_t)s * p.G + (t.l * V + q) / size;
+      mu[q] = w.mean[at];
+      rs[q] = w.rstd[at];
+      a1[q] = a2[q] = 0.0f;
+    }
+    for (long r = b + t.rr; r < e; r += GN_ROWS * t.slots) {
+      float v[GN_ROWS][V], d[GN_ROWS][V];
+#pragma unroll
+      for (int k = 0; k < GN_ROWS; ++k) {
+        const long at = min(r + (long)k * t.slots, e - 1);
+        rt_load<T, V>(x + at * x_stride + t.l * V, v[k]);
+        rt_load<T, V>(dy + at * dy_stride + t.l * V, d[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < GN_ROWS; ++k)
+        if (r + (long)k * t.slots < e)
+#pragma unroll
+          for (int q = 0; q < V; ++q) {
+            const float h = (v[k][q] - mu[q]) * rs[q], z = h * ga[q] + be[q], sig = gn_sigmoid(z);
+            const float dz = d[k][q] * sig * (1.0f + z * (1.0f - sig));
+            a1[q] += dz;
+            a2[q] += dz * h;
+          }
+    }
+#pragma unroll
+    for (int q = 0; q < V; ++q) rows[t.rr * p.C + t.l * V + q] = make_float2(a1[q], a2[q]);
+  }
+  gn_sum_over_rows(rows, t.slots, p.C);
+  for (int c = threadIdx.x; c < p.C; c += blockDim.x) {
+    total[c].x += rows[c].x;
+    total[c].y += rows[c].y;
+    groups[c] = make_double2((double)w.gamma[c] * rows[c].x, (double)w.gamma[c] * rows[c].y);
+  }
+  __syncthreads();
+  gn_sum_over_runs(groups, p.C, size);
+}
 
 template <class T, int V>
-__global__ __launch_bounds__(1024) void gn_adjoint_sums_kernel(GnShape p, GnAdjoint w, const T* x, long x_stride, const T* dy,
+__global__ __launch_bounds__(V == 1 ? 1024 : GN_THREADS) void gn_adjoint_sums_kernel(GnShape p, GnAdjoint w, const T* x, long x_stride, const T* dy,
                                                                long dy_stride, double2* part, float2* channel_part) {
-  extern __shared__ float2 srow[];    // [row slots][C], then [C] totals of the chunk
-  const int L = p.C / V, slots = blockDim.x / L, l = threadIdx.x % L, rr = threadIdx.x / L;
-  float2* total = srow + (size_t)slots * p.C;
+  extern __shared__ float2 srow[];
+  const GnLanes t = gn_lanes<V>(p.C);
+  float2* total = srow + (size_t)t.slots * p.C;
+  double2* groups = (double2*)(srow + (size_t)((t.slots + 2) & ~1) * p.C);
   const long r0 = (long)blockIdx.x * p.rows, r1 = min(r0 + p.rows, p.n);
   const int size = p.C / p.G;
   float ga[V], be[V];
 #pragma unroll
   for (int q = 0; q < V; ++q) {
-    ga[q] = w.gamma[l * V + q];
-    be[q] = w.beta[l * V + q];
+    ga[q] = w.gamma[t.l * V + q];
+    be[q] = w.beta[t.l * V + q];
   }
   for (int c = threadIdx.x; c < p.C; c += blockDim.x) total[c] = make_float2(0.0f, 0.0f);
   for (int s = gn_first_segment(p, r0); s < p.S; ++s) {
     const long b = max(gn_begin(p, s), r0), e = min(gn_begin(p, s + 1), r1);
     if (gn_begin(p, s) >= r1) break;
     if (b >= e) continue;
-    if (rr < slots) {
-      float mu[V], rs[V], a1[V], a2[V];
-#pragma unroll
-      for (int q = 0; q < V; ++q) {
-        const size_t at = (size_t)s * p.G + (l * V + q) / size;
-        mu[q] = w.mean[at];
-        rs[q] = w.rstd[at];
-        a1[q] = a2[q] = 0.0f;
-      }
-      for (long r = b + rr; r < e; r += slots) {
-        float v[V], d[V];
-        rt_load<T, V>(x + r * x_stride + l * V, v);
-        rt_load<T, V>(dy + r * dy_stride + l * V, d);
-#pragma unroll
-        for (int q = 0; q < V; ++q) {
-          const float h = (v[q] - mu[q]) * rs[q], z = h * ga[q] + be[q], sig = gn_sigmoid(z);
-          const float dz = d[q] * sig * (1.0f + z * (1.0f - sig));
-          a1[q] += dz;
-          a2[q] += dz * h;
-        }
-      }
-#pragma unroll
-      for (int q = 0; q < V; ++q) srow[rr * p.C + l * V + q] = make_float2(a1[q], a2[q]);
-    }
-    __syncthreads();
-    for (int c = threadIdx.x; c < p.C; c += blockDim.x) {
-      float2 t = srow[c];
-      for (int r = 1; r < slots; ++r) {
-        t.x += srow[r * p.C + c].x;
-        t.y += srow[r * p.C + c].y;
-      }
-      srow[c] = t;
-      total[c].x += t.x;
-      total[c].y += t.y;
-    }
-    __syncthreads();
-    for (int g = threadIdx.x; g < p.G; g += blockDim.x) {
-      double t1 = 0.0, t2 = 0.0;
-      for (int c = g * size; c < (g + 1) * size; ++c) {
-        t1 += (double)w.gamma[c] * srow[c].x;
-        t2 += (double)w.gamma[c] * srow[c].y;
-      }
-      part[(size_t)(blockIdx.x + s) * p.G + g] = make_double2(t1, t2);
-    }
+    gn_adjoint_rows<T, V>(p, w, x, x_stride, dy, dy_stride, s, b, e, ga, be, srow, total, groups);
+    for (int g = threadIdx.x; g < p.G; g += blockDim.x) part[(size_t)(blockIdx.x + s) * p.G + g] = groups[g * size];
     __syncthreads();
   }
   for (int c = threadIdx.x; c < p.C; c += blockDim.x) channel_part[(size_t)blockIdx.x * p.C + c] = total[c];
 }
 
-template <class T, int V>
-__global__ __launch_bounds__(1024) void gn_adjoint_write_kernel(GnShape p, GnAdjoint w, const T* x, long x_stride, const T* dy,
+template <class T, int V, bool ALONE>
+__global__ __launch_bounds__(V == 1 ? 1024 : GN_THREADS) void gn_adjoint_write_kernel(GnShape p, GnAdjoint w, const T* x, long x_stride, const T* dy,
                                                                 long dy_stride, T* dx, long dx_stride, float* dgamma,
                                                                 float* dbeta, const double2* part, const float2* channel_part) {
-  __shared__ double2 sums[1024], scratch[1024];
-  if ((int)blockIdx.x >= p.chunks) {   // the last workgroups add the channels' sums over the chunks, 16 channels each
+  extern __shared__ double2 smem[];
+  const GnLanes t = gn_lanes<V>(p.C);
+  float2* srow = (float2*)smem;                                             // ALONE: as in the sums
+  float2* total = srow + (size_t)t.slots * p.C;
+  double2* groups = ALONE ? (double2*)(srow + (size_t)((t.slots + 2) & ~1) * p.C) : smem;
+  if (!ALONE && (int)blockIdx.x >= p.chunks) {   // the last workgroups add the channels' sums over the chunks, 16 channels each
     const int c = ((int)blockIdx.x - p.chunks) * 16 + threadIdx.x % 16, per = blockDim.x / 16;
-    double2 t = make_double2(0.0, 0.0);
+    double2 u = make_double2(0.0, 0.0);
     if (c < p.C)
+#pragma unroll 4
       for (int k = threadIdx.x / 16; k < p.chunks; k += per) {
         const float2 v = channel_part[(size_t)k * p.C + c];
-        t.x += v.x;
-        t.y += v.y;
+        u.x += v.x;
+        u.y += v.y;
       }
-    scratch[threadIdx.x] = t;
-    __syncthreads();
+    smem[threadIdx.x] = u;
+    gn_sum_over_rows(smem, per, 16);
     if (threadIdx.x < 16 && c < p.C) {
-      for (int j = 1; j < per; ++j) {
-        t.x += scratch[j * 16 + threadIdx.x].x;
-        t.y += scratch[j * 16 + threadIdx.x].y;
-      }
-      dbeta[c] = (float)t.x;
-      dgamma[c] = (float)t.y;
+      dbeta[c] = (float)smem[threadIdx.x].x;
+      dgamma[c] = (float)smem[threadIdx.x].y;
     }
     return;
   }
-  const int L = p.C / V, slots = blockDim.x / L, l = threadIdx.x % L, rr = threadIdx.x / L;
   const long r0 = (long)blockIdx.x * p.rows, r1 = min(r0 + p.rows, p.n);
   const int size = p.C / p.G;
   float ga[V], be[V];
 #pragma unroll
   for (int q = 0; q < V; ++q) {
-    ga[q] = w.gamma[l * V + q];
-    be[q] = w.beta[l * V + q];
+    ga[q] = w.gamma[t.l * V + q];
+    be[q] = w.beta[t.l * V + q];
   }
+  if (ALONE)
+    for (int c = threadIdx.x; c < p.C; c += blockDim.x) total[c] = make_float2(0.0f, 0.0f);
   for (int s = gn_first_segment(p, r0); s < p.S; ++s) {
     const long sb = gn_begin(p, s), se = gn_begin(p, s + 1);
     const long b = max(sb, r0), e = min(se, r1);
     if (sb >= r1) break;
     if (b >= e) continue;
-    gn_segment_sums(p, part, s, sums, scratch);
-    if (rr < slots) {
+    if (ALONE) gn_adjoint_rows<T, V>(p, w, x, x_stride, dy, dy_stride, s, b, e, ga, be, srow, total, groups);
+    else gn_segment_sums(p, part, s, groups);
+    if (t.rr < t.slots) {
       float mu[V], rs[V], m1[V], m2[V];
       const double inv = 1.0 / ((double)(se - sb) * size);
 #pragma unroll
       for (int q = 0; q < V; ++q) {
-        const int g = (l * V + q) / size;
+        const int g = (t.l * V + q) / size;
         const size_t at = (size_t)s * p.G + g;
         mu[q] = w.mean[at];
         rs[q] = w.rstd[at];
-        m1[q] = (float)(sums[g].x * inv);
-        m2[q] = (float)(sums[g].y * inv);
+        m1[q] = (float)(groups[ALONE ? g * size : g].x * inv);
+        m2[q] = (float)(groups[ALONE ? g * size : g].y * inv);
       }
-      for (long r = b + rr; r < e; r += slots) {
-        float v[V], d[V];
-        rt_load<T, V>(x + r * x_stride + l * V, v);
-        rt_load<T, V>(dy + r * dy_stride + l * V, d);
+      gn_rows_backwards(b, e, t.rr, t.slots, [&](long r, int rows) {
+        float v[GN_ROWS][V], d[GN_ROWS][V];
 #pragma unroll
-        for (int q = 0; q < V; ++q) {
-          const float h = (v[q] - mu[q]) * rs[q], z = h * ga[q] + be[q], sig = gn_sigmoid(z);
-          const float dz = d[q] * sig * (1.0f + z * (1.0f - sig));
-          v[q] = rs[q] * (ga[q] * dz - m1[q] - h * m2[q]);
+        for (int k = 0; k < GN_ROWS; ++k) {
+          const long at = r + (long)min(k, rows - 1) * t.slots;
+          rt_load<T, V>(x + at * x_stride + t.l * V, v[k]);
+          rt_load<T, V>(dy + at * dy_stride + t.l * V, d[k]);
         }
-        rt_store<T, V>(dx + r * dx_stride + l * V, v);
-      }
+#pragma unroll
+        for (int k = 0; k < GN_ROWS; ++k) {
+          if (k >= rows) break;
+#pragma unroll
+          for (int q = 0; q < V; ++q) {
+            const float h = (v[k][q] - mu[q]) * rs[q], z = h * ga[q] + be[q], sig = gn_sigmoid(z);
+            const float dz = d[k][q] * sig * (1.0f + z * (1.0f - sig));
+            v[k][q] = rs[q] * (ga[q] * dz - m1[q] - h * m2[q]);
+          }
+          rt_store<T, V>(dx + (r + (long)k * t.slots) * dx_stride + t.l * V, v[k]);
+        }
+      });
     }
     __syncthreads();
+  }
+  if (ALONE) {
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.C; c += blockDim.x) {
+      dbeta[c] = total[c].x;
+      dgamma[c] = total[c].y;
+    }
   }
 }
 
@@ -335,6 +434,7 @@ GnShape gn_shape(int64_t n, int32_t C, int32_t G, int32_t S, const int32_t* ptr,
   const long least = (GN_CHUNK_BYTES + (long)C * element - 1) / ((long)C * element);
   p.rows = (n + GN_CHUNKS - 1) / GN_CHUNKS;
   if (p.rows < least) p.rows = least;
+  if ((double)n * C * element <= GN_ALONE_BYTES) p.rows = n > 0 ? n : 1;
   p.chunks = (int)((n + p.rows - 1) / p.rows);
   return p;
 }
@@ -368,21 +468,28 @@ int gn_width(int32_t C, std::initializer_list<const void*> at, std::initializer_
 }
 
 struct GnLaunch { int threads, slots; };
-GnLaunch gn_launch(int C, int V) {
-  const int L = C / V, threads = L <= 256 ? 256 : 1024;
+GnLaunch gn_launch(int C, int V, bool halved = false) {
+  const int L = C / V, threads = L > GN_THREADS ? 1024 : halved ? GN_THREADS / 2 : GN_THREADS;      // (V > 1: at most 256 pieces)
   return {threads, threads / L};
 }
 
 template <class T, int V>
 int gn_forward(egnn_ctx* ctx, const GnShape& p, const void* x, int64_t xs, const float* gamma, const float* beta, float eps, void* y,
                int64_t ys, float* mean, float* rstd, void* ws, hipStream_t st) {
-  const GnLaunch at = gn_launch(p.C, V);
+  // eight sums a thread, where a thread's values are of several groups: half the threads, for LDS
+  const GnLaunch at = gn_launch(p.C, V, V == 8 && p.C / p.G % V != 0);
   double2* part = (double2*)ws;
   float* first = (float*)((char*)ws + gn_part_bytes(p));
-  hipLaunchKernelGGL((gn_sums_kernel<T, V>), dim3(p.chunks), dim3(at.threads), (size_t)at.slots * p.C * sizeof(double2), st, p,
-                     (const T*)x, (long)xs, part, first);
-  hipLaunchKernelGGL((gn_write_kernel<T, V>), dim3(p.chunks), dim3(at.threads), 0, st, p, (const T*)x, (long)xs, gamma, beta, eps,
-                     (T*)y, (long)ys, mean, rstd, (const double2*)part, (const float*)first);
+  const size_t sums = (size_t)at.slots * (p.C / p.G % V ? p.C : p.C / V) * sizeof(double2);
+  if (p.chunks == 1) {
+    hipLaunchKernelGGL((gn_write_kernel<T, V, true>), dim3(1), dim3(at.threads), sums, st, p, (const T*)x, (long)xs, gamma, beta, eps, (T*)y,
+                       (long)ys, mean, rstd, (const double2*)nullptr, (const float*)nullptr);
+  } else {
+    const size_t slots = (size_t)(p.G > at.threads ? p.G : at.threads) * sizeof(double2);
+    hipLaunchKernelGGL((gn_sums_kernel<T, V>), dim3(p.chunks), dim3(at.threads), sums, st, p, (const T*)x, (long)xs, part, first);
+    hipLaunchKernelGGL((gn_write_kernel<T, V, false>), dim3(p.chunks), dim3(at.threads), slots, st, p, (const T*)x, (long)xs, gamma, beta, eps,
+                       (T*)y, (long)ys, mean, rstd, (const double2*)part, (const float*)first);
+  }
   EGNN_LAUNCH_CHECK(ctx, "group_norm");
   return EGNN_OK;
 }
@@ -393,11 +500,18 @@ int gn_backward(egnn_ctx* ctx, const GnShape& p, const GnAdjoint& w, const void*
   const GnLaunch at = gn_launch(p.C, V);
   double2* part = (double2*)ws;
   float2* channel_part = (float2*)((char*)ws + gn_part_bytes(p));
-  hipLaunchKernelGGL((gn_adjoint_sums_kernel<T, V>), dim3(p.chunks), dim3(at.threads), (size_t)(at.slots + 1) * p.C * sizeof(float2),
-                     st, p, w, (const T*)x, (long)xs, (const T*)dy, (long)dys, part, channel_part);
-  hipLaunchKernelGGL((gn_adjoint_write_kernel<T, V>), dim3(p.chunks + (p.C + 15) / 16), dim3(at.threads), 0, st, p, w, (const T*)x,
-                     (long)xs, (const T*)dy, (long)dys, (T*)dx, (long)dxs, dgamma, dbeta, (const double2*)part,
-                     (const float2*)channel_part);
+  const size_t sums = gn_adjoint_lds(p.C, at.slots);
+  if (p.chunks == 1) {
+    hipLaunchKernelGGL((gn_adjoint_write_kernel<T, V, true>), dim3(1), dim3(at.threads), sums, st, p, w, (const T*)x, (long)xs,
+                       (const T*)dy, (long)dys, (T*)dx, (long)dxs, dgamma, dbeta, (const double2*)nullptr, (const float2*)nullptr);
+  } else {
+    const size_t slots = (size_t)(p.G > at.threads ? p.G : at.threads) * sizeof(double2);
+    hipLaunchKernelGGL((gn_adjoint_sums_kernel<T, V>), dim3(p.chunks), dim3(at.threads), sums, st, p, w, (const T*)x, (long)xs,
+                       (const T*)dy, (long)dys, part, channel_part);
+    hipLaunchKernelGGL((gn_adjoint_write_kernel<T, V, false>), dim3(p.chunks + (p.C + 15) / 16), dim3(at.threads), slots, st, p, w, (const T*)x,
+                       (long)xs, (const T*)dy, (long)dys, (T*)dx, (long)dxs, dgamma, dbeta, (const double2*)part,
+                       (const float2*)channel_part);
+  }
   EGNN_LAUNCH_CHECK(ctx, "group_norm_backward");
   return EGNN_OK;
 }
