@@ -25,6 +25,7 @@ __global__ __launch_bounds__(GR_THREADS) void gr_count_kernel(const int* key, lo
   for (int g = threadIdx.x; g < G; g += GR_THREADS) counts[(size_t)blockIdx.x * G + g] = s[g];
 }
 
+// counts NULL: the only workgroup, which counts itself
 __global__ __launch_bounds__(GR_THREADS) void gr_place_kernel(const int* key, long n, int G, int lmax, long chunk, const int* counts,
                                                               int* ptr, int* perm) {
   __shared__ int base[GR_MAX_GROUPS], total[GR_MAX_GROUPS], first[GR_MAX_GROUPS], wave_count[GR_WAVES][GR_MAX_GROUPS];
@@ -32,21 +33,33 @@ __global__ __launch_bounds__(GR_THREADS) void gr_place_kernel(const int* key, lo
   const int degrees = lmax < 0 ? 1 : lmax + 1, D = degrees * degrees;
   for (int g = tid; g < G; g += GR_THREADS) {
     int before = 0, all = 0;
-    for (int c = 0; c < (int)gridDim.x; ++c) {
-      const int v = counts[(size_t)c * G + g];
-      before += c < (int)blockIdx.x ? v : 0;
-      all += v;
-    }
+    if (counts)
+#pragma unroll 8
+      for (int c = 0; c < (int)gridDim.x; ++c) {
+        const int v = counts[(size_t)c * G + g];
+        before += c < (int)blockIdx.x ? v : 0;
+        all += v;
+      }
     base[g] = before;
     total[g] = all;
     for (int w = 0; w < GR_WAVES; ++w) wave_count[w][g] = 0;
   }
+  if (!counts) {
+    __syncthreads();
+    for (long i = tid; i < n; i += GR_THREADS) atomicAdd(&total[gr_key(key, i, G)], 1);   // whole numbers: any order
+  }
   __syncthreads();
-  if (tid == 0) {
+  if (wave == 0) {
     int at = 0;
-    for (int g = 0; g < G; ++g) {
-      first[g] = at;
-      at += total[g];
+    for (int g0 = 0; g0 < G; g0 += 64) {
+      const int mine = g0 + lane < G ? total[g0 + lane] : 0;
+      int sum = mine;
+      for (int h = 1; h < 64; h <<= 1) {
+        const int v = __shfl_up(sum, h);
+        if (lane >= h) sum += v;
+      }
+      if (g0 + lane < G) first[g0 + lane] = at + sum - mine;
+      at += __shfl(sum, 63);
     }
   }
   __syncthreads();
@@ -1016,9 +1029,9 @@ extern "C" int egnn_group_rows(egnn_ctx* ctx, const int32_t* key, int64_t n, int
     return egnn_fail(ctx, EGNN_EWS, "group_rows: workspace too small or not 256-byte aligned");
   hipStream_t st = (hipStream_t)stream;
   const unsigned chunks = (unsigned)gr_chunks(n);
-  hipLaunchKernelGGL(gr_count_kernel, dim3(chunks), dim3(GR_THREADS), 0, st, key, (long)n, n_groups, gr_chunk(n), (int*)ws);
-  hipLaunchKernelGGL(gr_place_kernel, dim3(chunks), dim3(GR_THREADS), 0, st, key, (long)n, n_groups, lmax, gr_chunk(n), (const int*)ws,
-                     ptr, perm);
+  if (chunks > 1) hipLaunchKernelGGL(gr_count_kernel, dim3(chunks), dim3(GR_THREADS), 0, st, key, (long)n, n_groups, gr_chunk(n), (int*)ws);
+  hipLaunchKernelGGL(gr_place_kernel, dim3(chunks), dim3(GR_THREADS), 0, st, key, (long)n, n_groups, lmax, gr_chunk(n),
+                     chunks > 1 ? (const int*)ws : nullptr, ptr, perm);
   EGNN_LAUNCH_CHECK(ctx, "group_rows");
   return EGNN_OK;
 }

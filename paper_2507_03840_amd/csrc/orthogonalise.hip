@@ -124,7 +124,13 @@ __global__ __launch_bounds__(256) void ou_pieces_kernel(OuShape p, OuInput<T> in
 enum OuProduct { OU_GRAM, OU_POLY, OU_UPDATE, OU_LAST };
 
 template <class T>
-struct OuOut { T* y; const float* W; float keep, scale; bool eights; };   // y = q, or keep W - scale q; rows of y in aligned eights
+struct OuOut {     // y = q, or keep W - scale q
+  T* y;
+  const float* W;
+  float keep, scale;
+  bool eights;        // rows of y in aligned eights
+  bool fours;         // tall, and rows of all the caller's matrices in aligned fours
+};
 
 struct OuOperands {
   const _Float16 *A, *B;   // per matrix [P pieces][I][K], [P pieces][J][K]; x^T always has two pieces
@@ -151,39 +157,42 @@ __device__ __forceinline__ void ou_lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// C = A B^T of one tile TILE x TILE: four waves, each a quarter (TILE / 2 squared) in 32 x 32 blocks.  64 contraction indices a
+// C = A B^T of one tile TILE x TILE: four waves, each a quarter (TILE / 2 squared) in 32 x 32 blocks; for tiles of 64 twice four, each
+// with half of a turn's contraction (the chain of dependent products of a turn is what a small tile waits for).  64 contraction indices a
 // turn, brought straight into one of STAGES LDS buffers, STAGES - 1 turns ahead: with one wave per SIMD nothing else hides the way to
 // memory.  A row of 128 bytes lies in LDS as eight pieces of 16 bytes, piece c at place c ^ (row & 7): eight lanes that read the same
 // piece of eight rows meet all banks.  The operands of a step of 16 are read from LDS while the products of the one before run.
 template <int P, int TILE>
 struct OuTile {
   static constexpr int STAGES = P * TILE >= 256 ? 2 : 4;
+  static constexpr int SETS = TILE == 64 ? 2 : 1, THREADS = 256 * SETS;   // sets of four waves
   static constexpr int PLANE = TILE * 8, STAGE = 2 * P * PLANE;          // uint4
-  static constexpr int LOADS = 2 * P * TILE / 32;                         // of a wave per turn
+  static constexpr int LOADS = 2 * P * TILE / 32 / SETS;                  // of a wave per turn
   static constexpr size_t LDS = (size_t)STAGES * STAGE * 16;
 };
 
 template <class T, int P, int TILE, OuProduct WHAT>
-__global__ __launch_bounds__(256) void ou_product_kernel(OuShape p, OuOperands o, OuOut<T> out) {
+__global__ __launch_bounds__((OuTile<P, TILE>::THREADS)) void ou_product_kernel(OuShape p, OuOperands o, OuOut<T> out) {
   extern __shared__ uint4 smem[];                     // [STAGES][2 operands][P][TILE][8]
   constexpr bool STEP = WHAT == OU_UPDATE || WHAT == OU_LAST;   // p x
   constexpr int PB = STEP ? 2 : P;
   typedef OuTile<P, TILE> Tile;
   constexpr int HALF = TILE / 2, B = HALF / 32, PLANE = Tile::PLANE, STAGE = Tile::STAGE, STAGES = Tile::STAGES;
+  constexpr int SETS = Tile::SETS, THREADS = Tile::THREADS, ROUNDS = TILE / 32 / SETS;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const size_t z = blockIdx.z;
   const int i0 = blockIdx.y * TILE, j0 = blockIdx.x * TILE;
   const size_t plane_a = (size_t)o.I * o.K, plane_b = (size_t)o.J * o.K;
   const _Float16* A = o.A + z * P * plane_a;
   const _Float16* Bm = o.B + z * PB * plane_b;
-  const int wi = (wave >> 1) * HALF, wj = (wave & 1) * HALF;
+  const int wi = (wave >> 1 & 1) * HALF, wj = (wave & 1) * HALF, set = wave >> 2;
 
   // lane's place in a load of eight rows
   const int lrow = lane >> 3, lpiece = (lane & 7) ^ lrow;
-  const _Float16 *pa[TILE / 32], *pb[TILE / 32];
+  const _Float16 *pa[ROUNDS], *pb[ROUNDS];
 #pragma unroll
-  for (int r = 0; r < TILE / 32; ++r) {
-    const int row = (r * 4 + wave) * 8 + lrow;
+  for (int r = 0; r < ROUNDS; ++r) {
+    const int row = (r * 4 * SETS + wave) * 8 + lrow;
     pa[r] = A + (size_t)min(i0 + row, o.I - 1) * o.K + lpiece * 8;
     pb[r] = Bm + (size_t)min(j0 + row, o.J - 1) * o.K + lpiece * 8;
   }
@@ -192,9 +201,9 @@ __global__ __launch_bounds__(256) void ou_product_kernel(OuShape p, OuOperands o
 #pragma unroll
     for (int q = 0; q < P; ++q)
 #pragma unroll
-      for (int r = 0; r < TILE / 32; ++r) {
-        __builtin_amdgcn_global_load_lds((ou_gp)(pa[r] + q * plane_a + turn * 64), (ou_lp)(to + q * PLANE + r * 256), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((ou_gp)(pb[r] + q * plane_b + turn * 64), (ou_lp)(to + (P + q) * PLANE + r * 256), 16, 0, 0);
+      for (int r = 0; r < ROUNDS; ++r) {
+        __builtin_amdgcn_global_load_lds((ou_gp)(pa[r] + q * plane_a + turn * 64), (ou_lp)(to + q * PLANE + r * 256 * SETS), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((ou_gp)(pb[r] + q * plane_b + turn * 64), (ou_lp)(to + (P + q) * PLANE + r * 256 * SETS), 16, 0, 0);
       }
   };
 
@@ -219,7 +228,7 @@ __global__ __launch_bounds__(256) void ou_product_kernel(OuShape p, OuOperands o
     stage = stage + 1 == STAGES ? 0 : stage + 1;
     ou_h8 a[2][B][P], b[2][B][P];
     auto operands = [&](int s) {
-      const int place = (2 * s + hh) ^ (r32 & 7);
+      const int place = (2 * (s + set * (4 / SETS)) + hh) ^ (r32 & 7);
 #pragma unroll
       for (int x = 0; x < B; ++x)
 #pragma unroll
@@ -230,8 +239,8 @@ __global__ __launch_bounds__(256) void ou_product_kernel(OuShape p, OuOperands o
     };
     operands(0);
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      if (s < 3) operands(s + 1);
+    for (int s = 0; s < 4 / SETS; ++s) {
+      if (s + 1 < 4 / SETS) operands(s + 1);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int t = P == 2 ? 0 : 2; t < 3; ++t)     // lo hi, hi lo, hi hi
@@ -253,22 +262,32 @@ __global__ __launch_bounds__(256) void ou_product_kernel(OuShape p, OuOperands o
   float4* tile = (float4*)smem;                      // [j][SLOTS]
   auto slot = [](int j, int i4) { return j * SLOTS + (i4 ^ (j & (SLOTS - 1))); };
 #pragma unroll
-  for (int x = 0; x < B; ++x)
+  for (int part = 0; part < SETS; ++part) {
+    if (set == part)
 #pragma unroll
-    for (int y = 0; y < B; ++y)
+      for (int x = 0; x < B; ++x)
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        tile[slot(wj + 32 * y + r32, (wi + 32 * x + 8 * r + 4 * hh) >> 2)] =
-            make_float4(acc[x][y][4 * r], acc[x][y][4 * r + 1], acc[x][y][4 * r + 2], acc[x][y][4 * r + 3]);
+        for (int y = 0; y < B; ++y)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float4& t = tile[slot(wj + 32 * y + r32, (wi + 32 * x + 8 * r + 4 * hh) >> 2)];
+            float4 v = make_float4(acc[x][y][4 * r], acc[x][y][4 * r + 1], acc[x][y][4 * r + 2], acc[x][y][4 * r + 3]);
+            if (part) {
+              v.x += t.x; v.y += t.y; v.z += t.z; v.w += t.w;
+            }
+            t = v;
+          }
+    if (part + 1 < SETS) ou_lds_barrier();
+  }
   // Whatever has to be loaded is loaded before the first result is stored: loads and stores return in order, and a load behind a store
   // would wait for it (so did barriers that wait for stores).
   const size_t plane_c = (size_t)o.I * o.J;
-  constexpr int ACROSS = TILE / 8, ITEMS = TILE * ACROSS / 256;   // threads along a row, eight values each
+  constexpr int ACROSS = TILE / 8, ITEMS = TILE * ACROSS / THREADS;   // threads along a row, eight values each
   constexpr bool OLD = WHAT == OU_POLY || (STEP && P == 1);       // + b g, or + a x
   const int n = p.n, m = p.m, across = tid % ACROSS * 8;
   ou_h8 oh[OLD ? ITEMS : 1], ol[OLD && PB == 2 ? ITEMS : 1];
   auto along_i = [&](int e, int& i, int& j, int& jl) {            // eight i of one j
-    jl = tid / ACROSS + e * (256 / ACROSS);
+    jl = tid / ACROSS + e * (THREADS / ACROSS);
     i = i0 + across;
     j = j0 + jl;
     return i < o.I && j < o.J;
@@ -287,7 +306,7 @@ __global__ __launch_bounds__(256) void ou_product_kernel(OuShape p, OuOperands o
   if (WHAT == OU_LAST && out.W)
 #pragma unroll
     for (int e = 0; e < ITEMS; ++e) {
-      const int r = (flip ? i0 : j0) + tid / ACROSS + e * (256 / ACROSS), c = (flip ? j0 : i0) + across;
+      const int r = (flip ? i0 : j0) + tid / ACROSS + e * (THREADS / ACROSS), c = (flip ? j0 : i0) + across;
       const float* w = out.W + z * n * m + (size_t)min(r, (flip ? n : m) - 1) * p.cols;
 #pragma unroll
       for (int q = 0; q < 8; ++q) keep[e][q] = out.keep * w[min(c + q, p.cols - 1)];
@@ -351,7 +370,7 @@ __global__ __launch_bounds__(256) void ou_product_kernel(OuShape p, OuOperands o
   const float* flat = (const float*)smem;
 #pragma unroll
   for (int e = 0; e < ITEMS; ++e) {                                // eight j of one i
-    const int il = tid / ACROSS + e * (256 / ACROSS), i = i0 + il, j = j0 + across;
+    const int il = tid / ACROSS + e * (THREADS / ACROSS), i = i0 + il, j = j0 + across;
     if (i >= o.I || j >= o.J) continue;
     float v[8];
 #pragma unroll
@@ -455,30 +474,55 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
     v[0] = __builtin_bit_cast(ou_h8, f[0]);
     v[1] = __builtin_bit_cast(ou_h8, f[64]);
   };
-  // element of the caller's matrix for register q of block b of fragments of x; -1 past the edges
-  auto place = [&](int first, int b, int q) -> long {
-    const int i = 32 * b + 8 * (q >> 2) + 4 * hh + (q & 3), c = first + r32;
-    return i < p.n && c < p.m ? (long)(at0 + (p.tall ? (size_t)c * p.cols + i : (size_t)i * p.cols + c)) : -1;
+  // First of the four elements of the caller's matrix (one apart, or a row) for registers 4 r .. 4 r + 3 of block b of fragments of x, and
+  // how many of them there are.
+  const size_t apart = p.tall ? 1 : p.cols;
+  auto place = [&](int first, int b, int r, size_t& at) {
+    const int i = 32 * b + 8 * r + 4 * hh, c = first + r32;
+    at = at0 + (p.tall ? (size_t)c * p.cols + i : (size_t)i * p.cols + c);
+    return c < p.m ? min(4, p.n - i) : 0;
+  };
+  auto load4 = [&](const auto* from, size_t at, int there, float (&v)[4]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = 0.0f;
+    if (out.fours && there == 4) {
+      rt_load(from + at, v);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (q < there) v[q] = (float)from[at + q * apart];
+    }
+  };
+  auto store4 = [&](auto* to, size_t at, int there, const float (&v)[4]) {
+    if (out.fours && there == 4) {
+      rt_store(to + at, v);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (q < there) to[at + q * apart] = (std::remove_pointer_t<decltype(to)>)v[q];
+    }
   };
   // u of one turn's rows; the new momentum on the way
   auto input = [&](int first, bool write, float (&u)[NB][16]) {
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int q = 0; q < 16; ++q) {
-        const long at = place(first, b, q);
-        float v = 0.0f;
-        if (at >= 0) {
-          v = (float)in.u[at];
-          if (m_old && write) {
-            const float mm = in.beta * m_old[at] + v;
-            m_new[at] = mm;
-            v = v + in.beta * mm;
-          } else if (m_old) {
-            v = v + in.beta * m_new[at];
+      for (int r = 0; r < 4; ++r) {
+        size_t at;
+        const int there = place(first, b, r, at);
+        float v[4], mm[4];
+        load4(in.u, at, there, v);
+        if (m_old) {
+          load4(write ? m_old : m_new, at, there, mm);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            if (write) mm[q] = in.beta * mm[q] + v[q];
+            v[q] = v[q] + in.beta * mm[q];
           }
+          if (write) store4(m_new, at, there, mm);
         }
-        u[b][q] = v;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) u[b][4 * r + q] = v[q];
       }
   };
 
@@ -664,16 +708,31 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
 
   auto finish = [&]() {
     for (int turn = 0; turn < turns; ++turn) {
+      float old[NB][4][4];
+      if (out.W)
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            size_t at;
+            const int there = place(row_of(turn), b, r, at);
+            load4(out.W, at, there, old[b][r]);
+          }
       if (!ALONE) load_x(turn);
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         const ou_f16v last = times_p(b, true);
 #pragma unroll
-        for (int q = 0; q < 16; ++q) {
-          const long at = place(row_of(turn), b, q);
-          if (at < 0) continue;
-          const float v = last[q] * (1.0f / (OU_SP * OU_SX));
-          out.y[at] = (T)(out.W ? out.keep * out.W[at] - out.scale * v : v);
+        for (int r = 0; r < 4; ++r) {
+          size_t at;
+          const int there = place(row_of(turn), b, r, at);
+          float v[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            v[q] = last[4 * r + q] * (1.0f / (OU_SP * OU_SX));
+            if (out.W) v[q] = out.keep * old[b][r][q] - out.scale * v[q];
+          }
+          store4(out.y, at, there, v);
         }
       }
     }
@@ -809,7 +868,7 @@ int ou_product_tile(egnn_ctx* ctx, const OuShape& p, const OuOperands& o, const 
     ready = true;
   }
   const dim3 grid((o.J + TILE - 1) / TILE, (o.I + TILE - 1) / TILE, p.batch);
-  hipLaunchKernelGGL((ou_product_kernel<T, P, TILE, WHAT>), grid, dim3(256), lds, st, p, o, out);
+  hipLaunchKernelGGL((ou_product_kernel<T, P, TILE, WHAT>), grid, dim3(OuTile<P, TILE>::THREADS), lds, st, p, o, out);
   EGNN_LAUNCH_CHECK(ctx, "orthogonalise");
   return EGNN_OK;
 }
@@ -860,7 +919,8 @@ int ou_check(egnn_ctx* ctx, const char* who, int32_t batch, int32_t rows, int32_
 template <class T>
 int ou_matrices(egnn_ctx* ctx, int32_t dtype, const OuShape& p, const void* g, int steps, void* y, void* ws, hipStream_t st) {
   const OuInput<T> in{(const T*)g, nullptr, 0.0f};
-  const OuOut<T> out{(T*)y, nullptr, 0.0f, 0.0f, p.cols % 8 == 0 && (uintptr_t)y % 16 == 0};
+  const OuOut<T> out{(T*)y, nullptr, 0.0f, 0.0f, p.cols % 8 == 0 && (uintptr_t)y % 16 == 0,
+                     p.tall && p.cols % 4 == 0 && ((uintptr_t)g | (uintptr_t)y) % (4 * sizeof(T)) == 0};
   if constexpr (std::is_same<T, __bf16>::value)
     if (ou_pieces(p, dtype) == 1) return ou_run<T, 1>(ctx, p, in, nullptr, nullptr, steps, out, ws, st);
   return ou_run<T, 2>(ctx, p, in, nullptr, nullptr, steps, out, ws, st);
@@ -903,6 +963,7 @@ extern "C" int egnn_muon_step(egnn_ctx* ctx, const float* W, const float* g, con
     return egnn_fail(ctx, EGNN_EWS, "muon_step: workspace too small or not 256-byte aligned");
   const float scale = (float)((double)lr * sqrt(rows > cols ? (double)rows / cols : 1.0));
   const float keep = (float)(1.0 - (double)lr * (double)weight_decay);
-  return ou_run<float, 2>(ctx, p, OuInput<float>{g, m_out, beta}, m, m_out, steps, OuOut<float>{W_out, W, keep, scale, cols % 8 == 0 && (uintptr_t)W_out % 16 == 0}, ws,
-                          (hipStream_t)stream);
+  const uintptr_t all = (uintptr_t)g | (uintptr_t)m | (uintptr_t)m_out | (uintptr_t)W | (uintptr_t)W_out;
+  const OuOut<float> out{W_out, W, keep, scale, cols % 8 == 0 && (uintptr_t)W_out % 16 == 0, p.tall && cols % 4 == 0 && all % 16 == 0};
+  return ou_run<float, 2>(ctx, p, OuInput<float>{g, m_out, beta}, m, m_out, steps, out, ws, (hipStream_t)stream);
 }
