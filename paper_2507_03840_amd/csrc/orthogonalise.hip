@@ -400,8 +400,8 @@ __global__ __launch_bounds__((OuTile<P, TILE>::THREADS)) void ou_product_kernel(
 // Everything stays in the order in which 32 x 32 products land in the accumulators: a lane holds one column and sixteen rows, eight and
 // eight (fragment t = 0, 1).  Read as an operand, the lane's column is the operand's row and the sixteen rows are contraction indices, in an
 // order that does not matter as long as both operands share it.  So the fragments of g serve as both operands of g g (g and p are
-// symmetric), those of x^T (lane = column j, registers = rows k) as both operands of g, and those of x (lane = k, registers = i) with p's
-// make the next x^T and, with the operands exchanged, the next x: twice the products, but no value ever changes lanes.
+// symmetric), those of x (lane = k, registers = i) with p's make the next x, and x^T (lane = column j, registers = rows k), both operands of g,
+// is x times the identity: no value ever changes lanes but in the matrix cores.
 // Until step 1 a slab is scaled by its own norm: the sums of squares of the others come with their parts of g, no pass for |u| alone.
 //
 // What bounds it: the chain of dependent products, conversions and barriers of a step, and the reading of the parts (16 KB a slab from L2).
@@ -572,6 +572,21 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
         for (int b = 0; b < NB; ++b) g[a][b] = os_product(xt[a][t], xt[b][t], g[a][b]);
   };
 
+  // x^T of block b of x by a product with the identity: exact, as every value is two pieces.  (Made by a product with p of its own, as x
+  // is, x^T would be rounded apart from x: twice the error of a result of full rank.)
+  auto turned = [&](int b, ou_h8 (&to)[2][2]) {
+    ou_f16v rows = os_zero();
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      ou_h8 one;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) one[q] = (_Float16)(16 * t + 8 * (q >> 2) + 4 * hh + (q & 3) == r32 ? 1.0f : 0.0f);
+      rows = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[b][t][1], one, rows, 0, 0, 0);
+      rows = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[b][t][0], one, rows, 0, 0, 0);
+    }
+    cut(rows, 1.0f, to);
+  };
+
   // step 0: x = u / |u| and its g
   auto begin = [&]() {
     float u[NB][16];
@@ -592,20 +607,14 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
       ou_h8 xt[NB][2][2];
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        ou_f16v rows = os_zero();      // x^T by a product with the identity: exact, as every value is two pieces
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           float v[8];
 #pragma unroll
           for (int q = 0; q < 8; ++q) v[q] = (float)((double)u[b][8 * t + q] * inverse);
           os_cut(v, OU_SX, x[b][t][0], x[b][t][1]);
-          ou_h8 one;
-#pragma unroll
-          for (int q = 0; q < 8; ++q) one[q] = (_Float16)(16 * t + 8 * (q >> 2) + 4 * hh + (q & 3) == r32 ? 1.0f : 0.0f);
-          rows = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[b][t][1], one, rows, 0, 0, 0);
-          rows = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[b][t][0], one, rows, 0, 0, 0);
         }
-        cut(rows, 1.0f, xt[b]);
+        turned(b, xt[b]);
       }
       if (!ALONE) store_x(turn);
       add_g(xt);
@@ -674,8 +683,8 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
     __syncthreads();
   };
 
-  // x^T p (FLIP: p x) of column block b
-  auto times_p = [&](int b, bool flip) {
+  // p x, row block b
+  auto times_p = [&](int b) {
     ou_f16v acc = os_zero();
 #pragma unroll
     for (int c = 0; c < NB; ++c)
@@ -683,7 +692,7 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
       for (int t = 0; t < 2; ++t) {
         ou_h8 pf[2];
         fragment(sp, c, b, t, pf);
-        acc = flip ? os_product(pf, x[c][t], acc) : os_product(x[c][t], pf, acc);
+        acc = os_product(pf, x[c][t], acc);
       }
     return acc;
   };
@@ -695,13 +704,12 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
       ou_h8 xt[NB][2][2];
       ou_f16v next[NB];
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        cut(times_p(b, false), 1.0f / OU_SP, xt[b]);
-        next[b] = times_p(b, true);
-      }
+      for (int b = 0; b < NB; ++b) next[b] = times_p(b);
 #pragma unroll
       for (int b = 0; b < NB; ++b) cut(next[b], 1.0f / OU_SP, x[b]);
       if (!ALONE) store_x(turn);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) turned(b, xt[b]);
       add_g(xt);
     }
   };
@@ -721,7 +729,7 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
       if (!ALONE) load_x(turn);
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        const ou_f16v last = times_p(b, true);
+        const ou_f16v last = times_p(b);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           size_t at;
