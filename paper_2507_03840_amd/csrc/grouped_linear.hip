@@ -342,13 +342,54 @@ __device__ __forceinline__ bool gl_slot(const GlRows& p, long chunk, int t, int&
   return c >= 0 && r0 < r1;
 }
 
+// Units (group, tile of its weight gradient) of one XCD where every slot is a group: consecutive ones, so that the tiles of a group share
+// its rows in one L2, and so many that each XCD gets an eighth of the rows to be read (groups may differ in size by any factor).
+// 256 threads; returns the units first .. last - 1.
+__device__ __forceinline__ void gl_units(const GlRows& p, int tiles, int xcd, long& first, long& last) {
+  constexpr long LEAST = 64;                      // a unit costs as much as so many rows, whatever its rows
+  __shared__ long s_sum[4], s_unit[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  long total = (long)p.G * LEAST;
+  {
+    long rows = 0;
+    for (int g = tid; g < p.G; g += 256) rows += max(gl_begin(p, g + 1) - gl_begin(p, g), 0l);
+    for (int h = 32; h; h >>= 1) rows += __shfl_xor(rows, h);
+    if (lane == 0) s_sum[wave] = rows;
+    if (tid < 2) s_unit[tid] = (long)p.G * tiles;
+    __syncthreads();
+    total += s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
+  }
+  long before = 0;
+  for (int g0 = 0; g0 < p.G; g0 += 256) {
+    const int g = g0 + tid;
+    const long mine = g < p.G ? max(gl_begin(p, g + 1) - gl_begin(p, g), 0l) + LEAST : 0;
+    long sum = mine;
+    for (int h = 1; h < 64; h <<= 1) {
+      const long v = __shfl_up(sum, h);
+      if (lane >= h) sum += v;
+    }
+    __syncthreads();
+    if (lane == 63) s_sum[wave] = sum;
+    __syncthreads();
+    long start = before + sum - mine;
+    for (int w = 0; w < wave; ++w) start += s_sum[w];
+    for (int x = 0; x < 2; ++x) {                 // the first unit whose work begins at or behind the XCD's share
+      const long at = total * (xcd + x) / 8;
+      if (mine && at >= start && at < start + mine) s_unit[x] = (long)g * tiles + ((at - start) * tiles + mine - 1) / mine;
+    }
+    before += s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
+  }
+  __syncthreads();
+  first = s_unit[0];
+  last = xcd == 7 ? (long)p.G * tiles : s_unit[1];
+}
+
 // 256 threads, four waves, each a quarter of the BM x BN tile in 32 x 32 blocks.  Tiles go from memory to registers DEPTH turns ahead, are cut
 // into pieces on the way to one of two LDS buffers, and are contracted from the other.
 // NARROW: a side that is read along has fewer than eight values.
 constexpr int GL_PIECE = 2048;     // GL_WEIGHTS: row numbers kept in LDS (a row number loaded in turn would have to wait for the rows before it)
 template <class T, GlKind KIND, int BM, int BN, int KS, bool NARROW>
-__global__ __launch_bounds__(256) void gl_tile_kernel(GlArgs<T> g) {
-  extern __shared__ __align__(16) char smem[];
+__device__ __forceinline__ void gl_tile(const GlArgs<T>& g, long tile, char* smem) {
   constexpr int NP = GlType<T>::PIECES, MB = BM / 64, NB = BN / 64;
   typedef typename GlType<T>::Raw Raw;
   typedef GlTile<BM, KS, KIND == GL_WEIGHTS> TA;
@@ -357,9 +398,6 @@ __global__ __launch_bounds__(256) void gl_tile_kernel(GlArgs<T> g) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r32 = lane & 31, hh = lane >> 5;
 
-  // Neighbouring tiles to the same XCD (workgroups go round the eight of them in turn), the columns of a tile of rows one after the other.
-  const long per = ((long)gridDim.x + 7) >> 3, tile = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  if ((blockIdx.x >> 3) >= per) return;
   int group;
   long r0, r1;
   const long rt = tile / g.tiles_j;
@@ -609,6 +647,23 @@ __global__ __launch_bounds__(256) void gl_tile_kernel(GlArgs<T> g) {
       for (int q = 0; q < 8; ++q)
         if (q < valid) to[q] = (T)v[q];
     }
+  }
+}
+
+// Neighbouring tiles to the same XCD (workgroups go round the eight of them in turn), the columns of a tile of rows one after the other.
+template <class T, GlKind KIND, int BM, int BN, int KS, bool NARROW>
+__global__ __launch_bounds__(256) void gl_tile_kernel(GlArgs<T> g) {
+  extern __shared__ __align__(16) char smem[];
+  const long per = gridDim.x >> 3, place = blockIdx.x >> 3;
+  if (KIND == GL_WEIGHTS && g.chunk >= g.rows.n) {
+    long tile, end;
+    gl_units(g.rows, g.tiles_j, blockIdx.x & 7, tile, end);
+    for (tile += place; tile < end; tile += per) {
+      gl_tile<T, KIND, BM, BN, KS, NARROW>(g, tile, smem);
+      __syncthreads();
+    }
+  } else {
+    gl_tile<T, KIND, BM, BN, KS, NARROW>(g, (blockIdx.x & 7) * per + place, smem);
   }
 }
 
