@@ -160,8 +160,9 @@ __device__ __forceinline__ void ou_lds_barrier() {
 // C = A B^T of one tile TILE x TILE: four waves, each a quarter (TILE / 2 squared) in 32 x 32 blocks; for tiles of 64 twice four, each
 // with half of a turn's contraction (the chain of dependent products of a turn is what a small tile waits for).  64 contraction indices a
 // turn, brought straight into one of STAGES LDS buffers, STAGES - 1 turns ahead: with one wave per SIMD nothing else hides the way to
-// memory.  A row of 128 bytes lies in LDS as eight pieces of 16 bytes, piece c at place c ^ (row & 7): eight lanes that read the same
-// piece of eight rows meet all banks.  The operands of a step of 16 are read from LDS while the products of the one before run.
+// memory.  A row of 128 bytes lies in LDS as eight pieces of 16 bytes, piece c at place c ^ (row / 2 & 7): the sixteen lanes whose
+// 16-byte reads go together (0-3, 12-15, 20-23, 24-27 and the others) then meet all 64 banks (with c ^ (row & 7) half of the LDS cycles were
+// conflicts).  The operands of a step of 16 are read from LDS while the products of the one before run.
 template <int P, int TILE>
 struct OuTile {
   static constexpr int STAGES = P * TILE >= 256 ? 2 : 4;
@@ -188,7 +189,7 @@ __global__ __launch_bounds__((OuTile<P, TILE>::THREADS)) void ou_product_kernel(
   const int wi = (wave >> 1 & 1) * HALF, wj = (wave & 1) * HALF, set = wave >> 2;
 
   // lane's place in a load of eight rows
-  const int lrow = lane >> 3, lpiece = (lane & 7) ^ lrow;
+  const int lrow = lane >> 3, lpiece = (lane & 7) ^ ((wave & 1) << 2 | lrow >> 1);
   const _Float16 *pa[ROUNDS], *pb[ROUNDS];
 #pragma unroll
   for (int r = 0; r < ROUNDS; ++r) {
@@ -228,7 +229,7 @@ __global__ __launch_bounds__((OuTile<P, TILE>::THREADS)) void ou_product_kernel(
     stage = stage + 1 == STAGES ? 0 : stage + 1;
     ou_h8 a[2][B][P], b[2][B][P];
     auto operands = [&](int s) {
-      const int place = (2 * (s + set * (4 / SETS)) + hh) ^ (r32 & 7);
+      const int place = (2 * (s + set * (4 / SETS)) + hh) ^ (r32 >> 1 & 7);
 #pragma unroll
       for (int x = 0; x < B; ++x)
 #pragma unroll
