@@ -51,20 +51,36 @@ __device__ __forceinline__ void ou_cut(float v, _Float16& hi, _Float16& lo) {
 }
 
 // ---- sums of squares (fp64: no overflow, no underflow), and the new momentum
-template <class T>
+// V values at a time (4 where every matrix begins and ends in aligned fours), sixteen a thread and round, all loaded before the first is used.
+constexpr int OU_ROUND = 4096;      // values of a workgroup and round
+template <class T, int V>
 __global__ __launch_bounds__(256) void ou_square_kernel(OuInput<T> in, const float* m_old, float* m_new, size_t size, double* part) {
   __shared__ double s[256];
+  constexpr int U = 16 / V;
   const size_t at = (size_t)blockIdx.y * size;
-  const size_t per = (size + gridDim.x - 1) / gridDim.x, b = blockIdx.x * per, e = min(b + per, size);
   double t = 0.0;
-  for (size_t i = b + threadIdx.x; i < e; i += 256) {
-    float v = (float)in.u[at + i];
-    if (m_old) {
-      const float mm = in.beta * m_old[at + i] + v;
-      m_new[at + i] = mm;
-      v = v + in.beta * mm;
+  for (size_t b = (size_t)blockIdx.x * OU_ROUND; b < size; b += (size_t)gridDim.x * OU_ROUND) {
+    float v[U][V], mm[U][V];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const size_t i = b + (size_t)(k * 256 + threadIdx.x) * V, from = at + (i < size ? i : size - V);
+      rt_load<T, V>(in.u + from, v[k]);
+      if (m_old) rt_load<float, V>(m_old + from, mm[k]);
     }
-    t += (double)v * (double)v;
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const size_t i = b + (size_t)(k * 256 + threadIdx.x) * V;
+      const bool there = i < size;
+#pragma unroll
+      for (int q = 0; q < V; ++q) {
+        if (m_old) {
+          mm[k][q] = in.beta * mm[k][q] + v[k][q];
+          v[k][q] = v[k][q] + in.beta * mm[k][q];
+        }
+        if (there) t += (double)v[k][q] * (double)v[k][q];
+      }
+      if (m_old && there) rt_store<float, V>(m_new + at + i, mm[k]);
+    }
   }
   s[threadIdx.x] = t;
   for (int h = 128; h; h >>= 1) {
@@ -88,15 +104,21 @@ __global__ __launch_bounds__(256) void ou_pieces_kernel(OuShape p, OuInput<T> in
                                                         _Float16* xt) {
   __shared__ float tile[64][65];    // [i][j] of x
   const size_t z = blockIdx.z;
-  const double inv = ou_inverse_norm(part + z * OU_PARTS, parts) * (double)OU_SX;
   const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64, t = threadIdx.x;
-  for (int k = 0; k < 16; ++k) {
+  float v[16];
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {                     // (never under a condition: all loads before the first is waited for)
     const int a = (t >> 6) + 4 * k, b = t & 63;       // b along the caller's rows
-    const int i = i0 + (p.tall ? b : a), j = j0 + (p.tall ? a : b);
-    const bool there = i < p.n && j < p.m;
-    const size_t at = z * p.rows * p.cols + (p.tall ? (size_t)j * p.cols + i : (size_t)i * p.cols + j);
-    const float v = there ? (float)((double)ou_value(in, at) * inv) : 0.0f;
-    if (p.tall) tile[b][a] = v; else tile[a][b] = v;
+    const int i = min(i0 + (p.tall ? b : a), p.n - 1), j = min(j0 + (p.tall ? a : b), p.m - 1);
+    v[k] = ou_value(in, z * p.rows * p.cols + (p.tall ? (size_t)j * p.cols + i : (size_t)i * p.cols + j));
+  }
+  const double inv = ou_inverse_norm(part + z * OU_PARTS, parts) * (double)OU_SX;
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const int a = (t >> 6) + 4 * k, b = t & 63;
+    const bool there = i0 + (p.tall ? b : a) < p.n && j0 + (p.tall ? a : b) < p.m;
+    const float x0 = there ? (float)((double)v[k] * inv) : 0.0f;
+    if (p.tall) tile[b][a] = x0; else tile[a][b] = x0;
   }
   __syncthreads();
   const size_t plane = (size_t)p.np * p.mp;
@@ -824,7 +846,7 @@ OsSpace os_space(const OuShape& p) {
   return s;
 }
 
-int ou_parts(size_t size) { return (int)(size > (size_t)OU_PARTS * 4096 ? OU_PARTS : (size + 4095) / 4096); }
+int ou_parts(size_t size) { return (int)(size > (size_t)OU_PARTS * OU_ROUND ? OU_PARTS : (size + OU_ROUND - 1) / OU_ROUND); }
 
 // Side of at most 32: one block of 32 x 32 holds g, otherwise four do (a step of 15 matrices 32 x 32 took OS_32 us with one and OS_64 us with four).
 template <class T, int NB>
@@ -903,7 +925,11 @@ int ou_run(egnn_ctx* ctx, const OuShape& p, const OuInput<T>& in, const float* m
   _Float16* q = (_Float16*)((char*)ws + s.g + (s.bytes - s.g) / 2);
   const size_t size = (size_t)p.rows * p.cols;
   const int parts = ou_parts(size);
-  hipLaunchKernelGGL((ou_square_kernel<T>), dim3(parts, p.batch), dim3(256), 0, st, in, m_old, m_new, size, part);
+  const uintptr_t all = (uintptr_t)in.u | (uintptr_t)m_old | (uintptr_t)m_new;
+  if (size % 4 == 0 && all % 16 == 0)
+    hipLaunchKernelGGL((ou_square_kernel<T, 4>), dim3(parts, p.batch), dim3(256), 0, st, in, m_old, m_new, size, part);
+  else
+    hipLaunchKernelGGL((ou_square_kernel<T, 1>), dim3(parts, p.batch), dim3(256), 0, st, in, m_old, m_new, size, part);
   hipLaunchKernelGGL((ou_pieces_kernel<T, P>), dim3(p.mp / 64, p.np / 64, p.batch), dim3(256), 0, st, p, in, part, parts, x, xt);
   EGNN_LAUNCH_CHECK(ctx, "orthogonalise");
   const OuOut<float> none{};
