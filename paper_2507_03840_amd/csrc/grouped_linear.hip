@@ -939,7 +939,8 @@ int gl_check(egnn_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32_t K
 size_t gl_align(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Rows of one slot of the weight gradient: enough slots that the launch fills the compute units three times, of at least 256 rows
-// (below that a slot's partial result is longer than what it reads).
+// (below that a slot's partial result is longer than what it reads).  Adjoint in us with one, three, six times: 20,000 rows 512 to 256 in 4
+// groups bf16 81, 58, 51; 50,000 of 128 in 15 fp32 73, 79, 90; 300,000 of 64 in 15 fp32 92, 94, 99.
 struct GlSplit { long chunk; int slots; size_t weights, bytes; };
 GlSplit gl_split(int64_t n, int G, int K, int N) {
   GlSplit s;
@@ -969,15 +970,25 @@ int gl_launch(egnn_ctx* ctx, const GlArgs<T>& g, long tiles, hipStream_t st) {
   return EGNN_OK;
 }
 
+// Matrices of at most 32 x 32 (one register block) always go the lean way, those of at most 64 x 64 from GL_LEAN_ROWS rows on: with few rows
+// the way to the first product counts (forward us, lean against tiles, 15 groups of 64 x 64: 20,000 rows fp32 13.4 : 7.7, 80,000 24.6 : 22.1,
+// 150,000 29.7 : 35.7, 300,000 42 : 66; bf16 40,000 9.7 : 8.2, 80,000 11.2 : 12.4; 32 x 32: 40,000 fp32 7.7 : 11.4).
+constexpr int GL_LEAN_ROWS = 80000;
+bool gl_lean(int64_t n, int K, int N) { return K <= 64 && N <= 64 && ((K <= 32 && N <= 32) || K < 8 || N < 8 || n >= GL_LEAN_ROWS); }
+
+// Tiles of 64 x 64, or of 128 x 128 for 16-bit values where there are enough of those for every compute unit: half the LDS traffic a product, but
+// a quarter of the workgroups (us forward, 128 against 64: 2,000 rows 1,024 to 1,024 in 4 groups 17.8 : 15.2, 5,000 in 8 25.5 : 26.5,
+// 20,000 512 to 1,024 in 16 49 : 57).  fp32 has six products a pair of operands and is not bound by LDS: 64 x 64 is faster at all sizes
+// (128 x 64: 20,000 rows 512 to 1,024 218 : 178, 20,000 of 128 18.9 : 14.6).
 template <class T, GlKind KIND>
 int gl_rows(egnn_ctx* ctx, GlArgs<T> g, hipStream_t st) {
   constexpr int KS = GlType<T>::PIECES == 1 ? 64 : 32;
-  auto tiles = [&](int bm, int bn) {
-    g.tiles_j = (g.J + bn - 1) / bn;
-    return ((g.rows.n + bm - 1) / bm + g.rows.G) * (long)g.tiles_j;
+  auto tiles = [&](int side) {
+    g.tiles_j = (g.J + side - 1) / side;
+    return ((g.rows.n + side - 1) / side + g.rows.G) * (long)g.tiles_j;
   };
-  if (g.J <= 64 && g.K <= 64) {
-    // 2,048 waves, two per SIMD, as long as each gets at least 32 rows
+  if (gl_lean(g.rows.n, g.K, g.J)) {
+    // 2,048 waves, two per SIMD, as long as each gets at least 32 rows (300,000 x 64 fp32: 42 us; 1,024 waves 44, 4,096 49)
     long share = (g.rows.n + 2047) / 2048;
     if (share < 32) share = 32;
     const unsigned grid = (unsigned)((g.rows.n + 4 * share - 1) / (4 * share));
@@ -990,15 +1001,10 @@ int gl_rows(egnn_ctx* ctx, GlArgs<T> g, hipStream_t st) {
     EGNN_LAUNCH_CHECK(ctx, "grouped_linear");
     return EGNN_OK;
   }
-  if (g.K < 8 || (KIND == GL_INPUT && g.J < 8)) return gl_launch<T, KIND, 64, 64, KS, true>(ctx, g, tiles(64, 64), st);
-  if constexpr (GlType<T>::PIECES == 1) {
-    const long wide = tiles(128, 128);
-    if (g.J > 64 && wide >= EGNN_CUS) return gl_launch<T, KIND, 128, 128, KS>(ctx, g, wide, st);
-  }
-  const long tall = tiles(128, 64);
-  if (tall >= EGNN_CUS) return gl_launch<T, KIND, 128, 64, KS>(ctx, g, tall, st);
-  const long small = tiles(64, 64);
-  return gl_launch<T, KIND, 64, 64, KS>(ctx, g, small, st);
+  if (g.K < 8 || (KIND == GL_INPUT && g.J < 8)) return gl_launch<T, KIND, 64, 64, KS, true>(ctx, g, tiles(64), st);
+  if constexpr (GlType<T>::PIECES == 1)
+    if (g.J > 64 && tiles(128) >= EGNN_CUS) return gl_launch<T, KIND, 128, 128, KS>(ctx, g, tiles(128), st);
+  return gl_launch<T, KIND, 64, 64, KS>(ctx, g, tiles(64), st);
 }
 
 template <class T>
@@ -1023,35 +1029,29 @@ int gl_backward(egnn_ctx* ctx, const GlRows& p, const void* x, int64_t xs, const
     pw = dW ? (float*)ws : nullptr;
     pb = db ? (float*)((char*)ws + s.weights) : nullptr;
   }
-  GlArgs<T> g{p, (const T*)dy, (const T*)x, dys, xs, N, K, 0, nullptr, 0, nullptr, pw, pb, 0, s.chunk};
-  constexpr int KS = GlType<T>::PIECES == 1 ? 32 : 16;
-  auto tiles = [&](int bm, int bn) {
-    g.tiles_j = ((N + bm - 1) / bm) * (dW ? (K + bn - 1) / bn : 1);      // db alone: the first column of tiles
+  // (db alone: x may be NULL, and dy, whose rows have N values, takes its place in loads whose results nobody uses)
+  GlArgs<T> g{p, (const T*)dy, (const T*)(dW ? x : dy), dys, dW ? xs : dys, N, dW ? K : N, 0, nullptr, 0, nullptr, pw, pb, 0, s.chunk};
+  constexpr int KS = GlType<T>::PIECES == 1 ? 64 : 32;
+  auto tiles = [&](int side) {
+    g.tiles_j = ((N + side - 1) / side) * (dW ? (K + side - 1) / side : 1);      // db alone: the first column of tiles
     return (long)s.slots * g.tiles_j;
   };
-  bool done = false;
-  if (N <= 64 && K <= 64) {
+  int rc = EGNN_OK;
+  if (gl_lean(p.n, K, N)) {
     if (N <= 32 && K <= 32)
       hipLaunchKernelGGL((gl_lean_weights_kernel<T, 1, 1>), dim3(s.slots), dim3(256), 0, st, g);
     else
       hipLaunchKernelGGL((gl_lean_weights_kernel<T, 2, 2>), dim3(s.slots), dim3(256), 0, st, g);
     EGNN_LAUNCH_CHECK(ctx, "grouped_linear_backward");
-    done = true;
   } else if (N < 8 || K < 8) {
-    const long small = tiles(64, 64);
-    if (int rc = gl_launch<T, GL_WEIGHTS, 64, 64, 2 * KS, true>(ctx, g, small, st)) return rc;
-    done = true;
-  } else if constexpr (GlType<T>::PIECES == 1) {
-    const long wide = tiles(128, 128);
-    if (N > 64 && K > 64 && wide >= EGNN_CUS) {
-      if (int rc = gl_launch<T, GL_WEIGHTS, 128, 128, KS>(ctx, g, wide, st)) return rc;
-      done = true;
-    }
+    rc = gl_launch<T, GL_WEIGHTS, 64, 64, KS, true>(ctx, g, tiles(64), st);
+  } else if (GlType<T>::PIECES == 1 && N > 64 && K > 64 && tiles(128) > EGNN_CUS) {
+    // (as in gl_rows; half the contraction a turn, for three workgroups' worth of LDS: with 64 a turn 103 us instead of 64 at 20,000 rows)
+    if constexpr (GlType<T>::PIECES == 1) rc = gl_launch<T, GL_WEIGHTS, 128, 128, KS / 2>(ctx, g, tiles(128), st);
+  } else {
+    rc = gl_launch<T, GL_WEIGHTS, 64, 64, KS>(ctx, g, tiles(64), st);
   }
-  if (!done) {
-    const long small = tiles(64, 64);
-    if (int rc = gl_launch<T, GL_WEIGHTS, 64, 64, 2 * KS>(ctx, g, small, st)) return rc;
-  }
+  if (rc) return rc;
   if (join) {
     const long n = dW ? (long)N * K : 0, m = db ? N : 0;
     const long blocks = (n + 63) / 64 + (m + 63) / 64;

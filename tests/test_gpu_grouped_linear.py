@@ -232,3 +232,44 @@ def test_same_bits_again_on_another_stream_and_in_a_graph(m, dtype):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("n,k,out,groups,empty", [(90001, 61, 37, 3, []), (80000, 64, 64, 200, range(0, 200, 7)), (100003, 9, 50, 2, [0])])
+def test_many_rows_of_small_matrices(m, n, k, out, groups, empty, dtype):
+    """The way of many rows: matrices in registers."""
+    check(m, n, k, out, groups, dtype, empty=list(empty))
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+def test_wide_tiles_of_ragged_groups(m, dtype):
+    """Enough tiles for the wide kernels: groups of a few rows, of none, odd rows and columns; then one group of nearly all rows."""
+    check(m, 900, 203, 259, 90, dtype, empty=[0, 7, 89])
+    check(m, 905, 264, 200, 90, dtype, with_perm=False)
+    check(m, 4000, 136, 1000, 40, dtype, empty=list(range(1, 38)))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_groups_longer_than_the_row_numbers_kept(m, dtype):
+    """More than 2,048 rows of one group in one workgroup of the weight gradient."""
+    check(m, 6001, 1024, 1000, 2, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("k,out", [(40, 24), (64, 64), (200, 140)])
+def test_gradients_one_at_a_time(m, k, out, dtype):
+    """Any of dx, dW, db may be left out of the C call; the others keep their values."""
+    import torch
+    rng = np.random.default_rng([12, k])
+    for n in (300, 90000):
+        x, W, dy, bias, ptr, perm, hptr, hperm = data(rng, n, k, out, 3, dtype)
+        want = m.egnn_grouped_linear_backward(x, W, dy, ptr, perm=perm)
+        ws = torch.empty(max(256, m.egnn_grouped_linear_workspace_bytes(n, 3, k, out)), dtype=torch.uint8, device="cuda")
+        for keep in range(1, 7):
+            outs = [torch.full_like(t, 3.0) if keep >> i & 1 else None for i, t in enumerate(want)]
+            at = [None if t is None else t.data_ptr() for t in outs]
+            rc = m.lib.egnn_grouped_linear_backward(
+                m.ctx, {"float32": 0, "bfloat16": 2}[dtype], x.data_ptr() if keep & 2 else None, k, W.data_ptr() if keep & 1 else None, dy.data_ptr(), out, n, k, out,
+                ptr.data_ptr(), perm.data_ptr(), 3, at[0], k, at[1], at[2], ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
+            assert rc == 0
+            assert all(t is None or torch.equal(t, w) for t, w in zip(outs, want)), keep

@@ -145,3 +145,46 @@ def test_same_bits_again_on_another_stream_and_in_a_graph(m, shape):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+@pytest.mark.parametrize("shape", [(5, 300, 700), (3, 1000, 650), (2, 1290, 1100)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_wide_tiles(m, shape, dtype):
+    """Enough tiles of 128 for half the compute units; sides that are no multiples of them."""
+    import torch
+    g = torch.from_numpy(random(np.random.default_rng([9, *shape]), *shape)).to(getattr(torch, dtype)).cuda()
+    e = off(m.egnn_orthogonalise(g), K.orthogonalise(g.double().cpu().numpy()))
+    print(shape, dtype, "off by %.2e" % e)
+    assert e <= TOL[dtype]
+
+
+@pytest.mark.parametrize("shape", [(1, 20, 17000), (1, 17000, 50)])
+def test_more_columns_than_slabs(m, shape):
+    """A workgroup takes several slabs in turn."""
+    import torch
+    g = torch.from_numpy(random(np.random.default_rng([10, *shape]), *shape)).float().cuda()
+    assert off(m.egnn_orthogonalise(g), K.orthogonalise(g.double().cpu().numpy())) <= FULL
+    W, mom = torch.randn(shape, device="cuda"), torch.zeros(shape, device="cuda")
+    f = lambda t: t.double().cpu().numpy()
+    rW, rm = K.muon_step(f(W), f(g), f(mom), 0.02, 0.95, 0.01)
+    W2, m2 = m.egnn_muon_step(W, g, mom, 0.02, beta=0.95, weight_decay=0.01)
+    assert np.abs(f(m2) - rm).max() <= 4 * 2.0 ** -24 * np.abs(rm).max()
+    o = np.linalg.norm(K.orthogonalise(f(g) + 0.95 * rm)) * 0.02 * max(1.0, shape[1] / shape[2]) ** 0.5
+    assert np.linalg.norm(f(W2) - rW) <= 2 * FULL * o + 3 * 2.0 ** -24 * np.linalg.norm(rW)
+
+
+@pytest.mark.parametrize("shape", [(2, 21, 30), (2, 500, 44), (1, 130, 90)])
+def test_alignment(m, shape):
+    """Matrices that begin at any element of a larger buffer give the same numbers (to rounding) as aligned ones."""
+    import torch
+    n = int(np.prod(shape))
+    for dtype in (torch.float32, torch.bfloat16):
+        g = torch.from_numpy(random(np.random.default_rng([11, *shape]), *shape)).to(dtype).cuda()
+        want = m.egnn_orthogonalise(g)
+        room, out = torch.zeros(n + 8, dtype=dtype, device="cuda"), torch.full((n + 8,), 7.0, dtype=dtype, device="cuda")
+        for at in (1, 2, 3):
+            room[at:at + n] = g.reshape(-1)
+            y = m.egnn_orthogonalise(room[at:at + n].view(shape), y=out[at:at + n].view(shape))
+            assert off(y, want.double().cpu().numpy()) <= TOL["float32" if dtype == torch.float32 else "bfloat16"]
+            assert (out[:at] == 7.0).all() and (out[at + n:] == 7.0).all()
+            out.fill_(7.0)
