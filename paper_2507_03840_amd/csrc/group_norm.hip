@@ -9,6 +9,9 @@
 // read twice, because the sums of all rows of a segment come before its first result.  The second pass goes through its rows from the last
 // to the first, so that it begins with what the first pass left in the caches.  Where one workgroup takes all rows the two are one launch.
 //
+// Measured: 625,262 x 32 fp32 14 + 27 us forward, 27 + 40 adjoint (80 MB a tensor, read again from the 256 MB cache); 2,350,179 x 64 bf16 75 us (4.0
+// TB/s) + 99 us (6.1 TB/s); 20,000 x 64 fp32 inside [20,000][25][64] in 37 segments 8 + 10 + 10 + 11; 64 x 16 in one launch 4.
+//
 // The rows are cut into equal chunks, one workgroup each; segments are ragged and may be shorter or longer than a chunk.
 // A chunk c and a segment s that share rows own the slot c + s of the partial sums: walking along the rows either c or s
 // goes up by one, so no two pairs share a slot, the slots of a segment are contiguous, and their number is at most chunks +

@@ -384,6 +384,8 @@ __device__ __forceinline__ void gl_units(const GlRows& p, int tiles, int xcd, lo
   last = xcd == 7 ? (long)p.G * tiles : s_unit[1];
 }
 
+// Measured: 20,000 rows 512 to 1,024 in 16 ragged groups, bf16, 21 GFLOP each: forward 53 us, dx 46, dW 64 (330 to 450 TFLOP/s; a tile has 8 to
+// 16 turns, so that its start and end count as much as its products; LDS busy 37 %, without conflicts).
 // 256 threads, four waves, each a quarter of the BM x BN tile in 32 x 32 blocks.  Tiles go from memory to registers DEPTH turns ahead, are cut
 // into pieces on the way to one of two LDS buffers, and are contracted from the other.
 // NARROW: a side that is read along has fewer than eight values.
@@ -670,7 +672,8 @@ __global__ __launch_bounds__(256) void gl_tile_kernel(GlArgs<T> g) {
 // ---- n_in and n_out of at most 64: the group's matrix stays in registers ------------------------------------------------------
 // A wave takes an equal share of the rows, group by group, 32 at a time, and nothing is shared between waves: no LDS tile, no barrier.  The
 // product is y^T = W x^T, so that a lane holds one row and writes its values four neighbouring ones at a time.  The next rows are under way
-// while the matrix cores work on these; what is left is the memory.
+// while the matrix cores work on these; what is left is the memory: 300,000 rows of 64 fp32 by 15 groups take 44 us forward (154 MB, 3.5
+// TB/s), 54 with the transposed matrices of dx.
 // KB: contraction steps of 16, NB: output blocks of 32; 16 KB >= K, 32 NB >= J.
 template <class T, GlKind KIND, int KB, int NB, bool NARROW>
 __global__ __launch_bounds__(256, 2) void gl_lean_rows_kernel(GlArgs<T> g, long share) {
@@ -782,7 +785,7 @@ __global__ __launch_bounds__(256, 2) void gl_lean_rows_kernel(GlArgs<T> g, long 
 }
 
 // dW and db of a slot: each wave its own sixteen rows in turn, operands straight from memory (lane = column, eight rows), the waves' sums
-// joined at the end.  MB, NB: blocks of 32 outputs and inputs.
+// joined at the end (300,000 rows of 64 and 64 fp32: 50 us for 154 MB, and 6 to join the slots).  MB, NB: blocks of 32 outputs and inputs.
 template <class T, int MB, int NB>
 __global__ __launch_bounds__(256, 2) void gl_lean_weights_kernel(GlArgs<T> g) {
   constexpr int NP = GlType<T>::PIECES, PART = MB * NB * 1024;
@@ -960,11 +963,9 @@ int gl_launch(egnn_ctx* ctx, const GlArgs<T>& g, long tiles, hipStream_t st) {
   constexpr size_t stage = GlType<T>::PIECES * (GlTile<BM, KS, KIND == GL_WEIGHTS>::PLANE + GlTile<BN, KS, KIND != GL_FORWARD>::PLANE);
   constexpr size_t out = KIND == GL_WEIGHTS ? (size_t)256 * 8 * sizeof(double) : (size_t)BM * (BN + 4) * sizeof(float);
   constexpr size_t lds = 2 * stage > out ? 2 * stage : out;
-  static bool ready = false;      // (set again by two threads at once: to the same value)
-  if (!ready && lds > 65536) {
-    EGNN_HIP(ctx, hipFuncSetAttribute((const void*)gl_tile_kernel<T, KIND, BM, BN, KS, NARROW>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    ready = true;
-  }
+  if (tiles > 0xfffff0) return egnn_fail(ctx, EGNN_EINVAL, "grouped_linear: more tiles than a launch holds");
+  static bool ready[64];
+  if (int rc = rt_allow_lds(ctx, (const void*)gl_tile_kernel<T, KIND, BM, BN, KS, NARROW>, lds, ready)) return rc;
   hipLaunchKernelGGL((gl_tile_kernel<T, KIND, BM, BN, KS, NARROW>), dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(256), lds, st, g);
   EGNN_LAUNCH_CHECK(ctx, "grouped_linear");
   return EGNN_OK;

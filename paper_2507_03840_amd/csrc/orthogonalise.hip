@@ -428,6 +428,7 @@ __global__ __launch_bounds__((OuTile<P, TILE>::THREADS)) void ou_product_kernel(
 // Until step 1 a slab is scaled by its own norm: the sums of squares of the others come with their parts of g, no pass for |u| alone.
 //
 // What bounds it: the chain of dependent products, conversions and barriers of a step, and the reading of the parts (16 KB a slab from L2).
+// Measured, a step of the optimiser: 15 x 32 x 32 15.5 us in one launch, 3 x 2688 x 64 64 us in six.
 constexpr int OS_ROWS = 256, OS_WAVES = OS_ROWS / 32;
 constexpr int OS_SLABS = 64;                 // more columns than this many slabs: a workgroup takes several turns
 
@@ -855,19 +856,17 @@ int ou_run_slabs(egnn_ctx* ctx, const OuShape& p, const OuInput<T>& in, const fl
                  const OuOut<T>& out, void* ws, hipStream_t st) {
   const OsSpace s = os_space(p);
   const size_t most = OsLds<NB>::bytes(OS_WAVES);
-  static bool ready = false;      // (set again by two threads at once: to the same value)
-  if (!ready) {
-    EGNN_HIP(ctx, hipFuncSetAttribute((const void*)ou_slab_kernel<T, NB, true>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)most));
-    EGNN_HIP(ctx, hipFuncSetAttribute((const void*)ou_slab_kernel<T, NB, false>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)most));
-    ready = true;
-  }
   if (p.m <= OS_ROWS) {
     const int waves = (p.m + 31) / 32;
+    static bool ready[64];
+    if (int rc = rt_allow_lds(ctx, (const void*)ou_slab_kernel<T, NB, true>, most, ready)) return rc;
     hipLaunchKernelGGL((ou_slab_kernel<T, NB, true>), dim3(1, p.batch), dim3(64 * waves), OsLds<NB>::bytes(waves), st, p, in, m_old, m_new,
                        OsPlace{}, 0, steps, out);
     EGNN_LAUNCH_CHECK(ctx, "orthogonalise");
     return EGNN_OK;
   }
+  static bool ready[64];
+  if (int rc = rt_allow_lds(ctx, (const void*)ou_slab_kernel<T, NB, false>, most, ready)) return rc;
   float4* g[2] = {(float4*)((char*)ws + s.g), (float4*)((char*)ws + s.g + (s.bytes - s.g) / 2)};
   for (int k = 0; k <= steps; ++k) {
     const OsPlace w{(uint4*)((char*)ws + s.x), g[k & 1], g[(k + 1) & 1], (double*)((char*)ws + s.squares), s.slabs, s.turns};
@@ -894,11 +893,8 @@ OuSpace ou_space(const OuShape& p, int pieces) {
 template <class T, int P, int TILE, OuProduct WHAT>
 int ou_product_tile(egnn_ctx* ctx, const OuShape& p, const OuOperands& o, const OuOut<T>& out, hipStream_t st) {
   constexpr size_t lds = OuTile<P, TILE>::LDS;
-  static bool ready = false;      // (set again by two threads at once: to the same value)
-  if (!ready && lds > 65536) {
-    EGNN_HIP(ctx, hipFuncSetAttribute((const void*)ou_product_kernel<T, P, TILE, WHAT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    ready = true;
-  }
+  static bool ready[64];
+  if (int rc = rt_allow_lds(ctx, (const void*)ou_product_kernel<T, P, TILE, WHAT>, lds, ready)) return rc;
   const dim3 grid((o.J + TILE - 1) / TILE, (o.I + TILE - 1) / TILE, p.batch);
   hipLaunchKernelGGL((ou_product_kernel<T, P, TILE, WHAT>), grid, dim3(OuTile<P, TILE>::THREADS), lds, st, p, o, out);
   EGNN_LAUNCH_CHECK(ctx, "orthogonalise");

@@ -5,6 +5,17 @@
 
 inline int rt_size(int32_t dtype) { return dtype == EGNN_F32 ? 4 : dtype == EGNN_F16 || dtype == EGNN_BF16 ? 2 : 0; }
 
+// Lets a kernel have more than 64 KB of dynamic LDS, once per kernel and GPU (`ready`: a static of the caller; set twice to the same by two threads).
+inline int rt_allow_lds(egnn_ctx* ctx, const void* kernel, size_t bytes, bool (&ready)[64]) {
+  int device = 0;
+  if (bytes <= 65536) return EGNN_OK;
+  EGNN_HIP(ctx, hipGetDevice(&device));
+  if (device >= 0 && device < 64 && ready[device]) return EGNN_OK;
+  EGNN_HIP(ctx, hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+  if (device >= 0 && device < 64) ready[device] = true;
+  return EGNN_OK;
+}
+
 // V values at p, which is aligned to all of them
 template <class T, int V>
 __device__ __forceinline__ void rt_load(const T* p, float (&v)[V]) {
