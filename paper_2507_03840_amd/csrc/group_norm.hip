@@ -22,9 +22,10 @@ namespace {
 
 constexpr int GN_CHUNKS = 512;        // two workgroups per compute unit; the second pass reads all partial sums of a segment (625,262 x 32 fp32
                                       // forward 40 us, 2,350,179 x 64 bf16 177; 256 chunks 41 and 187, 1,024 46 and 184)
-constexpr int GN_CHUNK_BYTES = 16384; // a chunk holds at least this much of x: below it the launch is longer than the reading
-constexpr int GN_ALONE_BYTES = 131072; // up to this much of x one workgroup takes all rows (1,000 x 32 fp32 9.8 us alone, 12.1 in two launches;
-                                       // 2,000 x 32 14.8 and 12.2)
+constexpr int GN_CHUNK_BYTES = 16384; // a chunk holds at least this much of x, unless its segments are short: below it the launch is longer than
+                                      // the reading
+constexpr int GN_ALONE_BYTES = 131072; // up to this much of x, of two segments at most, one workgroup takes all rows (1,000 x 32 fp32
+                                       // 9.8 us alone, 12.1 in two launches; 2,000 x 32 14.8 and 12.2)
 constexpr int GN_THREADS = 512;       // 1,024 where a row has more than 512 pieces
 constexpr int GN_ROWS = 4;            // rows of a thread under way at once
 
@@ -436,10 +437,15 @@ size_t gn_align(size_t n) { return (n + 255) & ~(size_t)255; }
 GnShape gn_shape(int64_t n, int32_t C, int32_t G, int32_t S, const int32_t* ptr, int element) {
   GnShape p;
   p.n = n; p.C = C; p.G = G; p.S = S; p.ptr = ptr;
-  const long least = (GN_CHUNK_BYTES + (long)C * element - 1) / ((long)C * element);
+  long least = (GN_CHUNK_BYTES + (long)C * element - 1) / ((long)C * element);
+  // a workgroup takes its segments one after the other: about two of them each (forward of 1,000 x 32 fp32 in 100 segments 14 us, in one
+  // workgroup 256; 5,000 x 64 in 300 19 us, in chunks of 16 KB 28)
+  if (S > 1 && 2 * n / S < least) least = 2 * n / S > 0 ? 2 * n / S : 1;
   p.rows = (n + GN_CHUNKS - 1) / GN_CHUNKS;
   if (p.rows < least) p.rows = least;
-  if ((double)n * C * element <= GN_ALONE_BYTES) p.rows = n > 0 ? n : 1;
+  // groups of fewer than four channels keep a sum per value instead of one per thread (325 x 200 fp16 in 200 groups 12 us, alone 18)
+  const double alone = C / G < 4 ? GN_ALONE_BYTES / 4 : GN_ALONE_BYTES;
+  if (S <= 2 && (double)n * C * element <= alone) p.rows = n > 0 ? n : 1;
   p.chunks = (int)((n + p.rows - 1) / p.rows);
   return p;
 }

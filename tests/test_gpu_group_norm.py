@@ -83,6 +83,14 @@ def test_segments_that_span_many_chunks(m):
     check(m, 300001, 64, 8, "bfloat16", None, seed=1)
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("ptr", [[0] * 20 + [3] * 20 + [5], [0, 4] + [7] * 60 + [900], list(range(0, 1201, 60)), list(range(0, 41))])
+def test_many_short_segments(m, ptr, dtype):
+    """More segments than rows, one long segment behind many empty ones, a row to a segment."""
+    check(m, ptr[-1], 32, 4, dtype, ptr)
+    check(m, ptr[-1], 20, 20, dtype, ptr, planes=2)
+
+
 @pytest.mark.parametrize("dtype", ["float32", "float16"])
 def test_a_plane_of_a_node_tensor(m, dtype):
     """x, dy and every output inside [n][25][64]; the rest of the tensors is left alone."""
