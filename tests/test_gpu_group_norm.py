@@ -110,6 +110,26 @@ def test_a_plane_of_a_node_tensor(m, dtype):
     assert (grad[:, :3] == 5.0).all() and (grad[:, 4:] == 5.0).all() and torch.isfinite(grad).all()
 
 
+def test_offsets_past_32_bits(m):
+    """Rows 100,000 values apart: the last lie behind 2^32 values (8 GB)."""
+    import torch
+    rng = np.random.default_rng(5)
+    n, c = 50000, 64
+    x, _ = tensors(rng, n, c, "float16")
+    dy, _ = tensors(rng, n, c, "float16", 1, 0.0, 1.0)
+    whole = torch.empty((n, 100000), dtype=torch.float16, device="cuda")
+    X, D, Y, G = (whole[:, 1000 * k:1000 * k + c] for k in range(4))
+    X.copy_(x), D.copy_(dy)
+    one, zero = torch.ones(c, device="cuda"), torch.zeros(c, device="cuda")
+    y, mean, rstd = m.egnn_group_norm(x, 8, one, zero)
+    dx, dg, db = m.egnn_group_norm_backward(x, dy, mean, rstd, 8, one, zero)
+    _, mean2, rstd2 = m.egnn_group_norm(X, 8, one, zero, y=Y)
+    _, dg2, db2 = m.egnn_group_norm_backward(X, D, mean, rstd, 8, one, zero, dx=G)
+    assert torch.equal(X, x) and torch.equal(D, dy)
+    assert torch.equal(Y, y) and torch.equal(mean2, mean) and torch.equal(rstd2, rstd)
+    assert torch.equal(G, dx) and torch.equal(dg2, dg) and torch.equal(db2, db)
+
+
 def test_in_place(m):
     import torch
     rng = np.random.default_rng(4)

@@ -273,3 +273,21 @@ def test_gradients_one_at_a_time(m, k, out, dtype):
                 ptr.data_ptr(), perm.data_ptr(), 3, at[0], k, at[1], at[2], ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
             assert rc == 0
             assert all(t is None or torch.equal(t, w) for t, w in zip(outs, want)), keep
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16"])
+@pytest.mark.parametrize("k,out", [(24, 40), (128, 136)])
+def test_offsets_past_32_bits(m, k, out, dtype):
+    """Rows 100,000 values apart: the last lie behind 2^32 values."""
+    import torch
+    n = 50000
+    x, W, dy, bias, ptr, perm, _, _ = data(np.random.default_rng([6, k]), n, k, out, 3, dtype)
+    whole = torch.empty((n, 100000), dtype=x.dtype, device="cuda")
+    X, G, D, Y = (whole[:, 1000 * i:1000 * i + c] for i, c in enumerate((k, k, out, out)))
+    X.copy_(x), D.copy_(dy)
+    y = m.egnn_grouped_linear(x, W, ptr, perm=perm, bias=bias)
+    dx, dW, db = m.egnn_grouped_linear_backward(x, W, dy, ptr, perm=perm)
+    m.egnn_grouped_linear(X, W, ptr, perm=perm, bias=bias, y=Y)
+    _, dW2, db2 = m.egnn_grouped_linear_backward(X, W, D, ptr, perm=perm, dx=G)
+    assert torch.equal(X, x) and torch.equal(D, dy)
+    assert torch.equal(Y, y) and torch.equal(G, dx) and torch.equal(dW2, dW) and torch.equal(db2, db)
