@@ -9,8 +9,8 @@
 // rounded to 11 bits, and hi hi + hi lo + lo hi (the dropped lo lo is 2^-24 of the product).  |x_0|_F <= 1 and the steps keep
 // the singular values below 1.2025, so every entry of x, g and p is bounded whatever the input, and one fixed power of two as
 // scale s leaves nothing to overflow and nothing above 2^-39 to underflow.
-// Results in bfloat16 of wide updates (both sides at least OU_ONE_PIECE) need no lo in the products: see ou_pieces().  The largest term
-// of a step, a x, then stays out of them: x^T keeps both pieces, and p is b g + c g^2 alone.
+// Every type of result comes from both pieces: with hi alone bfloat16 results of wide updates were 4e-4 to 6e-4 off beside their last rounding
+// (1.7e-3).
 #include "row_types.h"
 #include "stream_gemm.h"
 #include <math.h>
@@ -23,7 +23,6 @@ constexpr double OU_EPS = 1e-7;
 // entries of x are at most 1.2025, of g 1.446, of p 3.4445 (its eigenvalues lie between 0.6 and a): times these at most 56,500
 constexpr float OU_SX = 32768.0f, OU_SG = 32768.0f, OU_SP = 16384.0f;
 constexpr int OU_PARTS = 512;       // partial sums of squares per matrix, at most
-constexpr int OU_ONE_PIECE = 256;
 
 typedef _Float16 ou_h8 __attribute__((ext_vector_type(8)));
 typedef float ou_f16v __attribute__((ext_vector_type(16)));
@@ -98,8 +97,8 @@ __device__ __forceinline__ double ou_inverse_norm(const double* part, int parts)
   return 1.0 / (sqrt(t) + OU_EPS);
 }
 
-// ---- x_0 in pieces, in both layouts: 64 x 64 tiles.  x [P pieces][np][mp], xt [2 pieces][mp][np] per matrix
-template <class T, int P>
+// ---- x_0 in pieces, in both layouts: 64 x 64 tiles.  x [hi, lo][np][mp], xt [hi, lo][mp][np] per matrix
+template <class T>
 __global__ __launch_bounds__(256) void ou_pieces_kernel(OuShape p, OuInput<T> in, const double* part, int parts, _Float16* x,
                                                         _Float16* xt) {
   __shared__ float tile[64][65];    // [i][j] of x
@@ -133,11 +132,11 @@ __global__ __launch_bounds__(256) void ou_pieces_kernel(OuShape p, OuInput<T> in
       ou_cut(tile[c + q][r], h, l);
       thi[q] = h; tlo[q] = l;
     }
-    _Float16* to = x + z * P * plane + (size_t)(i0 + r) * p.mp + j0 + c;
+    _Float16* to = x + z * 2 * plane + (size_t)(i0 + r) * p.mp + j0 + c;
     _Float16* tt = xt + z * 2 * plane + (size_t)(j0 + r) * p.np + i0 + c;
     *(ou_h8*)to = hi;
     *(ou_h8*)tt = thi;
-    if (P == 2) *(ou_h8*)(to + plane) = lo;
+    *(ou_h8*)(to + plane) = lo;
     *(ou_h8*)(tt + plane) = tlo;
   }
 }
@@ -155,8 +154,8 @@ struct OuOut {     // y = q, or keep W - scale q
 };
 
 struct OuOperands {
-  const _Float16 *A, *B;   // per matrix [P pieces][I][K], [P pieces][J][K]; x^T always has two pieces
-  _Float16 *C, *Ct;        // results in pieces: C [..][J][I] (the transpose; g and p are symmetric), Ct [P pieces][I][J]
+  const _Float16 *A, *B;   // per matrix [hi, lo][I][K], [hi, lo][J][K]
+  _Float16 *C, *Ct;        // results in pieces: C [hi, lo][J][I] (the transpose; g and p are symmetric), Ct [hi, lo][I][J]
   int I, J, K;             // multiples of 64
 };
 
@@ -185,29 +184,27 @@ __device__ __forceinline__ void ou_lds_barrier() {
 // memory.  A row of 128 bytes lies in LDS as eight pieces of 16 bytes, piece c at place c ^ (row / 2 & 7): the sixteen lanes whose
 // 16-byte reads go together (0-3, 12-15, 20-23, 24-27 and the others) then meet all 64 banks (with c ^ (row & 7) half of the LDS cycles were
 // conflicts).  The operands of a step of 16 are read from LDS while the products of the one before run.
-template <int P, int TILE>
+template <int TILE>
 struct OuTile {
-  static constexpr int STAGES = P * TILE >= 256 ? 2 : 4;
+  static constexpr int STAGES = TILE == 128 ? 2 : 4;
   static constexpr int SETS = TILE == 64 ? 2 : 1, THREADS = 256 * SETS;   // sets of four waves
-  static constexpr int PLANE = TILE * 8, STAGE = 2 * P * PLANE;          // uint4
-  static constexpr int LOADS = 2 * P * TILE / 32 / SETS;                  // of a wave per turn
+  static constexpr int PLANE = TILE * 8, STAGE = 4 * PLANE;              // uint4
+  static constexpr int LOADS = 4 * TILE / 32 / SETS;                      // of a wave per turn
   static constexpr size_t LDS = (size_t)STAGES * STAGE * 16;
 };
 
-template <class T, int P, int TILE, OuProduct WHAT>
-__global__ __launch_bounds__((OuTile<P, TILE>::THREADS)) void ou_product_kernel(OuShape p, OuOperands o, OuOut<T> out) {
-  extern __shared__ uint4 smem[];                     // [STAGES][2 operands][P][TILE][8]
-  constexpr bool STEP = WHAT == OU_UPDATE || WHAT == OU_LAST;   // p x
-  constexpr int PB = STEP ? 2 : P;
-  typedef OuTile<P, TILE> Tile;
+template <class T, int TILE, OuProduct WHAT>
+__global__ __launch_bounds__((OuTile<TILE>::THREADS)) void ou_product_kernel(OuShape p, OuOperands o, OuOut<T> out) {
+  extern __shared__ uint4 smem[];                     // [STAGES][2 operands][hi, lo][TILE][8]
+  typedef OuTile<TILE> Tile;
   constexpr int HALF = TILE / 2, B = HALF / 32, PLANE = Tile::PLANE, STAGE = Tile::STAGE, STAGES = Tile::STAGES;
   constexpr int SETS = Tile::SETS, THREADS = Tile::THREADS, ROUNDS = TILE / 32 / SETS;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const size_t z = blockIdx.z;
   const int i0 = blockIdx.y * TILE, j0 = blockIdx.x * TILE;
   const size_t plane_a = (size_t)o.I * o.K, plane_b = (size_t)o.J * o.K;
-  const _Float16* A = o.A + z * P * plane_a;
-  const _Float16* Bm = o.B + z * PB * plane_b;
+  const _Float16* A = o.A + z * 2 * plane_a;
+  const _Float16* Bm = o.B + z * 2 * plane_b;
   const int wi = (wave >> 1 & 1) * HALF, wj = (wave & 1) * HALF, set = wave >> 2;
 
   // lane's place in a load of eight rows
@@ -222,11 +219,11 @@ __global__ __launch_bounds__((OuTile<P, TILE>::THREADS)) void ou_product_kernel(
   auto fetch = [&](int turn, int stage) {
     uint4* to = smem + stage * STAGE + wave * 64;
 #pragma unroll
-    for (int q = 0; q < P; ++q)
+    for (int q = 0; q < 2; ++q)
 #pragma unroll
       for (int r = 0; r < ROUNDS; ++r) {
         __builtin_amdgcn_global_load_lds((ou_gp)(pa[r] + q * plane_a + turn * 64), (ou_lp)(to + q * PLANE + r * 256 * SETS), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((ou_gp)(pb[r] + q * plane_b + turn * 64), (ou_lp)(to + (P + q) * PLANE + r * 256 * SETS), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((ou_gp)(pb[r] + q * plane_b + turn * 64), (ou_lp)(to + (2 + q) * PLANE + r * 256 * SETS), 16, 0, 0);
       }
   };
 
@@ -247,15 +244,15 @@ __global__ __launch_bounds__((OuTile<P, TILE>::THREADS)) void ou_product_kernel(
     // (past the end the last turn is fetched again: the number of loads under way is the same in every turn)
     fetch(min(k + STAGES - 1, turns - 1), stage ? stage - 1 : STAGES - 1);
     const uint4* sa = smem + stage * STAGE + (wi + r32) * 8;
-    const uint4* sb = smem + stage * STAGE + P * PLANE + (wj + r32) * 8;
+    const uint4* sb = smem + stage * STAGE + 2 * PLANE + (wj + r32) * 8;
     stage = stage + 1 == STAGES ? 0 : stage + 1;
-    ou_h8 a[2][B][P], b[2][B][P];
+    ou_h8 a[2][B][2], b[2][B][2];
     auto operands = [&](int s) {
       const int place = (2 * (s + set * (4 / SETS)) + hh) ^ (r32 >> 1 & 7);
 #pragma unroll
       for (int x = 0; x < B; ++x)
 #pragma unroll
-        for (int q = 0; q < P; ++q) {
+        for (int q = 0; q < 2; ++q) {
           a[s & 1][x][q] = __builtin_bit_cast(ou_h8, sa[q * PLANE + x * 256 + place]);
           b[s & 1][x][q] = __builtin_bit_cast(ou_h8, sb[q * PLANE + x * 256 + place]);
         }
@@ -266,12 +263,12 @@ __global__ __launch_bounds__((OuTile<P, TILE>::THREADS)) void ou_product_kernel(
       if (s + 1 < 4 / SETS) operands(s + 1);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int t = P == 2 ? 0 : 2; t < 3; ++t)     // lo hi, hi lo, hi hi
+      for (int t = 0; t < 3; ++t)     // lo hi, hi lo, hi hi
 #pragma unroll
         for (int x = 0; x < B; ++x)
 #pragma unroll
           for (int y = 0; y < B; ++y)
-            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[s & 1][x][t == 0 ? P - 1 : 0], b[s & 1][y][t == 1 ? P - 1 : 0], acc[x][y], 0, 0, 0);
+            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[s & 1][x][t == 0], b[s & 1][y][t == 1], acc[x][y], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
@@ -306,9 +303,9 @@ __global__ __launch_bounds__((OuTile<P, TILE>::THREADS)) void ou_product_kernel(
   // would wait for it (so did barriers that wait for stores).
   const size_t plane_c = (size_t)o.I * o.J;
   constexpr int ACROSS = TILE / 8, ITEMS = TILE * ACROSS / THREADS;   // threads along a row, eight values each
-  constexpr bool OLD = WHAT == OU_POLY || (STEP && P == 1);       // + b g, or + a x
+  constexpr bool OLD = WHAT == OU_POLY;       // + b g
   const int n = p.n, m = p.m, across = tid % ACROSS * 8;
-  ou_h8 oh[OLD ? ITEMS : 1], ol[OLD && PB == 2 ? ITEMS : 1];
+  ou_h8 oh[OLD ? ITEMS : 1], ol[OLD ? ITEMS : 1];
   auto along_i = [&](int e, int& i, int& j, int& jl) {            // eight i of one j
     jl = tid / ACROSS + e * (THREADS / ACROSS);
     i = i0 + across;
@@ -320,9 +317,9 @@ __global__ __launch_bounds__((OuTile<P, TILE>::THREADS)) void ou_product_kernel(
     for (int e = 0; e < ITEMS; ++e) {
       int i, j, jl;
       along_i(e, i, j, jl);
-      const _Float16* old = (STEP ? Bm : A) + (size_t)min(j, o.J - 1) * o.I + min(i, o.I - 8);
+      const _Float16* old = A + (size_t)min(j, o.J - 1) * o.I + min(i, o.I - 8);
       oh[e] = *(const ou_h8*)old;
-      if (PB == 2) ol[e] = *(const ou_h8*)(old + plane_c);
+      ol[e] = *(const ou_h8*)(old + plane_c);
     }
   const bool flip = WHAT == OU_UPDATE || (WHAT == OU_LAST && !p.tall);     // rows of (another) result run along j
   float keep[WHAT == OU_LAST ? ITEMS : 1][8];
@@ -361,13 +358,8 @@ __global__ __launch_bounds__((OuTile<P, TILE>::THREADS)) void ou_product_kernel(
     if (OLD)
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        const float g = (float)oh[e][q] + (PB == 2 ? (float)ol[e][q] : 0.0f);
-        if (STEP) {
-          v[q] += (OU_A / OU_SX) * g;
-        } else {
-          v[q] = OU_C * v[q] + (OU_B / OU_SG) * g;
-          if (P == 2 && i + q == j && j < n) v[q] += OU_A;
-        }
+        v[q] = OU_C * v[q] + (OU_B / OU_SG) * ((float)oh[e][q] + (float)ol[e][q]);
+        if (i + q == j && j < n) v[q] += OU_A;
       }
     if (flip) {
       tile[slot(jl, across >> 2)] = make_float4(v[0], v[1], v[2], v[3]);
@@ -384,9 +376,9 @@ __global__ __launch_bounds__((OuTile<P, TILE>::THREADS)) void ou_product_kernel(
       ou_cut(v[q] * scale, h, l);
       hi[q] = h; lo[q] = l;
     }
-    _Float16* c = o.C + z * (STEP ? 2 : P) * plane_c + (size_t)j * o.I + i;
+    _Float16* c = o.C + z * 2 * plane_c + (size_t)j * o.I + i;
     *(ou_h8*)c = hi;
-    if (STEP || P == 2) *(ou_h8*)(c + plane_c) = lo;
+    *(ou_h8*)(c + plane_c) = lo;
   }
   if (!flip) return;
   ou_lds_barrier();
@@ -409,9 +401,9 @@ __global__ __launch_bounds__((OuTile<P, TILE>::THREADS)) void ou_product_kernel(
       ou_cut(v[q] * scale, h, l);
       hi[q] = h; lo[q] = l;
     }
-    _Float16* ct = o.Ct + z * P * plane_c + (size_t)i * o.J + j;
+    _Float16* ct = o.Ct + z * 2 * plane_c + (size_t)i * o.J + j;
     *(ou_h8*)ct = hi;
-    if (P == 2) *(ou_h8*)(ct + plane_c) = lo;
+    *(ou_h8*)(ct + plane_c) = lo;
   }
 }
 
@@ -832,11 +824,6 @@ OuShape ou_shape(int32_t batch, int32_t rows, int32_t cols) {
   return p;
 }
 
-// Pieces per operand.  One piece of 11 bits adds its error to that of a bfloat16 result (8 bits): measured on updates with a few
-// strong directions, 4e-4 to 6e-4 of the result beside the 1.7e-3 of the last rounding where both sides are at least 256, but 2e-3 at
-// 64 x 900 and more below; half precision and fp32 results would lose 2 and 400 times their own accuracy.
-int ou_pieces(const OuShape& p, int32_t dtype) { return dtype == EGNN_BF16 && p.n >= OU_ONE_PIECE ? 1 : 2; }
-
 struct OsSpace { size_t squares, x, g, bytes; int slabs, turns, blocks; };
 OsSpace os_space(const OuShape& p) {
   OsSpace s;
@@ -882,44 +869,44 @@ int ou_run_slabs(egnn_ctx* ctx, const OuShape& p, const OuInput<T>& in, const fl
 }
 
 struct OuSpace { size_t part, x, xt, g, bytes; };
-OuSpace ou_space(const OuShape& p, int pieces) {
+OuSpace ou_space(const OuShape& p) {
   if (p.n <= 64) return {0, 0, 0, 0, os_space(p).bytes};
   OuSpace s;
   s.part = 0;
   s.x = ou_align((size_t)p.batch * OU_PARTS * sizeof(double));
-  const size_t x = ou_align((size_t)p.batch * 2 * p.np * p.mp * 2), g = ou_align((size_t)p.batch * pieces * p.np * p.np * 2);
+  const size_t x = ou_align((size_t)p.batch * 2 * p.np * p.mp * 2), g = ou_align((size_t)p.batch * 2 * p.np * p.np * 2);
   s.xt = s.x + x;             // twice: a product reads one and writes the other
   s.g = s.xt + 2 * x;         // g and p
   s.bytes = s.g + 2 * g;
   return s;
 }
 
-template <class T, int P, int TILE, OuProduct WHAT>
+template <class T, int TILE, OuProduct WHAT>
 int ou_product_tile(egnn_ctx* ctx, const OuShape& p, const OuOperands& o, const OuOut<T>& out, hipStream_t st) {
-  constexpr size_t lds = OuTile<P, TILE>::LDS;
+  constexpr size_t lds = OuTile<TILE>::LDS;
   static bool ready[64];
-  if (int rc = rt_allow_lds(ctx, (const void*)ou_product_kernel<T, P, TILE, WHAT>, lds, ready)) return rc;
+  if (int rc = rt_allow_lds(ctx, (const void*)ou_product_kernel<T, TILE, WHAT>, lds, ready)) return rc;
   const dim3 grid((o.J + TILE - 1) / TILE, (o.I + TILE - 1) / TILE, p.batch);
-  hipLaunchKernelGGL((ou_product_kernel<T, P, TILE, WHAT>), grid, dim3(OuTile<P, TILE>::THREADS), lds, st, p, o, out);
+  hipLaunchKernelGGL((ou_product_kernel<T, TILE, WHAT>), grid, dim3(OuTile<TILE>::THREADS), lds, st, p, o, out);
   EGNN_LAUNCH_CHECK(ctx, "orthogonalise");
   return EGNN_OK;
 }
 
 // Tiles of 128 where half the compute units get one, else of 64: a wide tile takes half the LDS traffic a product, but four times as long
 // (us a step, 128 against 64: 1 x 768 x 768 fp32 367 : 149, 1 x 1280 x 2048 633 : 515, 2 x 1310 x 1071 529 : 603, 1 x 1536 x 2048 684 : 732).
-template <class T, int P, OuProduct WHAT>
+template <class T, OuProduct WHAT>
 int ou_product(egnn_ctx* ctx, const OuShape& p, const OuOperands& o, const OuOut<T>& out, hipStream_t st) {
   const long wide = (long)((o.I + 127) / 128) * ((o.J + 127) / 128) * p.batch;
-  if (wide >= 128) return ou_product_tile<T, P, 128, WHAT>(ctx, p, o, out, st);
-  return ou_product_tile<T, P, 64, WHAT>(ctx, p, o, out, st);
+  if (wide >= 128) return ou_product_tile<T, 128, WHAT>(ctx, p, o, out, st);
+  return ou_product_tile<T, 64, WHAT>(ctx, p, o, out, st);
 }
 
-template <class T, int P>
+template <class T>
 int ou_run(egnn_ctx* ctx, const OuShape& p, const OuInput<T>& in, const float* m_old, float* m_new, int steps, const OuOut<T>& out,
            void* ws, hipStream_t st) {
   if (p.n <= 32) return ou_run_slabs<T, 1>(ctx, p, in, m_old, m_new, steps, out, ws, st);
   if (p.n <= 64) return ou_run_slabs<T, 2>(ctx, p, in, m_old, m_new, steps, out, ws, st);
-  const OuSpace s = ou_space(p, P);
+  const OuSpace s = ou_space(p);
   double* part = (double*)((char*)ws + s.part);
   _Float16* x = (_Float16*)((char*)ws + s.x);
   _Float16* xt = (_Float16*)((char*)ws + s.xt);
@@ -933,14 +920,14 @@ int ou_run(egnn_ctx* ctx, const OuShape& p, const OuInput<T>& in, const float* m
     hipLaunchKernelGGL((ou_square_kernel<T, 4>), dim3(parts, p.batch), dim3(256), 0, st, in, m_old, m_new, size, part);
   else
     hipLaunchKernelGGL((ou_square_kernel<T, 1>), dim3(parts, p.batch), dim3(256), 0, st, in, m_old, m_new, size, part);
-  hipLaunchKernelGGL((ou_pieces_kernel<T, P>), dim3(p.mp / 64, p.np / 64, p.batch), dim3(256), 0, st, p, in, part, parts, x, xt);
+  hipLaunchKernelGGL((ou_pieces_kernel<T>), dim3(p.mp / 64, p.np / 64, p.batch), dim3(256), 0, st, p, in, part, parts, x, xt);
   EGNN_LAUNCH_CHECK(ctx, "orthogonalise");
   const OuOut<float> none{};
   for (int k = 0; k < steps; ++k) {
-    if (int rc = ou_product<float, P, OU_GRAM>(ctx, p, {x, x, g, nullptr, p.np, p.np, p.mp}, none, st)) return rc;
-    if (int rc = ou_product<float, P, OU_POLY>(ctx, p, {g, g, q, nullptr, p.np, p.np, p.np}, none, st)) return rc;
-    if (k + 1 == steps) return ou_product<T, P, OU_LAST>(ctx, p, {q, xt, nullptr, nullptr, p.np, p.mp, p.np}, out, st);
-    if (int rc = ou_product<float, P, OU_UPDATE>(ctx, p, {q, xt, xt2, x, p.np, p.mp, p.np}, none, st)) return rc;
+    if (int rc = ou_product<float, OU_GRAM>(ctx, p, {x, x, g, nullptr, p.np, p.np, p.mp}, none, st)) return rc;
+    if (int rc = ou_product<float, OU_POLY>(ctx, p, {g, g, q, nullptr, p.np, p.np, p.np}, none, st)) return rc;
+    if (k + 1 == steps) return ou_product<T, OU_LAST>(ctx, p, {q, xt, nullptr, nullptr, p.np, p.mp, p.np}, out, st);
+    if (int rc = ou_product<float, OU_UPDATE>(ctx, p, {q, xt, xt2, x, p.np, p.mp, p.np}, none, st)) return rc;
     _Float16* t = xt; xt = xt2; xt2 = t;
   }
   return EGNN_OK;
@@ -955,13 +942,11 @@ int ou_check(egnn_ctx* ctx, const char* who, int32_t batch, int32_t rows, int32_
 }
 
 template <class T>
-int ou_matrices(egnn_ctx* ctx, int32_t dtype, const OuShape& p, const void* g, int steps, void* y, void* ws, hipStream_t st) {
+int ou_matrices(egnn_ctx* ctx, const OuShape& p, const void* g, int steps, void* y, void* ws, hipStream_t st) {
   const OuInput<T> in{(const T*)g, nullptr, 0.0f};
   const OuOut<T> out{(T*)y, nullptr, 0.0f, 0.0f, p.cols % 8 == 0 && (uintptr_t)y % 16 == 0,
                      p.tall && p.cols % 4 == 0 && ((uintptr_t)g | (uintptr_t)y) % (4 * sizeof(T)) == 0};
-  if constexpr (std::is_same<T, __bf16>::value)
-    if (ou_pieces(p, dtype) == 1) return ou_run<T, 1>(ctx, p, in, nullptr, nullptr, steps, out, ws, st);
-  return ou_run<T, 2>(ctx, p, in, nullptr, nullptr, steps, out, ws, st);
+  return ou_run<T>(ctx, p, in, nullptr, nullptr, steps, out, ws, st);
 }
 
 }  // namespace
@@ -969,7 +954,7 @@ int ou_matrices(egnn_ctx* ctx, int32_t dtype, const OuShape& p, const void* g, i
 extern "C" int egnn_orthogonalise_workspace_bytes(const egnn_ctx* ctx, int32_t batch, int32_t rows, int32_t cols, size_t* bytes) {
   if (!ctx || !bytes) return egnn_fail(const_cast<egnn_ctx*>(ctx), EGNN_EINVAL, "orthogonalise_workspace_bytes: null pointer");
   if (int rc = ou_check(const_cast<egnn_ctx*>(ctx), "orthogonalise_workspace_bytes", batch, rows, cols, 1)) return rc;
-  *bytes = ou_space(ou_shape(batch, rows, cols), 2).bytes;
+  *bytes = ou_space(ou_shape(batch, rows, cols)).bytes;
   return EGNN_OK;
 }
 
@@ -981,12 +966,12 @@ extern "C" int egnn_orthogonalise(egnn_ctx* ctx, int32_t dtype, const void* g, i
   if (batch == 0) return EGNN_OK;
   if (!g || !y) return egnn_fail(ctx, EGNN_EINVAL, "orthogonalise: null pointer");
   const OuShape p = ou_shape(batch, rows, cols);
-  if (!ws || (uintptr_t)ws % 256 || ws_bytes < ou_space(p, ou_pieces(p, dtype)).bytes)
+  if (!ws || (uintptr_t)ws % 256 || ws_bytes < ou_space(p).bytes)
     return egnn_fail(ctx, EGNN_EWS, "orthogonalise: workspace too small or not 256-byte aligned");
   hipStream_t st = (hipStream_t)stream;
-  if (dtype == EGNN_F32) return ou_matrices<float>(ctx, dtype, p, g, steps, y, ws, st);
-  if (dtype == EGNN_F16) return ou_matrices<_Float16>(ctx, dtype, p, g, steps, y, ws, st);
-  return ou_matrices<__bf16>(ctx, dtype, p, g, steps, y, ws, st);
+  if (dtype == EGNN_F32) return ou_matrices<float>(ctx, p, g, steps, y, ws, st);
+  if (dtype == EGNN_F16) return ou_matrices<_Float16>(ctx, p, g, steps, y, ws, st);
+  return ou_matrices<__bf16>(ctx, p, g, steps, y, ws, st);
 }
 
 extern "C" int egnn_muon_step(egnn_ctx* ctx, const float* W, const float* g, const float* m, int32_t batch, int32_t rows, int32_t cols,
@@ -997,11 +982,11 @@ extern "C" int egnn_muon_step(egnn_ctx* ctx, const float* W, const float* g, con
   if (batch == 0) return EGNN_OK;
   if (!W || !g || !m || !W_out || !m_out) return egnn_fail(ctx, EGNN_EINVAL, "muon_step: null pointer");
   const OuShape p = ou_shape(batch, rows, cols);
-  if (!ws || (uintptr_t)ws % 256 || ws_bytes < ou_space(p, 2).bytes)
+  if (!ws || (uintptr_t)ws % 256 || ws_bytes < ou_space(p).bytes)
     return egnn_fail(ctx, EGNN_EWS, "muon_step: workspace too small or not 256-byte aligned");
   const float scale = (float)((double)lr * sqrt(rows > cols ? (double)rows / cols : 1.0));
   const float keep = (float)(1.0 - (double)lr * (double)weight_decay);
   const uintptr_t all = (uintptr_t)g | (uintptr_t)m | (uintptr_t)m_out | (uintptr_t)W | (uintptr_t)W_out;
   const OuOut<float> out{W_out, W, keep, scale, cols % 8 == 0 && (uintptr_t)W_out % 16 == 0, p.tall && cols % 4 == 0 && all % 16 == 0};
-  return ou_run<float, 2>(ctx, p, OuInput<float>{g, m_out, beta}, m, m_out, steps, out, ws, (hipStream_t)stream);
+  return ou_run<float>(ctx, p, OuInput<float>{g, m_out, beta}, m, m_out, steps, out, ws, (hipStream_t)stream);
 }
