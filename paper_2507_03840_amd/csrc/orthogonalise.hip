@@ -1,6 +1,6 @@
 // An update orthogonalised by Newton-Schulz products, and the optimiser's step around it.
 //
-//   x_0 = u / (|u|_F + 1e-7),   x_{k+1} = p x_k,   p = a I + b g + c g^2,   g = x_k x_k^T  (x from the side with fewer rows),
+//   x_0 = u / (|u|_F + 1e-7),   x_{k+1} = a x_k + p x_k,   p = b g + c g^2,   g = x_k x_k^T  (x from the side with fewer rows),
 // with the published coefficients of the Muon optimiser: the singular values of u go to within about 0.7 .. 1.2.
 // Step: m' = beta m + g, u = g + beta m', W' = (1 - lr weight_decay) W - lr sqrt(max(1, rows / cols)) orthogonalise(u).
 //
@@ -9,6 +9,8 @@
 // rounded to 11 bits, and hi hi + hi lo + lo hi (the dropped lo lo is 2^-24 of the product).  |x_0|_F <= 1 and the steps keep
 // the singular values below 1.2025, so every entry of x, g and p is bounded whatever the input, and one fixed power of two as
 // scale s leaves nothing to overflow and nothing above 2^-39 to underflow.
+// p stays without its a I, and a x is added to (b g + c g^2) x in fp32: pieces of 22 bits of a on the diagonal of p would take the same part
+// of every singular value's last bits, again in every step (1536 x 2048 1.33e-5 off 64 bits with it in p, 5.4e-6 without; torch in fp32 8.3e-6).
 // Every type of result comes from both pieces: with hi alone bfloat16 results of wide updates were 4e-4 to 6e-4 off beside their last rounding
 // (1.7e-3).
 #include "row_types.h"
@@ -20,7 +22,7 @@ namespace {
 
 constexpr float OU_A = 3.4445f, OU_B = -4.7750f, OU_C = 2.0315f;
 constexpr double OU_EPS = 1e-7;
-// entries of x are at most 1.2025, of g 1.446, of p 3.4445 (its eigenvalues lie between 0.6 and a): times these at most 56,500
+// entries of x are at most 1.2025, of g 1.446, of p 2.81 (its eigenvalues lie between b^2 / 4c = -2.81 and 0): times these at most 47,400
 constexpr float OU_SX = 32768.0f, OU_SG = 32768.0f, OU_SP = 16384.0f;
 constexpr int OU_PARTS = 512;       // partial sums of squares per matrix, at most
 
@@ -303,7 +305,8 @@ __global__ __launch_bounds__((OuTile<TILE>::THREADS)) void ou_product_kernel(OuS
   // would wait for it (so did barriers that wait for stores).
   const size_t plane_c = (size_t)o.I * o.J;
   constexpr int ACROSS = TILE / 8, ITEMS = TILE * ACROSS / THREADS;   // threads along a row, eight values each
-  constexpr bool OLD = WHAT == OU_POLY;       // + b g
+  constexpr bool STEP = WHAT == OU_UPDATE || WHAT == OU_LAST;   // p x
+  constexpr bool OLD = WHAT == OU_POLY || STEP;                 // + b g, or + a x
   const int n = p.n, m = p.m, across = tid % ACROSS * 8;
   ou_h8 oh[OLD ? ITEMS : 1], ol[OLD ? ITEMS : 1];
   auto along_i = [&](int e, int& i, int& j, int& jl) {            // eight i of one j
@@ -317,7 +320,7 @@ __global__ __launch_bounds__((OuTile<TILE>::THREADS)) void ou_product_kernel(OuS
     for (int e = 0; e < ITEMS; ++e) {
       int i, j, jl;
       along_i(e, i, j, jl);
-      const _Float16* old = A + (size_t)min(j, o.J - 1) * o.I + min(i, o.I - 8);
+      const _Float16* old = (STEP ? Bm : A) + (size_t)min(j, o.J - 1) * o.I + min(i, o.I - 8);
       oh[e] = *(const ou_h8*)old;
       ol[e] = *(const ou_h8*)(old + plane_c);
     }
@@ -358,8 +361,8 @@ __global__ __launch_bounds__((OuTile<TILE>::THREADS)) void ou_product_kernel(OuS
     if (OLD)
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        v[q] = OU_C * v[q] + (OU_B / OU_SG) * ((float)oh[e][q] + (float)ol[e][q]);
-        if (i + q == j && j < n) v[q] += OU_A;
+        const float before = (float)oh[e][q] + (float)ol[e][q];
+        v[q] = STEP ? v[q] + (OU_A / OU_SX) * before : OU_C * v[q] + (OU_B / OU_SG) * before;
       }
     if (flip) {
       tile[slot(jl, across >> 2)] = make_float4(v[0], v[1], v[2], v[3]);
@@ -640,7 +643,7 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
     }
   };
 
-  // p = a I + b g + c g g in LDS, from the parts of g of all waves or of all slabs; in step 1 times the scale of this slab's x
+  // p = b g + c g g in LDS, from the parts of g of all waves or of all slabs; in step 1 times the scale of this slab's x, which is returned
   auto make_p = [&](bool first) {
     double norm = 1.0, factor = 1.0;
     if (!ALONE && first) {
@@ -689,9 +692,7 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
         float v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-          const int i = 16 * t + 8 * (q >> 2) + 4 * hh + (q & 3);
           v[q] = (OU_C / (OU_SG * OU_SG)) * acc[8 * t + q] + (OU_B / OU_SG) * ((float)ge[0][q] + (float)ge[1][q]);
-          v[q] += a == b && i == r32 ? OU_A : 0.0f;
           v[q] *= (float)factor;
         }
         os_cut(v, OU_SP, h, l);
@@ -701,10 +702,11 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
       }
     }
     __syncthreads();
+    return (float)factor;
   };
 
-  // p x, row block b
-  auto times_p = [&](int b) {
+  // a x + p x, row block b
+  auto times_p = [&](int b, float factor) {
     ou_f16v acc = os_zero();
 #pragma unroll
     for (int c = 0; c < NB; ++c)
@@ -714,17 +716,22 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
         fragment(sp, c, b, t, pf);
         acc = os_product(pf, x[c][t], acc);
       }
+    const float a = factor * (OU_A * OU_SP);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) acc[8 * t + q] += a * ((float)x[b][t][0][q] + (float)x[b][t][1][q]);
     return acc;
   };
 
-  auto advance = [&]() {
+  auto advance = [&](float factor) {
     clear();
     for (int turn = 0; turn < turns; ++turn) {
       if (!ALONE) load_x(turn);
       ou_h8 xt[NB][2][2];
       ou_f16v next[NB];
 #pragma unroll
-      for (int b = 0; b < NB; ++b) next[b] = times_p(b);
+      for (int b = 0; b < NB; ++b) next[b] = times_p(b, factor);
 #pragma unroll
       for (int b = 0; b < NB; ++b) cut(next[b], 1.0f / OU_SP, x[b]);
       if (!ALONE) store_x(turn);
@@ -734,7 +741,7 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
     }
   };
 
-  auto finish = [&]() {
+  auto finish = [&](float factor) {
     for (int turn = 0; turn < turns; ++turn) {
       float old[NB][4][4];
       if (out.W)
@@ -749,7 +756,7 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
       if (!ALONE) load_x(turn);
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        const ou_f16v last = times_p(b);
+        const ou_f16v last = times_p(b, factor);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           size_t at;
@@ -793,22 +800,20 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
     begin();
     publish();
     for (int k = 1; k < steps; ++k) {
-      make_p(false);
-      advance();
+      advance(make_p(false));
       publish();
     }
-    make_p(false);
-    finish();
+    finish(make_p(false));
   } else if (step == 0) {
     begin();
     publish();
   } else {
-    make_p(step == 1);
+    const float factor = make_p(step == 1);
     if (step < steps) {
-      advance();
+      advance(factor);
       publish();
     } else {
-      finish();
+      finish(factor);
     }
   }
 }

@@ -34,3 +34,23 @@ def test_fewer_bits_are_the_last_rounding_alone(m, shape, dtype, bits, least):
     beyond = np.maximum(np.abs(m.egnn_orthogonalise(g).double().cpu().numpy() - want) - half, 0.0)
     print(shape, dtype, "beyond half a step: %.2e" % (np.linalg.norm(beyond) / np.linalg.norm(want)))
     assert np.linalg.norm(beyond) <= 2 * FULL * np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("shape", [(300, 301), (320, 960), (1500, 640), (900, 1200)])
+def test_no_farther_off_than_products_in_fp32(m, shape):
+    """Operands of 22 bits lose a little more than those of 24; but what a step does to x beyond a x is added to it in fp32, so that only the part
+    that changes x is made of them.  Both are sums of as many products in fp32: the distance from fp64 is no larger than that of the formula
+    with fp32 products of matrices (torch, on the same device)."""
+    import torch
+    a, b, c = K.COEFFICIENTS
+    g = torch.from_numpy(random(np.random.default_rng([2, *shape]), 1, *shape)).float().cuda()
+    want = K.orthogonalise(g.double().cpu().numpy())[0]
+    x = g[0] if shape[0] <= shape[1] else g[0].t().contiguous()
+    x = x / (x.square().sum().sqrt() + K.EPS_NORM_F)
+    for _ in range(5):
+        p = x @ x.t().contiguous()
+        x = a * x + (b * p + c * (p @ p)) @ x
+    x = x if shape[0] <= shape[1] else x.t()
+    off = lambda y: np.linalg.norm(y.double().cpu().numpy() - want) / np.linalg.norm(want)
+    print(shape, "off by %.2e, in fp32 products %.2e" % (off(m.egnn_orthogonalise(g)[0]), off(x)))
+    assert off(m.egnn_orthogonalise(g)[0]) <= off(x)
