@@ -518,7 +518,9 @@ int egnn_unpack_rows(egnn_ctx* ctx, const void* buf, int32_t n_rows, int32_t hal
  *
  * egnn_orthogonalise: y_b = q(g_b) for each of batch matrices [rows][cols]: x = g / (|g|_F + 1e-7), then `steps` times
  *   x <- 3.4445 x - 4.7750 (x x^T) x + 2.0315 (x x^T)^2 x (Newton-Schulz products with the coefficients published with the Muon
- *   optimiser; they bring the singular values near 1, not to it).  steps in 1..32.  y may be g.
+ *   optimiser; they bring the singular values near 1, not to it).  steps in 1..32.  y may be g.  The accuracy does not depend on |g|_F.
+ *   Products are fp32 sums; their operands are held to 2^-23 of themselves, but not below 2^-40 of the norm of g (of 1 once x has
+ *   grown): what lies so far below the rest of g is taken as zero, however many steps would raise it.
  * egnn_muon_step: m' = beta m + g, u = g + beta m', W' = (1 - lr weight_decay) W - lr sqrt(max(1, rows / cols)) q(u), all fp32;
  *   m_out may be m, W_out may be W. */
 #define EGNN_F32 0

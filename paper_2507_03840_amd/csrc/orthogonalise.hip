@@ -8,7 +8,12 @@
 // beside x.  They run on the matrix cores on half-precision pieces: v s = hi + lo, hi = v s rounded to 11 bits, lo = the rest
 // rounded to 11 bits, and hi hi + hi lo + lo hi (the dropped lo lo is 2^-24 of the product).  |x_0|_F <= 1 and the steps keep
 // the singular values below 1.2025, so every entry of x, g and p is bounded whatever the input, and one fixed power of two as
-// scale s leaves nothing to overflow and nothing above 2^-39 to underflow.
+// scale s leaves nothing to overflow.  Nothing above 2^-39 underflows, and that counts from the norm: what is kept is X, x = sigma X, from
+// X_0 = u / |u|, sigma_0 = |u| / (|u| + 1e-7) on, sigma_{k+1} = min(1, a sigma_k): where |u| is far below 1e-7, x is too, and a few steps
+// only multiply it by a.  With r = sigma_k / sigma_{k+1} = max(1 / a, sigma_k) a step is
+//   X_{k+1} = r (a X + (b sigma^2 G + c sigma^4 G^2) X),   G = X X^T,
+// whose factor of each singular value lies below that of sigma = 1, so the bounds hold for X as well.  Above |u| = 5e-8 sigma is 1 from the
+// second step on.
 // p stays without its a I, and a x is added to (b g + c g^2) x in fp32: pieces of 22 bits of a on the diagonal of p would take the same part
 // of every singular value's last bits, again in every step (1536 x 2048 1.33e-5 off 64 bits with it in p, 5.4e-6 without; torch in fp32 8.3e-6).
 // Every type of result comes from both pieces: with hi alone bfloat16 results of wide updates were 4e-4 to 6e-4 off beside their last rounding
@@ -91,17 +96,28 @@ __global__ __launch_bounds__(256) void ou_square_kernel(OuInput<T> in, const flo
   if (threadIdx.x == 0) part[(size_t)blockIdx.y * OU_PARTS + blockIdx.x] = s[0];
 }
 
-// 1 / (|u| + eps) of one matrix, in every lane
-__device__ __forceinline__ double ou_inverse_norm(const double* part, int parts) {
+// sum of squares of one matrix from its parts, in every lane
+__device__ __forceinline__ double ou_squares(const double* part, int parts) {
   double t = 0.0;
   for (int i = threadIdx.x & 63; i < parts; i += 64) t += part[i];
   for (int h = 32; h; h >>= 1) t += __shfl_xor(t, h);
-  return 1.0 / (sqrt(t) + OU_EPS);
+  return t;
+}
+
+__device__ __forceinline__ double ou_inverse(double squares) { return squares == 0.0 ? 0.0 : 1.0 / sqrt(squares); }   // (a NaN stays one)
+__device__ __forceinline__ double ou_sigma0(double squares) { return sqrt(squares) / (sqrt(squares) + OU_EPS); }
+
+// Factors of step k (0, 1, ..) of a matrix: X_{k+1} = x X + (g G + gg G^2) X, and sigma_{k+1}
+struct OuStep { float x, g, gg, sigma; };
+__device__ __forceinline__ OuStep ou_step(double sigma, int k) {
+  for (; k > 0 && sigma < 1.0; --k) sigma = fmin(1.0, (double)OU_A * sigma);
+  const double next = fmin(1.0, (double)OU_A * sigma), r = next < 1.0 ? 1.0 / (double)OU_A : sigma, s2 = sigma * sigma;
+  return {(float)(r * OU_A), (float)(r * OU_B * s2), (float)(r * OU_C * s2 * s2), (float)next};
 }
 
 // ---- x_0 in pieces, in both layouts: 64 x 64 tiles.  x [hi, lo][np][mp], xt [hi, lo][mp][np] per matrix
 template <class T>
-__global__ __launch_bounds__(256) void ou_pieces_kernel(OuShape p, OuInput<T> in, const double* part, int parts, _Float16* x,
+__global__ __launch_bounds__(256) void ou_pieces_kernel(OuShape p, OuInput<T> in, const double* part, int parts, double* sigma, _Float16* x,
                                                         _Float16* xt) {
   __shared__ float tile[64][65];    // [i][j] of x
   const size_t z = blockIdx.z;
@@ -113,7 +129,8 @@ __global__ __launch_bounds__(256) void ou_pieces_kernel(OuShape p, OuInput<T> in
     const int i = min(i0 + (p.tall ? b : a), p.n - 1), j = min(j0 + (p.tall ? a : b), p.m - 1);
     v[k] = ou_value(in, z * p.rows * p.cols + (p.tall ? (size_t)j * p.cols + i : (size_t)i * p.cols + j));
   }
-  const double inv = ou_inverse_norm(part + z * OU_PARTS, parts) * (double)OU_SX;
+  const double squares = ou_squares(part + z * OU_PARTS, parts), inv = ou_inverse(squares) * (double)OU_SX;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && t == 0) sigma[z] = ou_sigma0(squares);
 #pragma unroll
   for (int k = 0; k < 16; ++k) {
     const int a = (t >> 6) + 4 * k, b = t & 63;
@@ -159,6 +176,8 @@ struct OuOperands {
   const _Float16 *A, *B;   // per matrix [hi, lo][I][K], [hi, lo][J][K]
   _Float16 *C, *Ct;        // results in pieces: C [hi, lo][J][I] (the transpose; g and p are symmetric), Ct [hi, lo][I][J]
   int I, J, K;             // multiples of 64
+  const double* sigma;     // sigma_0 of every matrix
+  int step;
 };
 
 typedef const __attribute__((address_space(1))) void* ou_gp;
@@ -324,6 +343,7 @@ __global__ __launch_bounds__((OuTile<TILE>::THREADS)) void ou_product_kernel(OuS
       oh[e] = *(const ou_h8*)old;
       ol[e] = *(const ou_h8*)(old + plane_c);
     }
+  const OuStep step = OLD ? ou_step(o.sigma[z], o.step) : OuStep{};
   const bool flip = WHAT == OU_UPDATE || (WHAT == OU_LAST && !p.tall);     // rows of (another) result run along j
   float keep[WHAT == OU_LAST ? ITEMS : 1][8];
   if (WHAT == OU_LAST && out.W)
@@ -339,7 +359,7 @@ __global__ __launch_bounds__((OuTile<TILE>::THREADS)) void ou_product_kernel(OuS
     if (r >= p.rows || c >= p.cols) return;
 #pragma unroll
     for (int q = 0; q < 8; ++q)
-      if (out.W) v[q] = keep[e][q] - out.scale * v[q];
+      v[q] = out.W ? keep[e][q] - out.scale * step.sigma * v[q] : step.sigma * v[q];
     T* to = out.y + z * n * m + (size_t)r * p.cols + c;
     if (out.eights) {
       rt_store<T, 8>(to, v);
@@ -362,7 +382,7 @@ __global__ __launch_bounds__((OuTile<TILE>::THREADS)) void ou_product_kernel(OuS
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
         const float before = (float)oh[e][q] + (float)ol[e][q];
-        v[q] = STEP ? v[q] + (OU_A / OU_SX) * before : OU_C * v[q] + (OU_B / OU_SG) * before;
+        v[q] = STEP ? v[q] + step.x * (1.0f / OU_SX) * before : step.gg * v[q] + step.g * (1.0f / OU_SG) * before;
       }
     if (flip) {
       tile[slot(jl, across >> 2)] = make_float4(v[0], v[1], v[2], v[3]);
@@ -420,7 +440,7 @@ __global__ __launch_bounds__((OuTile<TILE>::THREADS)) void ou_product_kernel(OuS
 // order that does not matter as long as both operands share it.  So the fragments of g serve as both operands of g g (g and p are
 // symmetric), those of x (lane = k, registers = i) with p's make the next x, and x^T (lane = column j, registers = rows k), both operands of g,
 // is x times the identity: no value ever changes lanes but in the matrix cores.
-// Until step 1 a slab is scaled by its own norm: the sums of squares of the others come with their parts of g, no pass for |u| alone.
+// Until step 1 a slab is scaled by its own norm: the sums of squares of the others come with their parts of G, no pass for |u| alone.
 //
 // g g keeps lo lo as well: on its diagonal these are squares, which add up instead of averaging out (8 x 300 to 64 x 64 fp32, against 64
 // bits: 0.63 to 1.2e-6 off with it, 0.67 to 1.4e-6 without, torch in fp32 0.65 to 1.3e-6; 15 x 32 x 32 12.7 us against 12.6).
@@ -435,6 +455,7 @@ struct OsPlace {
   const float4* part_in;  // [batch][slabs][NB^2 blocks][4][64 lanes]: parts of g of this step
   float4* part_out;       // of the next one
   double* squares;        // [batch][slabs]: sums of squares of the slabs
+  double* sigma;          // [batch], from step 1 on
   int slabs, turns;
 };
 
@@ -609,7 +630,8 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
     cut(rows, 1.0f, to);
   };
 
-  // step 0: x = u / |u| and its g
+  // step 0: X = u / |u| (of the slab) and its G
+  double sigma0 = 0.0;
   auto begin = [&]() {
     float u[NB][16];
     double t = 0.0;
@@ -621,7 +643,8 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
         for (int q = 0; q < 16; ++q) t += (double)u[b][q] * (double)u[b][q];
     }
     t = os_sum(t, (double*)smem);
-    const double inverse = ALONE ? 1.0 / (sqrt(t) + OU_EPS) : t == 0.0 ? 0.0 : 1.0 / sqrt(t);
+    const double inverse = ou_inverse(t);
+    if (ALONE) sigma0 = ou_sigma0(t);
     if (!ALONE && tid == 0) w.squares[z * w.slabs + slab] = t;
     clear();
     for (int turn = 0; turn < turns; ++turn) {
@@ -643,16 +666,26 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
     }
   };
 
-  // p = b g + c g g in LDS, from the parts of g of all waves or of all slabs; in step 1 times the scale of this slab's x, which is returned
-  auto make_p = [&](bool first) {
+  // p of step k = 1, 2, .. in LDS, from the parts of G of all waves or of all slabs; in step 1 times the scale of this slab's X, as are the
+  // factors that are returned
+  auto make_p = [&](int k) {
+    const bool first = k == 1;
     double norm = 1.0, factor = 1.0;
-    if (!ALONE && first) {
-      double t = 0.0;
-      for (int i = lane; i < w.slabs; i += 64) t += w.squares[z * w.slabs + i];
-      for (int h = 32; h; h >>= 1) t += __shfl_xor(t, h);
-      norm = 1.0 / (sqrt(t) + OU_EPS);
-      factor = sqrt(w.squares[z * w.slabs + slab]) * norm;
+    if (!ALONE) {
+      if (first) {
+        const double t = ou_squares(w.squares + z * w.slabs, w.slabs);
+        norm = ou_inverse(t);
+        factor = sqrt(w.squares[z * w.slabs + slab]) * norm;
+        sigma0 = ou_sigma0(t);
+        if (slab == 0 && tid == 0) w.sigma[z] = sigma0;
+      } else {
+        sigma0 = w.sigma[z];
+      }
     }
+    OuStep at_step = ou_step(sigma0, k - 1);
+    at_step.x *= (float)factor;
+    at_step.g *= (float)factor;
+    at_step.gg *= (float)factor;
     const int parts = ALONE ? waves : w.slabs;
     const float4* from = ALONE ? sums : w.part_in + z * w.slabs * Lds::PARTS;
     for (int e = tid; e < NB * NB * 128; e += blockDim.x) {        // the values of one fragment are two float4 of a lane
@@ -692,8 +725,7 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
         float v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-          v[q] = (OU_C / (OU_SG * OU_SG)) * acc[8 * t + q] + (OU_B / OU_SG) * ((float)ge[0][q] + (float)ge[1][q]);
-          v[q] *= (float)factor;
+          v[q] = at_step.gg * (1.0f / (OU_SG * OU_SG)) * acc[8 * t + q] + at_step.g * (1.0f / OU_SG) * ((float)ge[0][q] + (float)ge[1][q]);
         }
         os_cut(v, OU_SP, h, l);
         uint4* to = sp + (e * 2 + t) * 128 + lane;
@@ -702,11 +734,11 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
       }
     }
     __syncthreads();
-    return (float)factor;
+    return at_step;
   };
 
-  // a x + p x, row block b
-  auto times_p = [&](int b, float factor) {
+  // the next X (times OU_SP OU_SX), row block b
+  auto times_p = [&](int b, const OuStep& f) {
     ou_f16v acc = os_zero();
 #pragma unroll
     for (int c = 0; c < NB; ++c)
@@ -716,7 +748,7 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
         fragment(sp, c, b, t, pf);
         acc = os_product(pf, x[c][t], acc);
       }
-    const float a = factor * (OU_A * OU_SP);
+    const float a = f.x * OU_SP;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -724,14 +756,14 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
     return acc;
   };
 
-  auto advance = [&](float factor) {
+  auto advance = [&](const OuStep& f) {
     clear();
     for (int turn = 0; turn < turns; ++turn) {
       if (!ALONE) load_x(turn);
       ou_h8 xt[NB][2][2];
       ou_f16v next[NB];
 #pragma unroll
-      for (int b = 0; b < NB; ++b) next[b] = times_p(b, factor);
+      for (int b = 0; b < NB; ++b) next[b] = times_p(b, f);
 #pragma unroll
       for (int b = 0; b < NB; ++b) cut(next[b], 1.0f / OU_SP, x[b]);
       if (!ALONE) store_x(turn);
@@ -741,7 +773,7 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
     }
   };
 
-  auto finish = [&](float factor) {
+  auto finish = [&](const OuStep& f) {
     for (int turn = 0; turn < turns; ++turn) {
       float old[NB][4][4];
       if (out.W)
@@ -756,7 +788,7 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
       if (!ALONE) load_x(turn);
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        const ou_f16v last = times_p(b, factor);
+        const ou_f16v last = times_p(b, f);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           size_t at;
@@ -764,7 +796,7 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
           float v[4];
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            v[q] = last[4 * r + q] * (1.0f / (OU_SP * OU_SX));
+            v[q] = last[4 * r + q] * (1.0f / (OU_SP * OU_SX)) * f.sigma;
             if (out.W) v[q] = out.keep * old[b][r][q] - out.scale * v[q];
           }
           store4(out.y, at, there, v);
@@ -800,20 +832,20 @@ __global__ __launch_bounds__(512) void ou_slab_kernel(OuShape p, OuInput<T> in, 
     begin();
     publish();
     for (int k = 1; k < steps; ++k) {
-      advance(make_p(false));
+      advance(make_p(k));
       publish();
     }
-    finish(make_p(false));
+    finish(make_p(steps));
   } else if (step == 0) {
     begin();
     publish();
   } else {
-    const float factor = make_p(step == 1);
+    const OuStep f = make_p(step);
     if (step < steps) {
-      advance(factor);
+      advance(f);
       publish();
     } else {
-      finish(factor);
+      finish(f);
     }
   }
 }
@@ -829,7 +861,7 @@ OuShape ou_shape(int32_t batch, int32_t rows, int32_t cols) {
   return p;
 }
 
-struct OsSpace { size_t squares, x, g, bytes; int slabs, turns, blocks; };
+struct OsSpace { size_t squares, sigma, x, g, bytes; int slabs, turns, blocks; };
 OsSpace os_space(const OuShape& p) {
   OsSpace s;
   const int slabs = (p.m + OS_ROWS - 1) / OS_ROWS;
@@ -837,7 +869,8 @@ OsSpace os_space(const OuShape& p) {
   s.turns = (slabs + OS_SLABS - 1) / OS_SLABS;
   s.slabs = (slabs + s.turns - 1) / s.turns;
   s.squares = 0;
-  s.x = ou_align((size_t)p.batch * s.slabs * sizeof(double));
+  s.sigma = ou_align((size_t)p.batch * s.slabs * sizeof(double));
+  s.x = s.sigma + ou_align((size_t)p.batch * sizeof(double));
   s.g = s.x + ou_align((size_t)p.batch * s.slabs * s.turns * OS_WAVES * s.blocks * 256 * sizeof(uint4));
   s.bytes = slabs == 1 ? 256 : s.g + 2 * ou_align((size_t)p.batch * s.slabs * s.blocks * s.blocks * 256 * sizeof(float4));
   return s;
@@ -865,7 +898,7 @@ int ou_run_slabs(egnn_ctx* ctx, const OuShape& p, const OuInput<T>& in, const fl
   if (int rc = rt_allow_lds(ctx, (const void*)ou_slab_kernel<T, NB, false>, most, ready)) return rc;
   float4* g[2] = {(float4*)((char*)ws + s.g), (float4*)((char*)ws + s.g + (s.bytes - s.g) / 2)};
   for (int k = 0; k <= steps; ++k) {
-    const OsPlace w{(uint4*)((char*)ws + s.x), g[k & 1], g[(k + 1) & 1], (double*)((char*)ws + s.squares), s.slabs, s.turns};
+    const OsPlace w{(uint4*)((char*)ws + s.x), g[k & 1], g[(k + 1) & 1], (double*)((char*)ws + s.squares), (double*)((char*)ws + s.sigma), s.slabs, s.turns};
     hipLaunchKernelGGL((ou_slab_kernel<T, NB, false>), dim3(s.slabs, p.batch), dim3(64 * OS_WAVES), most, st, p, in, m_old, m_new, w, k, steps,
                        out);
   }
@@ -873,12 +906,13 @@ int ou_run_slabs(egnn_ctx* ctx, const OuShape& p, const OuInput<T>& in, const fl
   return EGNN_OK;
 }
 
-struct OuSpace { size_t part, x, xt, g, bytes; };
+struct OuSpace { size_t part, sigma, x, xt, g, bytes; };
 OuSpace ou_space(const OuShape& p) {
-  if (p.n <= 64) return {0, 0, 0, 0, os_space(p).bytes};
+  if (p.n <= 64) return {0, 0, 0, 0, 0, os_space(p).bytes};
   OuSpace s;
   s.part = 0;
-  s.x = ou_align((size_t)p.batch * OU_PARTS * sizeof(double));
+  s.sigma = ou_align((size_t)p.batch * OU_PARTS * sizeof(double));
+  s.x = s.sigma + ou_align((size_t)p.batch * sizeof(double));
   const size_t x = ou_align((size_t)p.batch * 2 * p.np * p.mp * 2), g = ou_align((size_t)p.batch * 2 * p.np * p.np * 2);
   s.xt = s.x + x;             // twice: a product reads one and writes the other
   s.g = s.xt + 2 * x;         // g and p
@@ -913,9 +947,10 @@ int ou_run(egnn_ctx* ctx, const OuShape& p, const OuInput<T>& in, const float* m
   if (p.n <= 64) return ou_run_slabs<T, 2>(ctx, p, in, m_old, m_new, steps, out, ws, st);
   const OuSpace s = ou_space(p);
   double* part = (double*)((char*)ws + s.part);
+  double* sigma = (double*)((char*)ws + s.sigma);
   _Float16* x = (_Float16*)((char*)ws + s.x);
   _Float16* xt = (_Float16*)((char*)ws + s.xt);
-  _Float16* xt2 = (_Float16*)((char*)ws + s.xt + (s.xt - s.x));
+  _Float16* xt2 = (_Float16*)((char*)ws + s.xt + (s.g - s.xt) / 2);
   _Float16* g = (_Float16*)((char*)ws + s.g);
   _Float16* q = (_Float16*)((char*)ws + s.g + (s.bytes - s.g) / 2);
   const size_t size = (size_t)p.rows * p.cols;
@@ -925,14 +960,14 @@ int ou_run(egnn_ctx* ctx, const OuShape& p, const OuInput<T>& in, const float* m
     hipLaunchKernelGGL((ou_square_kernel<T, 4>), dim3(parts, p.batch), dim3(256), 0, st, in, m_old, m_new, size, part);
   else
     hipLaunchKernelGGL((ou_square_kernel<T, 1>), dim3(parts, p.batch), dim3(256), 0, st, in, m_old, m_new, size, part);
-  hipLaunchKernelGGL((ou_pieces_kernel<T>), dim3(p.mp / 64, p.np / 64, p.batch), dim3(256), 0, st, p, in, part, parts, x, xt);
+  hipLaunchKernelGGL((ou_pieces_kernel<T>), dim3(p.mp / 64, p.np / 64, p.batch), dim3(256), 0, st, p, in, part, parts, sigma, x, xt);
   EGNN_LAUNCH_CHECK(ctx, "orthogonalise");
   const OuOut<float> none{};
   for (int k = 0; k < steps; ++k) {
-    if (int rc = ou_product<float, OU_GRAM>(ctx, p, {x, x, g, nullptr, p.np, p.np, p.mp}, none, st)) return rc;
-    if (int rc = ou_product<float, OU_POLY>(ctx, p, {g, g, q, nullptr, p.np, p.np, p.np}, none, st)) return rc;
-    if (k + 1 == steps) return ou_product<T, OU_LAST>(ctx, p, {q, xt, nullptr, nullptr, p.np, p.mp, p.np}, out, st);
-    if (int rc = ou_product<float, OU_UPDATE>(ctx, p, {q, xt, xt2, x, p.np, p.mp, p.np}, none, st)) return rc;
+    if (int rc = ou_product<float, OU_GRAM>(ctx, p, {x, x, g, nullptr, p.np, p.np, p.mp, sigma, k}, none, st)) return rc;
+    if (int rc = ou_product<float, OU_POLY>(ctx, p, {g, g, q, nullptr, p.np, p.np, p.np, sigma, k}, none, st)) return rc;
+    if (k + 1 == steps) return ou_product<T, OU_LAST>(ctx, p, {q, xt, nullptr, nullptr, p.np, p.mp, p.np, sigma, k}, out, st);
+    if (int rc = ou_product<float, OU_UPDATE>(ctx, p, {q, xt, xt2, x, p.np, p.mp, p.np, sigma, k}, none, st)) return rc;
     _Float16* t = xt; xt = xt2; xt2 = t;
   }
   return EGNN_OK;

@@ -54,3 +54,31 @@ def test_no_farther_off_than_products_in_fp32(m, shape):
     off = lambda y: np.linalg.norm(y.double().cpu().numpy() - want) / np.linalg.norm(want)
     print(shape, "off by %.2e, in fp32 products %.2e" % (off(m.egnn_orthogonalise(g)[0]), off(x)))
     assert off(m.egnn_orthogonalise(g)[0]) <= off(x)
+
+
+@pytest.mark.parametrize("shape", [(2, 16, 16), (2, 40, 60), (2, 20, 700), (1, 900, 64), (2, 150, 100), (1, 500, 900)])
+@pytest.mark.parametrize("scale", [1e-7, 1e-10, 1e-14, 1e-16, 1e-18, 1e-30])
+def test_small_norms_keep_their_accuracy(m, shape, scale):
+    """Far below the 1e-7 that the formula adds to the norm, x is far below 1 and a step multiplies it by a: the roundings are parts of x."""
+    import torch
+    g = torch.from_numpy(random(np.random.default_rng([3, *shape]), *shape) * (scale * 1e3)).float().cuda()
+    want = K.orthogonalise(g.double().cpu().numpy())
+    y = m.egnn_orthogonalise(g)
+    assert np.linalg.norm(y.double().cpu().numpy() - want) <= FULL * np.linalg.norm(want)
+    W, mom = torch.zeros_like(g), torch.zeros_like(g)
+    rW, _ = K.muon_step(0 * want, g.double().cpu().numpy(), 0 * want, 1.0)
+    m.egnn_muon_step(W, g, mom, 1.0)
+    assert np.linalg.norm(W.double().cpu().numpy() - rW) <= 2 * FULL * np.linalg.norm(rW)
+
+
+@pytest.mark.parametrize("shape", [(2, 30, 30), (1, 60, 600), (2, 200, 150), (1, 300, 800)])
+@pytest.mark.parametrize("steps", [12, 20, 32])
+def test_many_steps(m, shape, steps):
+    """The polynomial takes [0.68, 1.21] into itself (its extremes there are 0.6817 and 1.2025) and multiplies smaller values by up to 3.4445 a
+    step: from 12 steps on the singular values lie there.  (Which point of it a value reaches depends on its last bits.)"""
+    import torch
+    g = torch.from_numpy(np.random.default_rng([4, *shape]).standard_normal(shape)).float().cuda()
+    low = np.linalg.svd(g.double().cpu().numpy(), compute_uv=False)
+    assert (low[:, -1] / np.linalg.norm(low, axis=1) * 3.4445 ** 9 > 10).all()
+    s = np.linalg.svd(m.egnn_orthogonalise(g, steps=steps).double().cpu().numpy(), compute_uv=False)
+    assert s.min() > 0.68 and s.max() < 1.203
