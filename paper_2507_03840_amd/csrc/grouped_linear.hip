@@ -121,7 +121,8 @@ __device__ __forceinline__ long gl_row(const GlRows& p, long at) {
 
 // The types on the matrix cores: fp32 as the three bf16 pieces of split_bf16.h (8 + 8 + 8 bits, exact, and of any magnitude: no scaling,
 // so gradients of any size keep their accuracy), whose six leading products are kept (the dropped ones are 2^-24 of the product);
-// half precision and bfloat16 as they are.
+// half precision and bfloat16 as they are.  An infinite value leaves NaN behind its first piece, and so do finite values whose pieces or
+// products overflow: fp32 results that are NaN are made again with the values themselves (gl_again), which leaves NaN only where it belongs.
 typedef _Float16 gl_h8 __attribute__((ext_vector_type(8)));
 typedef float gl_f16v __attribute__((ext_vector_type(16)));
 template <class T> struct GlType {
@@ -225,6 +226,12 @@ __device__ __forceinline__ void gl_cut(const GlType<float>::Raw& r, uint4 (&to)[
   to[1] = make_uint4(m[0], m[1], m[2], m[3]);
   to[2] = make_uint4(l[0], l[1], l[2], l[3]);
 }
+// sum of n products of values a_step and b_step apart
+__device__ __forceinline__ float gl_again(const float* a, long a_step, const float* b, long b_step, long n) {
+  float sum = 0.0f;
+  for (long k = 0; k < n && sum == sum; ++k) sum = __builtin_fmaf(a[k * a_step], b[k * b_step], sum);
+  return sum;
+}
 template <class T>
 __device__ __forceinline__ void gl_add(uint4 r, float (&to)[8]) {
   typedef T vec __attribute__((ext_vector_type(8)));
@@ -281,6 +288,23 @@ struct GlArgs {
   int tiles_j;                    // column tiles
   long chunk;                     // GL_WEIGHTS: rows of a slot at most
 };
+
+// Result j of row `row` of y or dx, and value (i, j) of dW over the rows r0 .. r1 - 1
+template <GlKind KIND>
+__device__ __forceinline__ float gl_again_row(const GlArgs<float>& g, int group, long row, int j) {
+  const float* W = g.b + (size_t)group * g.J * g.K;
+  const float* a = g.a + row * g.a_stride;
+  if (KIND == GL_INPUT) return gl_again(a, 1, W + j, g.J, g.K);
+  return gl_again(a, 1, W + (size_t)j * g.K, 1, g.K) + (g.bias ? g.bias[(size_t)group * g.J + j] : 0.0f);
+}
+__device__ __forceinline__ float gl_again_weight(const GlArgs<float>& g, long r0, long r1, int i, int j) {
+  float sum = 0.0f;
+  for (long r = r0; r < r1 && sum == sum; ++r) {
+    const long row = gl_row(g.rows, r);
+    sum = __builtin_fmaf(g.a[row * g.a_stride + i], g.b[row * g.b_stride + j], sum);
+  }
+  return sum;
+}
 
 // Tile `t` of the rows: group and first row; false past the end.  The tiles of a group start at its first row.
 __device__ __forceinline__ bool gl_find(const GlRows& p, long t, int size, int& group, long& r0, long& r1) {
@@ -595,6 +619,24 @@ __device__ __forceinline__ void gl_tile(const GlArgs<T>& g, long tile, char* sme
           const int i = i0 + wi + 32 * x + 8 * (q >> 2) + 4 * hh + (q & 3), j = j0 + wj + 32 * y + r32;
           if (to && i < g.I && j < g.J) to[(size_t)i * g.J + j] = acc[x][y][q];
         }
+    if constexpr (NP == 3) {
+      bool again = false;
+#pragma unroll
+      for (int x = 0; x < MB; ++x)
+#pragma unroll
+        for (int y = 0; y < NB; ++y)
+#pragma unroll
+          for (int q = 0; q < 16; ++q) again |= acc[x][y][q] != acc[x][y][q];
+      if (to && again)
+#pragma unroll 1
+        for (int k = 0; k < MB * NB * 16; ++k) {
+          const int x = k / (16 * NB), y = k / 16 % NB, q = k & 15;
+          const int i = i0 + wi + 32 * x + 8 * (q >> 2) + 4 * hh + (q & 3), j = j0 + wj + 32 * y + r32;
+          if (i >= g.I || j >= g.J) continue;
+          float* at = to + (size_t)i * g.J + j;
+          if (*at != *at) *at = gl_again_weight(g, r0, r1, i, j);
+        }
+    }
     if (sums) {                  // the threads of a column of pieces
       __syncthreads();
       double* s = reinterpret_cast<double*>(smem);
@@ -648,6 +690,15 @@ __device__ __forceinline__ void gl_tile(const GlArgs<T>& g, long tile, char* sme
 #pragma unroll
       for (int q = 0; q < 8; ++q)
         if (q < valid) to[q] = (T)v[q];
+    }
+    if constexpr (NP == 3) {
+      bool again = false;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) again |= v[q] != v[q];
+      if (again)
+#pragma unroll 1
+        for (int q = 0; q < min(8, valid); ++q)
+          if (to[q] != to[q]) to[q] = gl_again_row<KIND>(g, group, row[e], j + q);
     }
   }
 }
@@ -779,6 +830,19 @@ __global__ __launch_bounds__(256, 2) void gl_lean_rows_kernel(GlArgs<T> g, long 
                 if (j + q < g.J) to[j + q] = (T)t[q];
             }
           }
+        if constexpr (NP == 3) {
+          bool again = false;
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) again |= acc[n][i] != acc[n][i];
+          if (again)
+#pragma unroll 1
+            for (int k = 0; k < NB * 16; ++k) {
+              const int j = 8 * (k >> 2) + 4 * hh + (k & 3);
+              if (j < g.J && to[j] != to[j]) to[j] = gl_again_row<KIND>(g, group, mine, j);
+            }
+        }
       }
     }
   }
@@ -894,8 +958,11 @@ __global__ __launch_bounds__(256, 2) void gl_lean_weights_kernel(GlArgs<T> g) {
     for (int e = tid; e < PART / 2; e += 256) {
       const int l = e & 63, q = (e >> 6) & 7, n = (e >> 9) % NB, m = (e >> 9) / NB;
       const int i = 32 * m + 8 * (2 * half + (q >> 2)) + 4 * (l >> 5) + (q & 3), j = 32 * n + (l & 31);
-      if (i < g.I && j < g.J)
-        g.dW[((size_t)slot * g.I + i) * g.J + j] = (s_part[0][e] + s_part[1][e]) + (s_part[2][e] + s_part[3][e]);
+      if (i >= g.I || j >= g.J) continue;
+      float sum = (s_part[0][e] + s_part[1][e]) + (s_part[2][e] + s_part[3][e]);
+      if constexpr (NP == 3)
+        if (sum != sum) sum = gl_again_weight(g, r0, r1, i, j);
+      g.dW[((size_t)slot * g.I + i) * g.J + j] = sum;
     }
   }
 }

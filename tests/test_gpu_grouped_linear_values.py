@@ -1,0 +1,82 @@
+"""Grouped linear maps on values where pieces and sums can go wrong: infinities and overflow, sums that are exact in fp32, one-signed
+terms.  References in fp64, or equality."""
+import numpy as np
+import pytest
+
+from oracle import block_oracle as K
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def m():
+    from paper_2507_03840_amd import binding as B
+    return B.Egnn(2, 32, 16, 10.0, 200.0)
+
+
+def kinds(terms, axis):
+    """Of sums along the axis: +inf (1), -inf (-1), NaN (2) or finite (0), from their terms."""
+    plus, minus, nan = (f(terms).any(axis) for f in (np.isposinf, np.isneginf, np.isnan))
+    return np.where(nan | (plus & minus), 2, plus.astype(int) - minus.astype(int))
+
+
+def kind(a):
+    return np.where(np.isnan(a), 2, np.isposinf(a).astype(int) - np.isneginf(a).astype(int))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("n,k,out,groups", [(40, 16, 16, 2), (60, 3, 70, 2), (50, 70, 5, 3), (300, 40, 72, 3), (700, 130, 100, 2), (80001, 24, 40, 2), (80001, 5, 40, 1)])
+def test_infinities(m, n, k, out, groups, dtype):
+    """Sums with an infinite term are that infinity, NaN only with both signs, with 0 times infinity or with a NaN: of every result."""
+    import torch
+    rng = np.random.default_rng([1, n, k, out])
+    t = getattr(torch, dtype)
+    key = rng.integers(0, groups, n)
+    ptr, perm = K.group_rows(key, groups)
+    # whole numbers, zeros among them: their lower pieces are zero
+    x, W, dy = (rng.integers(-3, 4, s).astype(np.float64) for s in ((n, k), (groups, out, k), (n, out)))
+    bias = rng.standard_normal((groups, out))
+    for a in (x, dy):
+        for row, bad in zip(rng.integers(0, n, 6), (np.inf, -np.inf, np.inf, np.nan, -np.inf, np.inf)):
+            a[row, rng.integers(a.shape[1])] = bad
+    W[0, rng.integers(out), rng.integers(k)], W[groups - 1, rng.integers(out), rng.integers(k)] = -np.inf, np.inf
+    dev = lambda a, t: torch.from_numpy(np.ascontiguousarray(a)).to(t).cuda()
+    args = dev(x, t), dev(W, t)
+    p, q = dev(ptr, torch.int32), dev(perm, torch.int32)
+    at = lambda a: a.double().cpu().numpy()
+    y = at(m.egnn_grouped_linear(*args, p, perm=q, bias=dev(bias, torch.float32)))
+    dx, dW, db = (at(a) for a in m.egnn_grouped_linear_backward(*args, dev(dy, t), p, perm=q))
+    with np.errstate(all="ignore"):
+        for g in range(groups):
+            rows = perm[ptr[g]:ptr[g + 1]]
+            want_dW = np.zeros((out, k), int)
+            plus, minus, nan = (np.zeros((out, k), bool) for _ in range(3))
+            for b in range(0, len(rows), 4000):
+                r = rows[b:b + 4000]
+                assert np.array_equal(kind(y[r]), kinds(x[r][:, None, :] * W[g][None], 2))
+                assert np.array_equal(kind(dx[r]), kinds(dy[r][:, :, None] * W[g][None], 1))
+                terms = dy[r][:, :, None] * x[r][:, None, :]
+                plus, minus, nan = plus | np.isposinf(terms).any(0), minus | np.isneginf(terms).any(0), nan | np.isnan(terms).any(0)
+                fine = kind(y[r]) == 0
+                want = x[r] @ np.where(np.isfinite(W[g]), W[g], 0.0).T + bias[g]
+                assert np.allclose(np.where(fine, y[r], 0), np.where(fine, want, 0), rtol=2.0 ** -7, atol=1e-3)
+            want_dW = np.where(nan | (plus & minus), 2, plus.astype(int) - minus.astype(int))
+            assert np.array_equal(kind(dW[g]), want_dW)
+            assert np.array_equal(kind(db[g]), kinds(dy[rows], 0))
+
+
+@pytest.mark.parametrize("n,k,out", [(100, 16, 16), (300, 40, 72), (80001, 24, 40)])
+def test_largest_numbers(m, n, k, out):
+    """The largest fp32 numbers, whose first bfloat16 piece rounds to infinity, times small ones are finite; times 2 they are infinite."""
+    import torch
+    most = float(np.finfo(np.float32).max)
+    x, W = torch.full((n, k), 2.0 ** -10, device="cuda"), torch.full((1, out, k), 2.0 ** -10, device="cuda")
+    p = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    x[3, 1], W[0, 5, 0] = most, -most
+    y = m.egnn_grouped_linear(x, W, p)
+    dx, dW, _ = m.egnn_grouped_linear_backward(x, W, torch.full((n, out), 2.0 ** -20, device="cuda"), p)
+    assert torch.isfinite(y).all() and torch.isfinite(dx).all() and torch.isfinite(dW).all()
+    assert abs(float(y[3, 0]) / (most * 2.0 ** -10) - 1) < 1e-6 and abs(float(y[0, 5]) / (-most * 2.0 ** -10) - 1) < 1e-6
+    assert abs(float(dx[0, 0]) / (-most * 2.0 ** -20) - 1) < 1e-6 and abs(float(dW[0, 0, 1]) / (most * 2.0 ** -20) - 1) < 1e-6
+    W[0, 7, 1] = 2.0
+    assert torch.isposinf(m.egnn_grouped_linear(x, W, p)[3, 7])
