@@ -119,8 +119,12 @@ __device__ __forceinline__ long gl_row(const GlRows& p, long at) {
   return p.perm ? min(max((long)p.perm[at], 0l), p.n - 1) : at;
 }
 
-// The types on the matrix cores: fp32 as the three bf16 pieces of split_bf16.h (8 + 8 + 8 bits, exact, and of any magnitude: no scaling,
-// so gradients of any size keep their accuracy), whose six leading products are kept (the dropped ones are 2^-24 of the product);
+// The types on the matrix cores: fp32 as three bf16 pieces, each the rest of the ones before rounded to nearest (8 bits and a sign each: exact, no
+// scaling, so gradients of any size from 2^-112 on keep their accuracy; below, pieces underflow), whose six leading products are kept.  The dropped
+// ones, mid lo and smaller, are at most 2^-24 of the product and of either sign (with pieces cut off instead of rounded they were up to
+// 2^-21 and always of the product's sign).  Long contractions sum the five lesser products apart from hi hi: eight of them at a time are less than
+// half a step of a sum of some thousand terms, and would be rounded away one after the other (rows of 4,096 values from 1 to 2: off by 1.2e-5 with
+// pieces cut off and one sum, 6e-7 rounded and one sum, 3.4e-7 with two; torch in fp32 2.4e-7).
 // half precision and bfloat16 as they are.  An infinite value leaves NaN behind its first piece, and so do finite values whose pieces or
 // products overflow: fp32 results that are NaN are made again with the values themselves (gl_again), which leaves NaN only where it belongs.
 typedef _Float16 gl_h8 __attribute__((ext_vector_type(8)));
@@ -144,16 +148,45 @@ template <class T>
 __device__ __forceinline__ gl_f16v gl_product(const uint4 (&a)[1], const uint4 (&b)[1], gl_f16v c) {
   return gl_mfma(a[0], b[0], c, T());
 }
-template <class T>
-__device__ __forceinline__ gl_f16v gl_product(const uint4 (&a)[3], const uint4 (&b)[3], gl_f16v c) {
+__device__ __forceinline__ gl_f16v gl_lesser(const uint4 (&a)[3], const uint4 (&b)[3], gl_f16v c) {
   const __bf16 t = {};
   c = gl_mfma(a[2], b[0], c, t);
   c = gl_mfma(a[0], b[2], c, t);
   c = gl_mfma(a[1], b[1], c, t);
   c = gl_mfma(a[1], b[0], c, t);
-  c = gl_mfma(a[0], b[1], c, t);
-  return gl_mfma(a[0], b[0], c, t);
+  return gl_mfma(a[0], b[1], c, t);
 }
+template <class T>
+__device__ __forceinline__ gl_f16v gl_product(const uint4 (&a)[3], const uint4 (&b)[3], gl_f16v c) {
+  return gl_mfma(a[0], b[0], gl_lesser(a, b, c), __bf16{});
+}
+__device__ __forceinline__ gl_f16v gl_zero() {
+  gl_f16v v;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+  return v;
+}
+// A sum over a long contraction: fp32's lesser products apart from hi hi
+template <class T>
+struct GlSum {
+  gl_f16v sum = gl_zero();
+  template <class P> __device__ __forceinline__ void add(const P& a, const P& b) { sum = gl_product<T>(a, b, sum); }
+  __device__ __forceinline__ gl_f16v value() const { return sum; }
+};
+template <>
+struct GlSum<float> {
+  gl_f16v sum = gl_zero(), lesser = gl_zero();
+  __device__ __forceinline__ void add(const uint4 (&a)[3], const uint4 (&b)[3]) {
+    lesser = gl_lesser(a, b, lesser);
+    sum = gl_mfma(a[0], b[0], sum, __bf16{});
+  }
+  __device__ __forceinline__ gl_f16v value() const {
+    gl_f16v v;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = sum[i] + lesser[i];
+    return v;
+  }
+};
 
 // Eight values at p, aligned to one value.  Loads are never under a condition: a condition would end in a wait for the load.  At the end of
 // a row the last eight values of the row are taken instead (it has that many, or the row is narrow) and moved down by the places too many.
@@ -210,6 +243,12 @@ __device__ __forceinline__ void gl_shift(GlType<float>::Raw& r, int n) {
   r.a = make_uint4(w[0], w[1], w[2], w[3]);
   r.b = make_uint4(w[4], w[5], w[6], w[7]);
 }
+// two values rounded to bf16
+__device__ __forceinline__ uint32_t gl_round2(float a, float b) {
+  typedef __bf16 pair __attribute__((ext_vector_type(2)));
+  const pair v = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
 // -> pieces
 __device__ __forceinline__ void gl_cut(uint4 r, uint4 (&to)[1]) { to[0] = r; }
 __device__ __forceinline__ void gl_cut(const GlType<float>::Raw& r, uint4 (&to)[3]) {
@@ -217,10 +256,12 @@ __device__ __forceinline__ void gl_cut(const GlType<float>::Raw& r, uint4 (&to)[
   uint32_t h[4], m[4], l[4];
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    const Split3 s0 = split3(__uint_as_float(w[2 * q])), s1 = split3(__uint_as_float(w[2 * q + 1]));
-    h[q] = pack2(s0.hi, s1.hi);
-    m[q] = pack2(s0.mid, s1.mid);
-    l[q] = pack2(s0.lo, s1.lo);
+    float a = __uint_as_float(w[2 * q]), b = __uint_as_float(w[2 * q + 1]);
+    h[q] = gl_round2(a, b);
+    a -= __uint_as_float(h[q] << 16), b -= __uint_as_float(h[q] & 0xffff0000u);
+    m[q] = gl_round2(a, b);
+    a -= __uint_as_float(m[q] << 16), b -= __uint_as_float(m[q] & 0xffff0000u);
+    l[q] = gl_round2(a, b);
   }
   to[0] = make_uint4(h[0], h[1], h[2], h[3]);
   to[1] = make_uint4(m[0], m[1], m[2], m[3]);
@@ -542,13 +583,7 @@ __device__ __forceinline__ void gl_tile(const GlArgs<T>& g, long tile, char* sme
       for (int q = 0; q < 8; ++q) col_sum[q] += (double)turn_sum[q];
   };
 
-  gl_f16v acc[MB][NB];
-#pragma unroll
-  for (int x = 0; x < MB; ++x)
-#pragma unroll
-    for (int y = 0; y < NB; ++y)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[x][y][i] = 0.0f;
+  GlSum<T> total[MB][NB];
   const int wi = (wave >> 1) * (BM / 2), wj = (wave & 1) * (BN / 2);
   auto contract = [&](int k) {
     rb_release_barrier();        // (only LDS is waited for: the next turns' loads stay under way)
@@ -568,7 +603,7 @@ __device__ __forceinline__ void gl_tile(const GlArgs<T>& g, long tile, char* sme
 #pragma unroll
       for (int x = 0; x < MB; ++x)
 #pragma unroll
-        for (int y = 0; y < NB; ++y) acc[x][y] = gl_product<T>(fa[x], fb[y], acc[x][y]);
+        for (int y = 0; y < NB; ++y) total[x][y].add(fa[x], fb[y]);
     }
   };
   // turns k0 .. k1 - 1; their number of loads under way is the same in every turn of the first loop
@@ -608,6 +643,11 @@ __device__ __forceinline__ void gl_tile(const GlArgs<T>& g, long tile, char* sme
   }
 
   // a lane holds column j = lane & 31 of its blocks and four times four neighbouring rows i
+  gl_f16v acc[MB][NB];
+#pragma unroll
+  for (int x = 0; x < MB; ++x)
+#pragma unroll
+    for (int y = 0; y < NB; ++y) acc[x][y] = total[x][y].value();
   if (KIND == GL_WEIGHTS) {
     float* to = g.dW ? g.dW + (size_t)rt * g.I * g.J : nullptr;
 #pragma unroll
@@ -863,13 +903,7 @@ __global__ __launch_bounds__(256, 2) void gl_lean_weights_kernel(GlArgs<T> g) {
   const bool there = gl_slot(g.rows, g.chunk, slot, group, r0, r1);
   if (!there && (g.chunk < g.rows.n || slot >= g.rows.G)) return;
   if (!there) r0 = r1 = 0;                             // one chunk: a group without rows gets its zeros here
-  gl_f16v acc[MB][NB];
-#pragma unroll
-  for (int m = 0; m < MB; ++m)
-#pragma unroll
-    for (int n = 0; n < NB; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[m][n][i] = 0.0f;
+  GlSum<T> total[MB][NB];
   double col_sum[MB] = {};
   int ci[MB], cj[NB];
 #pragma unroll
@@ -931,7 +965,7 @@ __global__ __launch_bounds__(256, 2) void gl_lean_weights_kernel(GlArgs<T> g) {
 #pragma unroll
     for (int m = 0; m < MB; ++m)
 #pragma unroll
-      for (int n = 0; n < NB; ++n) acc[m][n] = gl_product<T>(a[m], b[n], acc[m][n]);
+      for (int n = 0; n < NB; ++n) total[m][n].add(a[m], b[n]);
   }
   if (g.db) {
 #pragma unroll
@@ -944,6 +978,11 @@ __global__ __launch_bounds__(256, 2) void gl_lean_weights_kernel(GlArgs<T> g) {
     }
   }
   if (!g.dW) return;
+  gl_f16v acc[MB][NB];
+#pragma unroll
+  for (int m = 0; m < MB; ++m)
+#pragma unroll
+    for (int n = 0; n < NB; ++n) acc[m][n] = total[m][n].value();
   // half of the values at a time: [register][lane] of every wave
 #pragma unroll
   for (int half = 0; half < 2; ++half) {

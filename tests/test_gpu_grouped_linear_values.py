@@ -80,3 +80,43 @@ def test_largest_numbers(m, n, k, out):
     assert abs(float(dx[0, 0]) / (-most * 2.0 ** -20) - 1) < 1e-6 and abs(float(dW[0, 0, 1]) / (most * 2.0 ** -20) - 1) < 1e-6
     W[0, 7, 1] = 2.0
     assert torch.isposinf(m.egnn_grouped_linear(x, W, p)[3, 7])
+
+
+def one_signed(error, terms, independent):
+    """Relative errors of sums of `terms` numbers from 1 to 4, in steps of 2^-24.  A rounding to nearest at each addition, of at most a step (a
+    third as the root of its mean square, and the sums grow evenly): sqrt(terms) / 3, and 1 for what the products lose and the last rounding.
+    To nearest means of either sign: the mean over many results is 0, up to four times its own spread and a quarter of a step."""
+    e = error.double().flatten() * 2.0 ** 24
+    spread = terms ** 0.5 / 3
+    print("%d terms: mean %.3f, root mean square %.3f of 2^-24" % (terms, e.mean(), e.square().mean() ** 0.5))
+    assert e.square().mean() ** 0.5 <= spread + 1
+    assert abs(e.mean()) <= 0.25 + 4 * spread / independent ** 0.5
+
+
+@pytest.mark.parametrize("n,k,out", [(3000, 16, 16), (3000, 64, 100), (90000, 64, 64), (3000, 512, 100), (3000, 4096, 64)])
+def test_positive_terms(m, n, k, out):
+    """Nothing of a product is left out with its sign, and small parts are not rounded away one after the other."""
+    import torch
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    x, W = torch.rand((n, k), generator=gen, device="cuda") + 1, torch.rand((1, out, k), generator=gen, device="cuda") + 1
+    p = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    want = torch.mm(x.double(), W[0].double().t().contiguous())
+    one_signed(m.egnn_grouped_linear(x, W, p) / want - 1, k, n)
+    back = W.transpose(1, 2).contiguous()            # dx of the transposed matrices is the same product
+    dx = m.egnn_grouped_linear_backward(torch.zeros((n, out), device="cuda"), back, x, p)[0]
+    one_signed(dx / want - 1, k, n)
+
+
+@pytest.mark.parametrize("k,out", [(200, 100), (64, 48)])
+def test_positive_terms_of_a_long_weight_gradient(m, k, out):
+    import torch
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(4)
+    n = 200000
+    x, dy = torch.rand((n, k), generator=gen, device="cuda") + 1, torch.rand((n, out), generator=gen, device="cuda") + 1
+    p = torch.tensor([0, n, n], dtype=torch.int32, device="cuda")
+    _, dW, db = m.egnn_grouped_linear_backward(x, torch.zeros((2, out, k), device="cuda"), dy, p)
+    one_signed(dW[0] / torch.mm(dy.double().t().contiguous(), x.double()) - 1, n, k * out)
+    one_signed(db[0] / dy.double().sum(0) - 1, n, out)
+    assert not dW[1].any() and not db[1].any()
