@@ -1,8 +1,9 @@
-"""The adjoint of the group norm against fp64 (oracle/block_oracle.py and formulas), with bounds that follow each value."""
+"""The group norm and its adjoint against fp64 (oracle/block_oracle.py and formulas), with bounds that follow each value."""
 import numpy as np
 import pytest
 
 from oracle import block_oracle as K
+from tests.group_norm_bounds import CASES, adjoint, forward, inputs
 
 pytestmark = pytest.mark.gpu
 U32 = 2.0 ** -24
@@ -36,3 +37,25 @@ def test_sums_of_equal_terms(m, n, c, segments, dtype):
     print("off by at most %.1f of 2^-24 of n |dy|" % (off.max() / (U32 * n * d)))
     assert (off <= U32 * n * d * (12 * (1 + np.abs(beta)) + 16 * 1.1)).all()
     assert not dgamma.any()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "%dx%d" % c[:2])
+def test_every_value_within_its_own_bound(m, case, dtype):
+    """y and dx against fp64 with bounds that a missing term or a few missing rows break (test_group_norm_bounds.py shows that they do)."""
+    import torch
+    t = getattr(torch, dtype)
+    n, c, groups, ptr = case[:4]
+    x, dy, gamma, beta = inputs(case)
+    x, dy = (torch.from_numpy(a).to(t).cuda() for a in (x, dy))
+    g, b = torch.from_numpy(gamma).cuda(), torch.from_numpy(beta).cuda()
+    p = None if ptr is None else torch.tensor(ptr, dtype=torch.int32, device="cuda")
+    at = lambda a: a.double().cpu().numpy()
+    y, mean, rstd = m.egnn_group_norm(x, groups, g, b, ptr=p)
+    want, bound = forward(case, at(x), gamma, beta, dtype)
+    print("y: %.2f of the bound" % (np.abs(at(y) - want) / bound).max())
+    assert (np.abs(at(y) - want) <= bound).all()
+    dx, _, _ = m.egnn_group_norm_backward(x, dy, mean, rstd, groups, g, b, ptr=p)
+    want, bound, _ = adjoint(case, at(x), at(dy), gamma, beta, dtype)
+    print("dx: %.2f of the bound" % (np.abs(at(dx) - want) / bound).max())
+    assert (np.abs(at(dx) - want) <= bound).all()
