@@ -120,3 +120,28 @@ def test_positive_terms_of_a_long_weight_gradient(m, k, out):
     one_signed(dW[0] / torch.mm(dy.double().t().contiguous(), x.double()) - 1, n, k * out)
     one_signed(db[0] / dy.double().sum(0) - 1, n, out)
     assert not dW[1].any() and not db[1].any()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("n,k,out,groups,empty", [(100003, 9, 50, 2, [0]), (90001, 61, 37, 3, []), (80000, 64, 64, 200, range(0, 200, 7)), (20000, 24, 40, 3, [2]),
+                                                  (2000, 64, 64, 700, []), (30000, 64, 64, 15, []), (6001, 1024, 1000, 2, []), (5000, 512, 384, 3, []),
+                                                  (900, 203, 259, 90, [0, 7, 89]), (20003, 130, 70, 4, [1]), (4097, 3, 200, 2, []), (513, 17, 65, 5, [])])
+def test_exact_sums(m, n, k, out, groups, empty, dtype):
+    """Whole numbers whose products and sums fp32 holds exactly, in any order: dW and db are equal to fp64's, and y and dx to those rounded once,
+    so a row lost or taken twice shows anywhere."""
+    import torch
+    rng = np.random.default_rng([2, n, k, out])
+    t = getattr(torch, dtype)
+    there = [g for g in range(groups) if g not in list(empty)]
+    ptr, perm = K.group_rows(rng.choice(there, n), groups)
+    x, W, dy = (torch.from_numpy(rng.integers(-2, 3, s)).to(t).cuda() for s in ((n, k), (groups, out, k), (n, out)))
+    bias = torch.from_numpy(rng.integers(-9, 10, (groups, out))).float().cuda()
+    p, q = torch.from_numpy(ptr).cuda(), torch.from_numpy(perm).cuda()
+    y = m.egnn_grouped_linear(x, W, p, perm=q, bias=bias)
+    dx, dW, db = m.egnn_grouped_linear_backward(x, W, dy, p, perm=q)
+    for g in range(groups):
+        rows = q[ptr[g]:ptr[g + 1]].long()
+        X, D, V = x[rows].double(), dy[rows].double(), W[g].double()
+        assert torch.equal(y[rows], (torch.mm(X, V.t().contiguous()) + bias[g].double()).to(t))
+        assert torch.equal(dx[rows], torch.mm(D, V).to(t))
+        assert torch.equal(dW[g].double(), torch.mm(D.t().contiguous(), X)) and torch.equal(db[g].double(), D.sum(0))
