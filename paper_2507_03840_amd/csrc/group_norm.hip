@@ -44,7 +44,7 @@ __device__ __forceinline__ long gn_begin(const GnShape& p, int s) { return p.ptr
 __device__ __forceinline__ int gn_first_segment(const GnShape& p, long row) {
   int lo = 0, hi = p.S;
   while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
+    const int mid = lo + ((hi - lo) >> 1);
     if (gn_begin(p, mid + 1) > row) hi = mid; else lo = mid + 1;
   }
   return lo;
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(V == 1 ? 1024 : GN_THREADS) void gn_sums_kernel(GnS
     const T* first = x + sb * x_stride;
     const int run = gn_segment_rows<T, V>(p, x, x_stride, first, b, e, smem);
     for (int g = threadIdx.x; g < p.G; g += blockDim.x) {
-      part[(size_t)(blockIdx.x + s) * p.G + g] = smem[g * run];
+      part[((size_t)blockIdx.x + s) * p.G + g] = smem[g * run];
       if (b == sb) first_of[(size_t)s * p.G + g] = (float)first[g * size];   // (y may be x: kept apart)
     }
     __syncthreads();
@@ -176,7 +176,7 @@ __device__ __forceinline__ void gn_segment_sums(const GnShape& p, const double2*
       double2 t = make_double2(0.0, 0.0);
 #pragma unroll 4
       for (int c = c0 + k; c <= c1; c += rows) {
-        const double2 u = part[(size_t)(c + s) * p.G + g];
+        const double2 u = part[((size_t)c + s) * p.G + g];
         t.x += u.x;
         t.y += u.y;
       }
@@ -199,9 +199,9 @@ __global__ __launch_bounds__(V == 1 ? 1024 : GN_THREADS) void gn_write_kernel(Gn
   const int size = p.C / p.G;
   // segments without rows: the first workgroup writes their zeros
   if (blockIdx.x == 0)
-    for (int s = threadIdx.x; s < p.S; s += blockDim.x)
-      if (gn_begin(p, s) >= gn_begin(p, s + 1))
-        for (int g = 0; g < p.G; ++g) mean[(size_t)s * p.G + g] = rstd[(size_t)s * p.G + g] = 0.0f;
+    for (long s = threadIdx.x; s < p.S; s += blockDim.x)
+      if (gn_begin(p, (int)s) >= gn_begin(p, (int)s + 1))
+        for (int g = 0; g < p.G; ++g) mean[s * p.G + g] = rstd[s * p.G + g] = 0.0f;
   float ga[V], be[V];
 #pragma unroll
   for (int q = 0; q < V; ++q) {
@@ -342,7 +342,7 @@ __global__ __launch_bounds__(V == 1 ? 1024 : GN_THREADS) void gn_adjoint_sums_ke
     if (gn_begin(p, s) >= r1) break;
     if (b >= e) continue;
     gn_adjoint_rows<T, V>(p, w, x, x_stride, dy, dy_stride, s, b, e, ga, be, srow, total, groups);
-    for (int g = threadIdx.x; g < p.G; g += blockDim.x) part[(size_t)(blockIdx.x + s) * p.G + g] = groups[g * size];
+    for (int g = threadIdx.x; g < p.G; g += blockDim.x) part[((size_t)blockIdx.x + s) * p.G + g] = groups[g * size];
     __syncthreads();
   }
   for (int c = threadIdx.x; c < p.C; c += blockDim.x) channel_part[(size_t)blockIdx.x * p.C + c] = make_float2((float)total[c].x, (float)total[c].y);
@@ -459,7 +459,7 @@ GnShape gn_shape(int64_t n, int32_t C, int32_t G, int32_t S, const int32_t* ptr,
 }
 
 // partial sums per slot, channel sums per chunk (element = 4: the most chunks any type gives)
-size_t gn_part_bytes(const GnShape& p) { return gn_align((size_t)(p.chunks + p.S) * p.G * sizeof(double2)); }
+size_t gn_part_bytes(const GnShape& p) { return gn_align(((size_t)p.chunks + p.S) * p.G * sizeof(double2)); }
 size_t gn_first_bytes(const GnShape& p) { return gn_align((size_t)p.S * p.G * sizeof(float)); }
 size_t gn_channel_bytes(const GnShape& p) { return gn_align((size_t)p.chunks * p.C * sizeof(float2)); }
 
