@@ -126,8 +126,16 @@ def _f3(a):
     return (C.c_float * 3)(*[float(v) for v in a])
 
 
+# (a stream's handle without an object for the stream, where this torch has these two)
+_device = getattr(torch._C, "_cuda_getDevice", None)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream():
-    return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))   # of the current stream, without an object for it
+    """Handle of the current stream of the current device."""
+    if _device is None or _raw_stream is None or not torch.cuda.is_initialized():
+        return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return C.c_void_p(_raw_stream(_device()))
 
 
 class Graph:
