@@ -772,16 +772,22 @@ class Egnn:
         return y
 
     def egnn_grouped_linear_backward(self, x, W, dy, ptr, perm=None, dx=None, dW=None, db=None, ws=None):
-        """Adjoint of egnn_grouped_linear; returns (dx, dW, db), dW and db in fp32."""
-        code, n, (groups, n_out, n_in) = self._dtype(x), x.shape[0], W.shape
-        dx = torch.empty((n, n_in), dtype=x.dtype, device=x.device) if dx is None else dx
-        dW = torch.empty((groups, n_out, n_in), dtype=torch.float32, device=x.device) if dW is None else dW
-        db = torch.empty((groups, n_out), dtype=torch.float32, device=x.device) if db is None else db
+        """Adjoint of egnn_grouped_linear; returns (dx, dW, db), dW and db in fp32.  dx, dW or db = False: it is not computed, and None is
+        returned in its place (x may be None where dW is left out)."""
+        code, n, (groups, n_out, n_in) = self._dtype(dy), dy.shape[0], W.shape
+
+        def result(t, shape, dtype):
+            return None if t is False else torch.empty(shape, dtype=dtype, device=dy.device) if t is None else t
+
+        dx, dW, db = result(dx, (n, n_in), dy.dtype), result(dW, W.shape, torch.float32), result(db, (groups, n_out), torch.float32)
+        if x is None and dW is not None:
+            raise ValueError("x is required unless dW is left out")
+        nothing = (None, n_in)
         ws, at, size = self._room(ws, self.lib.egnn_grouped_linear_workspace_bytes, n, groups, n_in, n_out)
         self._check(self.lib.egnn_grouped_linear_backward(
-            self.ctx, code, *_rows(x, n, n_in, x.dtype), _at(W, W.shape, x.dtype), *_rows(dy, n, n_out, x.dtype), n, n_in, n_out,
-            _at(ptr, (groups + 1,), torch.int32), _at(perm, (n,), torch.int32), groups, *_rows(dx, n, n_in, x.dtype), _at(dW, W.shape),
-            _at(db, (groups, n_out)), at, size, _stream()))
+            self.ctx, code, *(nothing if x is None else _rows(x, n, n_in, dy.dtype)), _at(W, W.shape, dy.dtype), *_rows(dy, n, n_out, dy.dtype), n,
+            n_in, n_out, _at(ptr, (groups + 1,), torch.int32), _at(perm, (n,), torch.int32), groups,
+            *(nothing if dx is None else _rows(dx, n, n_in, dy.dtype)), _at(dW, W.shape), _at(db, (groups, n_out)), at, size, _stream()))
         return dx, dW, db
 
     def egnn_orthogonalise_workspace_bytes(self, batch, rows, cols):

@@ -145,3 +145,22 @@ def test_exact_sums(m, n, k, out, groups, empty, dtype):
         assert torch.equal(y[rows], (torch.mm(X, V.t().contiguous()) + bias[g].double()).to(t))
         assert torch.equal(dx[rows], torch.mm(D, V).to(t))
         assert torch.equal(dW[g].double(), torch.mm(D.t().contiguous(), X)) and torch.equal(db[g].double(), D.sum(0))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("n,k,out", [(300, 24, 40), (90000, 64, 64), (700, 200, 140)])
+def test_gradients_left_out(m, n, k, out, dtype):
+    """dx, dW or db = False: the others are the same, and x is not needed without dW."""
+    import torch
+    rng = np.random.default_rng([5, k])
+    t = getattr(torch, dtype)
+    ptr, perm = (torch.from_numpy(a).cuda() for a in K.group_rows(rng.integers(0, 3, n), 3))
+    x, W, dy = (torch.from_numpy(rng.standard_normal(s)).to(t).cuda() for s in ((n, k), (3, out, k), (n, out)))
+    want = m.egnn_grouped_linear_backward(x, W, dy, ptr, perm=perm)
+    for keep in range(7):
+        out_of = {name: None if keep >> i & 1 else False for i, name in enumerate(("dx", "dW", "db"))}
+        got = m.egnn_grouped_linear_backward(x if keep & 2 else None, W, dy, ptr, perm=perm, **out_of)
+        for i, (a, b) in enumerate(zip(got, want)):
+            assert torch.equal(a, b) if keep >> i & 1 else a is None
+    with pytest.raises(ValueError):
+        m.egnn_grouped_linear_backward(None, W, dy, ptr, perm=perm, dx=False)
