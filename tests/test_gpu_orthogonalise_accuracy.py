@@ -82,3 +82,24 @@ def test_many_steps(m, shape, steps):
     assert (low[:, -1] / np.linalg.norm(low, axis=1) * 3.4445 ** 9 > 10).all()
     s = np.linalg.svd(m.egnn_orthogonalise(g, steps=steps).double().cpu().numpy(), compute_uv=False)
     assert s.min() > 0.68 and s.max() < 1.203
+
+
+@pytest.mark.parametrize("shape", [(64, 8, 8), (64, 9, 70), (64, 70, 9), (64, 12, 40), (64, 33, 64), (64, 64, 64), (16, 64, 300), (16, 600, 64), (16, 70, 90),
+                                   (8, 96, 128)])
+def test_small_matrices_as_products_in_fp32(m, shape):
+    """Values in two pieces of 11 bits are off by up to 2^-23 instead of 2^-24, one and a half times as far as fp32 values are in the root of their mean
+    square: over many matrices an update is off by no more than one and a half times what the formula in fp32 is (on the CPU)."""
+    import torch
+    a, b, c = K.COEFFICIENTS
+    g = torch.from_numpy(random(np.random.default_rng([5, *shape]), *shape)).float()
+    want = K.orthogonalise(g.double().numpy())
+    x = g if shape[1] <= shape[2] else g.transpose(1, 2).contiguous()
+    x = x / (x.square().sum((1, 2), keepdim=True).sqrt() + K.EPS_NORM_F)
+    for _ in range(5):
+        p = torch.bmm(x, x.transpose(1, 2).contiguous())
+        x = a * x + torch.bmm(b * p + c * torch.bmm(p, p), x)
+    x = x if shape[1] <= shape[2] else x.transpose(1, 2)
+    off = lambda y: ((np.linalg.norm(y.double().cpu().numpy() - want, axis=(1, 2)) / np.linalg.norm(want, axis=(1, 2))) ** 2).mean() ** 0.5
+    got = off(m.egnn_orthogonalise(g.cuda()))
+    print(shape, "off by %.2e, in fp32 products %.2e" % (got, off(x)))
+    assert got <= 1.5 * off(x)
