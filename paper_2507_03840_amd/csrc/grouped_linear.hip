@@ -1229,7 +1229,7 @@ extern "C" int egnn_grouped_linear_backward(egnn_ctx* ctx, int32_t dtype, const 
   if (!ctx) return EGNN_EINVAL;
   if (int rc = gl_check(ctx, "grouped_linear_backward", dtype, n_rows, n_in, n_out, n_groups, ptr)) return rc;
   if (n_rows > 0 && (!dy || (dx && !W) || (dW && !x))) return egnn_fail(ctx, EGNN_EINVAL, "grouped_linear_backward: null pointer");
-  if (x_stride < n_in || dy_stride < n_out || (dx && dx_stride < n_in))
+  if ((dW && x_stride < n_in) || dy_stride < n_out || (dx && dx_stride < n_in))
     return egnn_fail(ctx, EGNN_EINVAL, "grouped_linear_backward: a row stride below the row's length");
   size_t need = 0;
   egnn_grouped_linear_workspace_bytes(ctx, n_rows, n_groups, n_in, n_out, &need);
