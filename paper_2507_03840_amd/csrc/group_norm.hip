@@ -9,8 +9,10 @@
 // read twice, because the sums of all rows of a segment come before its first result.  The second pass goes through its rows from the last
 // to the first, so that it begins with what the first pass left in the caches.  Where one workgroup takes all rows the two are one launch.
 //
-// Measured: 625,262 x 32 fp32 14 + 27 us forward, 27 + 40 adjoint (80 MB a tensor, read again from the 256 MB cache); 2,350,179 x 64 bf16 75 us (4.0
-// TB/s) + 99 us (6.1 TB/s); 20,000 x 64 fp32 inside [20,000][25][64] in 37 segments 8 + 10 + 10 + 11; 64 x 16 in one launch 4.
+// Measured: 625,262 x 32 fp32 14 + 27 us forward, 27 + 39 adjoint (80 MB a tensor, read again from the 256 MB cache); 2,350,179 x 64 bf16 77 us (3.9
+// TB/s) + 101 us (6.0 TB/s); 20,000 x 64 fp32 inside [20,000][25][64] in 37 segments 9 + 11 + 10 + 11; 64 x 16 in one launch 4.6.  Where
+// tensors are small or segments many, it is not memory: a launch of ragged segments starts with a search of dependent loads for its first
+// segment, and a workgroup takes its segments in turn, each with several barriers (300 structures of one row beside one of 100,000: 810 us).
 //
 // The rows are cut into equal chunks, one workgroup each; segments are ragged and may be shorter or longer than a chunk.
 // A chunk c and a segment s that share rows own the slot c + s of the partial sums: walking along the rows either c or s
@@ -20,12 +22,13 @@
 
 namespace {
 
-constexpr int GN_CHUNKS = 512;        // two workgroups per compute unit; the second pass reads all partial sums of a segment (625,262 x 32 fp32
-                                      // forward 40 us, 2,350,179 x 64 bf16 177; 256 chunks 41 and 187, 1,024 46 and 184)
+constexpr int GN_CHUNKS = 512;        // two workgroups per compute unit; the second pass reads all partial sums of a segment (forward and
+                                      // adjoint of 625,262 x 32 fp32 41 and 65 us, of 2,350,179 x 64 bf16 177 and 297 over and over on one
+                                      // tensor; 256 chunks 41 and 63, 186 and 348; 1,024 47 and 70, 187 and 323)
 constexpr int GN_CHUNK_BYTES = 16384; // a chunk holds at least this much of x, unless its segments are short: below it the launch is longer than
                                       // the reading
 constexpr int GN_ALONE_BYTES = 131072; // up to this much of x, of two segments at most, one workgroup takes all rows (1,000 x 32 fp32
-                                       // 9.8 us alone, 12.1 in two launches; 2,000 x 32 14.8 and 12.2)
+                                       // 9.8 us alone, 12.1 in two launches; 2,000 x 32 14.8 and 11.9)
 constexpr int GN_THREADS = 512;       // 1,024 where a row has more than 512 pieces
 constexpr int GN_ROWS = 4;            // rows of a thread under way at once
 
@@ -446,12 +449,12 @@ GnShape gn_shape(int64_t n, int32_t C, int32_t G, int32_t S, const int32_t* ptr,
   GnShape p;
   p.n = n; p.C = C; p.G = G; p.S = S; p.ptr = ptr;
   long least = (GN_CHUNK_BYTES + (long)C * element - 1) / ((long)C * element);
-  // a workgroup takes its segments one after the other: about two of them each (forward of 1,000 x 32 fp32 in 100 segments 14 us, in one
-  // workgroup 256; 5,000 x 64 in 300 19 us, in chunks of 16 KB 28)
+  // a workgroup takes its segments one after the other: about two of them each (forward of 1,000 x 32 fp32 in 100 segments 15 us, in one
+  // workgroup 256; 5,000 x 64 in 300 20 us, in chunks of 16 KB 28)
   if (S > 1 && 2 * n / S < least) least = 2 * n / S > 0 ? 2 * n / S : 1;
   p.rows = (n + GN_CHUNKS - 1) / GN_CHUNKS;
   if (p.rows < least) p.rows = least;
-  // groups of fewer than four channels keep a sum per value instead of one per thread (325 x 200 fp16 in 200 groups 12 us, alone 18)
+  // groups of fewer than four channels keep a sum per value instead of one per thread (325 x 200 fp16 in 200 groups 13 us, alone 18)
   const double alone = C / G < 4 ? GN_ALONE_BYTES / 4 : GN_ALONE_BYTES;
   if (S <= 2 && (double)n * C * element <= alone) p.rows = n > 0 ? n : 1;
   p.chunks = (int)((n + p.rows - 1) / p.rows);

@@ -449,7 +449,7 @@ __device__ __forceinline__ void gl_units(const GlRows& p, int tiles, int xcd, lo
   last = xcd == 7 ? (long)p.G * tiles : s_unit[1];
 }
 
-// Measured: 20,000 rows 512 to 1,024 in 16 ragged groups, bf16, 21 GFLOP each: forward 53 us, dx 46, dW 64 (330 to 450 TFLOP/s; a tile has 8 to
+// Measured: 20,000 rows 512 to 1,024 in 16 ragged groups, bf16, 21 GFLOP each: forward 54 us, dx 48, dW 64 (330 to 440 TFLOP/s; a tile has 8 to
 // 16 turns, so that its start and end count as much as its products; LDS busy 37 %, without conflicts).
 // 256 threads, four waves, each a quarter of the BM x BN tile in 32 x 32 blocks.  Tiles go from memory to registers DEPTH turns ahead, are cut
 // into pieces on the way to one of two LDS buffers, and are contracted from the other.
@@ -763,8 +763,9 @@ __global__ __launch_bounds__(256) void gl_tile_kernel(GlArgs<T> g) {
 // ---- n_in and n_out of at most 64: the group's matrix stays in registers ------------------------------------------------------
 // A wave takes an equal share of the rows, group by group, 32 at a time, and nothing is shared between waves: no LDS tile, no barrier.  The
 // product is y^T = W x^T, so that a lane holds one row and writes its values four neighbouring ones at a time.  The next rows are under way
-// while the matrix cores work on these; what is left is the memory: 300,000 rows of 64 fp32 by 15 groups take 44 us forward (154 MB, 3.5
-// TB/s), 54 with the transposed matrices of dx.
+// while the matrix cores work on these: 300,000 rows of 64 fp32 by 15 groups take 46 us forward (154 MB, 3.3 TB/s), 56 with the
+// transposed matrices of dx.  At 64 x 64 the three pieces of an fp32 matrix are 192 registers and do not all stay: 22 values a lane are spilled
+// forward and 48 for dx (none of the 16-bit types, none at 32 x 32): half the rate of a copy.
 // KB: contraction steps of 16, NB: output blocks of 32; 16 KB >= K, 32 NB >= J.
 template <class T, GlKind KIND, int KB, int NB, bool NARROW>
 __global__ __launch_bounds__(256, 2) void gl_lean_rows_kernel(GlArgs<T> g, long share) {
@@ -889,7 +890,8 @@ __global__ __launch_bounds__(256, 2) void gl_lean_rows_kernel(GlArgs<T> g, long 
 }
 
 // dW and db of a slot: each wave its own sixteen rows in turn, operands straight from memory (lane = column, eight rows), the waves' sums
-// joined at the end (300,000 rows of 64 and 64 fp32: 50 us for 154 MB, and 6 to join the slots).  MB, NB: blocks of 32 outputs and inputs.
+// joined at the end (300,000 rows of 64 and 64 fp32: 51 us for 154 MB, and 6 to join the slots; its 248 registers allow 512 workgroups at a time,
+// and the 767 slots take one and a half rounds).  MB, NB: blocks of 32 outputs and inputs.
 template <class T, int MB, int NB>
 __global__ __launch_bounds__(256, 2) void gl_lean_weights_kernel(GlArgs<T> g) {
   constexpr int NP = GlType<T>::PIECES, PART = MB * NB * 1024;
@@ -1049,7 +1051,9 @@ size_t gl_align(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Rows of one slot of the weight gradient: enough slots that the launch fills the compute units three times, of at least 256 rows
 // (below that a slot's partial result is longer than what it reads).  Adjoint in us with one, three, six times: 20,000 rows 512 to 256 in 4
-// groups bf16 81, 58, 51; 50,000 of 128 in 15 fp32 73, 79, 90; 300,000 of 64 in 15 fp32 92, 94, 99.
+// groups bf16 77, 58, 50; 300,000 of 64 in 15 groups bf16 51, 47, 54, fp32 83, 88, 95; 50,000 of 128 in 15 fp32 64, 69, 80.  Three times is for
+// the 16-bit types, where few groups of wide matrices need it most; fp32, which loses 5 to 8 % by it, follows the same rule, as the
+// workspace is sized without the type.
 struct GlSplit { long chunk; int slots; size_t weights, bytes; };
 GlSplit gl_split(int64_t n, int G, int K, int N) {
   GlSplit s;
@@ -1078,15 +1082,16 @@ int gl_launch(egnn_ctx* ctx, const GlArgs<T>& g, long tiles, hipStream_t st) {
 }
 
 // Matrices of at most 32 x 32 (one register block) always go the lean way, those of at most 64 x 64 from GL_LEAN_ROWS rows on: with few rows
-// the way to the first product counts (forward us, lean against tiles, 15 groups of 64 x 64: 20,000 rows fp32 13.4 : 7.7, 80,000 24.6 : 22.1,
-// 150,000 29.7 : 35.7, 300,000 42 : 66; bf16 40,000 9.7 : 8.2, 80,000 11.2 : 12.4; 32 x 32: 40,000 fp32 7.7 : 11.4).
+// the way to the first product counts (us forward + adjoint, lean against tiles, 15 groups of 64 x 64 in any order: 20,000 rows fp32 14 + 34 : 9 + 25,
+// 80,000 24 + 48 : 18 + 48, 150,000 30 + 69 : 29 + 72, 300,000 42 + 96 : 52 + 109; bf16 40,000 10 + 26 : 8 + 19, 80,000 11 + 30 : 11 + 27,
+// 150,000 16 + 38 : 16 + 40; 32 x 32: 40,000 fp32 8 + 19 : 9 + 27).  Around 80,000 to 150,000 rows the two are within a tenth of each other.
 constexpr int GL_LEAN_ROWS = 80000;
 bool gl_lean(int64_t n, int K, int N) { return K <= 64 && N <= 64 && ((K <= 32 && N <= 32) || K < 8 || N < 8 || n >= GL_LEAN_ROWS); }
 
 // Tiles of 64 x 64, or of 128 x 128 for 16-bit values where there are enough of those for every compute unit: half the LDS traffic a product, but
-// a quarter of the workgroups (us forward, 128 against 64: 2,000 rows 1,024 to 1,024 in 4 groups 17.8 : 15.2, 5,000 in 8 25.5 : 26.5,
-// 20,000 512 to 1,024 in 16 49 : 57).  fp32 has six products a pair of operands and is not bound by LDS: 64 x 64 is faster at all sizes
-// (128 x 64: 20,000 rows 512 to 1,024 218 : 178, 20,000 of 128 18.9 : 14.6).
+// a quarter of the workgroups (us forward, 128 against 64: 2,000 rows 1,024 to 1,024 in 4 groups 14.6 : 15.8, 5,000 in 8 24.3 : 26.7,
+// 20,000 512 to 1,024 in 16 42 : 49).  fp32 has six products a pair of operands and is not bound by LDS: 64 x 64 is faster at all sizes
+// (128 x 64: 20,000 rows 512 to 1,024 221 : 190, 20,000 of 128 18.0 : 13.7).
 template <class T, GlKind KIND>
 int gl_rows(egnn_ctx* ctx, GlArgs<T> g, hipStream_t st) {
   constexpr int KS = GlType<T>::PIECES == 1 ? 64 : 32;

@@ -442,11 +442,11 @@ __global__ __launch_bounds__((OuTile<TILE>::THREADS)) void ou_product_kernel(OuS
 // is x times the identity: no value ever changes lanes but in the matrix cores.
 // Until step 1 a slab is scaled by its own norm: the sums of squares of the others come with their parts of G, no pass for |u| alone.
 //
-// g g keeps lo lo as well: on its diagonal these are squares, which add up instead of averaging out (8 x 300 to 64 x 64 fp32, against 64
-// bits: 0.63 to 1.2e-6 off with it, 0.67 to 1.4e-6 without, torch in fp32 0.65 to 1.3e-6; 15 x 32 x 32 12.7 us against 12.6).
+// g g keeps lo lo as well: on its diagonal these are squares, which add up instead of averaging out (8 x 8 to 64 x 64 fp32, 30 matrices each, against
+// 64 bits: 0.65 to 0.98e-6 off with it, 0.78 to 1.3e-6 without, torch in fp32 0.64 to 1.1e-6; 15 x 32 x 32 12.7 us against 12.8).
 //
 // What bounds it: the chain of dependent products, conversions and barriers of a step, and the reading of the parts (16 KB a slab from L2).
-// Measured, a step of the optimiser: 15 x 32 x 32 15.5 us in one launch, 3 x 2688 x 64 64 us in six.
+// Measured, a step of the optimiser: 15 x 32 x 32 15.7 us in one launch, 3 x 2688 x 64 65 us in six.
 constexpr int OS_ROWS = 256, OS_WAVES = OS_ROWS / 32;
 constexpr int OS_SLABS = 64;                 // more columns than this many slabs: a workgroup takes several turns
 
@@ -878,8 +878,8 @@ OsSpace os_space(const OuShape& p) {
 
 int ou_parts(size_t size) { return (int)(size > (size_t)OU_PARTS * OU_ROUND ? OU_PARTS : (size + OU_ROUND - 1) / OU_ROUND); }
 
-// Side of at most 32: one block of 32 x 32 holds g, otherwise four do (15 matrices 32 x 32: a step of the optimiser 15.5 us with one, 40 us
-// with four; 3 of 2,000 x 32: 38 and 55).
+// Side of at most 32: one block of 32 x 32 holds g, otherwise four do (15 matrices 32 x 32: a step of the optimiser 15.7 us with one, 42 us
+// with four; 3 of 2,000 x 32: 38 and 57).
 template <class T, int NB>
 int ou_run_slabs(egnn_ctx* ctx, const OuShape& p, const OuInput<T>& in, const float* m_old, float* m_new, int steps,
                  const OuOut<T>& out, void* ws, hipStream_t st) {
@@ -932,7 +932,7 @@ int ou_product_tile(egnn_ctx* ctx, const OuShape& p, const OuOperands& o, const 
 }
 
 // Tiles of 128 where half the compute units get one, else of 64: a wide tile takes half the LDS traffic a product, but four times as long
-// (us a step, 128 against 64: 1 x 768 x 768 fp32 367 : 149, 1 x 1280 x 2048 633 : 515, 2 x 1310 x 1071 529 : 603, 1 x 1536 x 2048 684 : 732).
+// (us a step of the optimiser, 128 against 64: 1 x 768 x 768 369 : 150, 1 x 1280 x 2048 637 : 516, 2 x 1310 x 1071 535 : 605, 1 x 1536 x 2048 689 : 738).
 template <class T, OuProduct WHAT>
 int ou_product(egnn_ctx* ctx, const OuShape& p, const OuOperands& o, const OuOut<T>& out, hipStream_t st) {
   const long wide = (long)((o.I + 127) / 128) * ((o.J + 127) / 128) * p.batch;
