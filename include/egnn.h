@@ -513,6 +513,8 @@ int egnn_unpack_rows(egnn_ctx* ctx, const void* buf, int32_t n_rows, int32_t hal
  * egnn_grouped_linear: y_r = W_g x_r + bias_g for every row r = perm[k], ptr[g] <= k < ptr[g+1].  W [n_groups][n_out][n_in] of the
  *   dtype, bias [n_groups][n_out] fp32 or NULL; perm NULL: row k itself (rows already lie group by group).  Groups may be empty.
  *   Values of ptr and perm outside 0 .. n_rows (- 1) are clamped; rows in no group are left unwritten.  y must not overlap x.
+ *   fp32 sums are as accurate as of fp32 products (values below 2^-112 lose their last bits); an infinite term makes a sum infinite or NaN
+ *   as in plain arithmetic, for every dtype and in the adjoint too.
  * egnn_grouped_linear_backward: dx_r = W_g^T dy_r, dW_g = sum_r dy_r x_r^T (fp32), db_g = sum_r dy_r (fp32); each of dx, dW, db may
  *   be NULL (not computed), all are overwritten (zeros for a group without rows).  x is read for dW only, W for dx only.
  *
