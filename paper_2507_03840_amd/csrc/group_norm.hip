@@ -395,7 +395,8 @@ __global__ __launch_bounds__(V == 1 ? 1024 : GN_THREADS) void gn_adjoint_write_k
     if (ALONE) gn_adjoint_rows<T, V>(p, w, x, x_stride, dy, dy_stride, s, b, e, ga, be, srow, total, groups);
     else gn_segment_sums(p, part, s, groups);
     if (t.rr < t.slots) {
-      float mu[V], rs[V], m1[V], m2[V];
+      float mu[V], rs[V];
+      double m1[V], m2[V];
       const double inv = 1.0 / ((double)(se - sb) * size);
 #pragma unroll
       for (int q = 0; q < V; ++q) {
@@ -403,8 +404,8 @@ __global__ __launch_bounds__(V == 1 ? 1024 : GN_THREADS) void gn_adjoint_write_k
         const size_t at = (size_t)s * p.G + g;
         mu[q] = w.mean[at];
         rs[q] = w.rstd[at];
-        m1[q] = (float)(groups[ALONE ? g * size : g].x * inv);
-        m2[q] = (float)(groups[ALONE ? g * size : g].y * inv);
+        m1[q] = groups[ALONE ? g * size : g].x * inv;
+        m2[q] = groups[ALONE ? g * size : g].y * inv;
       }
       gn_rows_backwards(b, e, t.rr, t.slots, [&](long r, int rows) {
         float v[GN_ROWS][V], d[GN_ROWS][V];
@@ -421,7 +422,7 @@ __global__ __launch_bounds__(V == 1 ? 1024 : GN_THREADS) void gn_adjoint_write_k
           for (int q = 0; q < V; ++q) {
             const float h = (v[k][q] - mu[q]) * rs[q], z = h * ga[q] + be[q], sig = gn_sigmoid(z);
             const float dz = d[k][q] * sig * (1.0f + z * (1.0f - sig));
-            v[k][q] = rs[q] * (ga[q] * dz - m1[q] - h * m2[q]);
+            v[k][q] = rs[q] * (float)((double)ga[q] * dz - m1[q] - (double)h * m2[q]);
           }
           rt_store<T, V>(dx + (r + (long)k * t.slots) * dx_stride + t.l * V, v[k]);
         }

@@ -59,3 +59,20 @@ def test_every_value_within_its_own_bound(m, case, dtype):
     want, bound, _ = adjoint(case, at(x), at(dy), gamma, beta, dtype)
     print("dx: %.2f of the bound" % (np.abs(at(dx) - want) / bound).max())
     assert (np.abs(at(dx) - want) <= bound).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("n,c", [(1, 96), (1, 7), (2, 96), (5, 33), (300, 64), (4000, 20)])
+def test_groups_of_one_value_have_no_gradient(m, n, c, dtype):
+    """A group of one value is its own mean: xhat = 0 and dx = rstd (gamma dz - gamma dz), with rstd = 316.  What the mean of one term is rounded
+    to would be all of the result, and is most of it in groups of two."""
+    import torch
+    rng = np.random.default_rng([6, n, c])
+    t = getattr(torch, dtype)
+    x, dy = (torch.from_numpy(rng.standard_normal((n, c))).to(t).cuda() for _ in range(2))
+    g, b = (torch.from_numpy(rng.standard_normal(c)).float().cuda() for _ in range(2))
+    ptr = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    _, mean, rstd = m.egnn_group_norm(x, c, g, b, ptr=ptr)
+    assert torch.equal(mean, x.float())
+    dx, _, dbeta = m.egnn_group_norm_backward(x, dy, mean, rstd, c, g, b, ptr=ptr)
+    assert not dx.any() and dbeta.all()
