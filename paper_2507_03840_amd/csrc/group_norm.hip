@@ -5,6 +5,7 @@
 //   xhat = (x - mean) rstd, z = gamma_c xhat + beta_c, y = z / (1 + exp(-z)).
 // Adjoint, with dz = dy sig (1 + z (1 - sig)), sig = 1 / (1 + exp(-z)):
 //   dgamma_c = sum_rows dz xhat, dbeta_c = sum_rows dz, dx = rstd (gamma_c dz - mean_g(gamma dz) - xhat mean_g(gamma dz xhat)).
+// (The three terms of dx cancel in small groups, and are all there is of it in groups of one or two values: they are subtracted in fp64.)
 // Both directions are a pass that sums and a pass that writes, one launch each.  What bounds them is memory: x (and dy) are
 // read twice, because the sums of all rows of a segment come before its first result.  The second pass goes through its rows from the last
 // to the first, so that it begins with what the first pass left in the caches.  Where one workgroup takes all rows the two are one launch.
@@ -528,8 +529,8 @@ int gn_backward(egnn_ctx* ctx, const GnShape& p, const GnAdjoint& w, const void*
                        (const T*)dy, (long)dys, (T*)dx, (long)dxs, dgamma, dbeta, (const double2*)nullptr, (const float2*)nullptr);
   } else {
     const size_t slots = (size_t)(p.G > at.threads ? p.G : at.threads) * sizeof(double2);
-    // (eight values a thread and their fp64 sums are 161 registers, for one workgroup per compute unit instead of two: 300,000 x 64 bf16 53.7 us,
-    // with four 48.1)
+    // (eight values a thread and their fp64 sums are 161 registers, for one workgroup per compute unit instead of two: adjoint of 300,000 x 64 bf16
+    // 53.8 us, with four 48.2)
     constexpr int VS = V == 8 ? 4 : V;
     const GnLaunch first = gn_launch(p.C, VS);
     hipLaunchKernelGGL((gn_adjoint_sums_kernel<T, VS>), dim3(p.chunks), dim3(first.threads), gn_adjoint_lds(p.C, first.slots), st, p, w, (const T*)x,
