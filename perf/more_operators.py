@@ -1,0 +1,508 @@
+"""Operators of a residual block in 8 bits and of its training, as cases that can be timed and compared.
+
+A residual block adds what the block before it gave, norms the sum degree by degree, and multiplies by the matrix of the row's
+group; its weights are trained after the gradients' common norm has been limited.  Kinds of case, and what each stands for in real use:
+  norm8         sum with the residual, root-mean-square norm, output in 8 bits with a scale for every 128 channels; inference
+  norm_train    the same with an output in the input's type, and its adjoint
+  quantise      rows to 8 bits with a scale for every 128 columns: what does not come from the norm (hidden layers, gradients)
+  quantise_w    matrices to 8 bits with a scale for every 128 x 128 values, also transposed: after a step of the optimiser
+  linear8       rows in 8 bits times the matrix of their group in 8 bits
+  clip          the norm of all gradients together, and the gradients scaled by what keeps it below a bound
+Rows, channels and degrees are those of the library's configurations (64, 1,000, 3,000 and 12,000 + 8,000 atoms; 16, 32
+and 64 channels; lmax 4; 625,262 and 2,350,179 edges) and generic ones, odd ones among them.
+
+8 bits: e4m3 codes (torch.float8_e4m3fn) of value / 2^e, and 2^e as torch.float8_e8m0fnu; e is the least integer for which the block's
+largest value / 2^e is at most 448, but -127 at least.  Rows of codes begin at multiples of 16 bytes.
+
+With own = False everything is computed with elementary torch operations in 32 bits; exact() restates it in 64 bits.
+"""
+import math
+
+import torch
+
+own = False
+
+EPS = 1e-5
+TINY = 1e-6                    # beside the gradients' norm
+BLOCK = 128
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+SIZES = {"f32": 4, "f16": 2, "bf16": 2}
+
+
+# ----------------------------------------------------------------------------------------------------------- cases
+def _norm(name, rows, channels, lmax=0, dtype="f32", residual=True, train=False):
+    """rows of (lmax + 1)^2 planes of channels"""
+    return dict(name=name, kind="norm_train" if train else "norm8", rows=rows, channels=channels, lmax=lmax, dtype=dtype, residual=residual)
+
+
+def _quantise(name, rows, cols, dtype="f32"):
+    return dict(name=name, kind="quantise", rows=rows, cols=cols, dtype=dtype)
+
+
+def _quantise_w(name, batch, rows, cols, dtype="f32"):
+    return dict(name=name, kind="quantise_w", batch=batch, rows=rows, cols=cols, dtype=dtype)
+
+
+def _linear(name, rows, n_in, n_out, groups=1, lmax=-1, dtype="f32", perm=True):
+    """lmax >= 0: rows is the number of atoms, whose (lmax + 1)^2 rows go by (species, degree): groups = species.  dtype: of the result."""
+    return dict(name=name, kind="linear8", rows=rows, n_in=n_in, n_out=n_out, groups=groups, lmax=lmax, dtype=dtype, perm=perm and groups > 1)
+
+
+def _clip(name, lmax, channels, layers, n_rbf=16, experts=0, n_in=0, n_out=0, matrices=0, dtype="f32", share=0.5):
+    """Gradients of `layers` layers, a readout and `matrices` sets of expert matrices; bound = share of their expected norm."""
+    return dict(name=name, kind="clip", lmax=lmax, channels=channels, layers=layers, n_rbf=n_rbf, experts=experts, n_in=n_in, n_out=n_out,
+                matrices=matrices, dtype=dtype, share=share)
+
+
+def listed():
+    return [
+        # embeddings of a molecule-sized cluster: launches and latency
+        _norm("norm8_64", 64, 16, lmax=2),
+        # scalars of the slab's edge embeddings in half the bytes, inference: the largest
+        _norm("norm8_edges_2350179_bf16", 2350179, 64, dtype="bf16"),
+        # node embeddings of the slab, all degrees, a training step
+        _norm("norm_train_nodes_20000", 20000, 64, lmax=4, train=True),
+        # a wide hidden layer over as many rows, bf16, a training step
+        _norm("norm_train_hidden_bf16", 20000, 1024, dtype="bf16", train=True),
+        # rows of the 12,000 owned atoms on their way back through a map
+        _quantise("quantise_rows_300000", 300000, 64),
+        # matrices of experts after a step, for both directions
+        _quantise_w("quantise_w_experts", 16, 1024, 512),
+        # one row through a wide map: latency, and the weights' bytes
+        _linear("linear8_1", 1, 2048, 4096, dtype="bf16"),
+        # node embeddings of the slab by species and degree
+        _linear("linear8_nodes_12000", 12000, 64, 64, groups=3, lmax=4),
+        # hidden layers of experts, rows in any order
+        _linear("linear8_experts_bf16", 20000, 512, 1024, groups=16, dtype="bf16"),
+        # a wide generic map of many rows: the largest product
+        _linear("linear8_wide_bf16", 8192, 4096, 4096, dtype="bf16"),
+        # gradients of the three-layer network with its readout: many small tensors
+        _clip("clip_network", 4, 32, 3),
+        # expert matrices in fp32 beside the network: more than the caches hold
+        _clip("clip_experts", 4, 64, 3, experts=16, n_in=512, n_out=1024, matrices=12),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(max(lo, hi))))))
+
+
+def draw(rng):
+    kind = rng.choice(("norm8", "norm8", "norm_train", "norm_train", "quantise", "quantise_w", "linear8", "linear8", "linear8", "clip", "clip"))
+    dtype = rng.choice(("f32", "f32", "bf16", "bf16", "f16"))
+    size = SIZES[dtype]
+    if kind.startswith("norm"):
+        lmax = rng.choice((0, 0, 0, 1, 2, 3, 4, 4))
+        channels = _log(rng, 8, 8192) if lmax == 0 else rng.choice((8, 16, 16, 24, 32, 32, 50, 64, 64, 100, 128, 200))
+        if lmax == 0 and rng.random() < 0.7:
+            channels = max(8, channels // 8 * 8)
+        most = 3e8 if kind == "norm8" else 1.2e8
+        rows = _log(rng, 1, most / (channels * (lmax + 1) ** 2 * size))
+        c = _norm("", rows, channels, lmax, dtype, rng.random() < 0.7, kind == "norm_train")
+    elif kind == "quantise":
+        cols = _log(rng, 8, 8192)
+        cols = max(8, cols // 8 * 8) if rng.random() < 0.7 else cols
+        c = _quantise("", _log(rng, 1, 2e8 / (cols * size)), cols, dtype)
+    elif kind == "quantise_w":
+        rows, cols = _log(rng, 8, 4096), _log(rng, 8, 4096)
+        if rng.random() < 0.7:
+            rows, cols = max(8, rows // 8 * 8), max(8, cols // 8 * 8)
+        c = _quantise_w("", _log(rng, 1, min(64.0, 3e7 / (rows * cols))), rows, cols, dtype)
+    elif kind == "linear8":
+        lmax = rng.choice((-1, -1, -1, 2, 3, 4))
+        if lmax < 0:
+            n_in, n_out, groups = _log(rng, 16, 8192), _log(rng, 8, 8192), rng.choice((1, 1, _log(rng, 2, 64)))
+            if rng.random() < 0.7:
+                n_in, n_out = max(16, n_in // 16 * 16), max(8, n_out // 8 * 8)
+            groups = max(1, min(groups, int(3e7 / (n_in * n_out))))
+        else:
+            n_in = n_out = rng.choice((16, 32, 64, 128))
+            groups = rng.choice((1, 2, 3, 4))
+        per = 1 if lmax < 0 else (lmax + 1) ** 2
+        rows = _log(rng, 1, max(2.0, min(8192 * 4096.0 * 4096 / (n_in * n_out), 1.5e8 / (n_in + 4 * n_out)) / per))
+        c = _linear("", rows, n_in, n_out, groups, lmax, dtype, rng.random() < 0.7 or lmax >= 0)
+    else:
+        experts = rng.choice((0, _log(rng, 1, 32)))
+        n_in, n_out = _log(rng, 16, 2048), _log(rng, 16, 2048)
+        matrices = _log(rng, 1, max(1.0, min(16.0, 1e8 / (experts * n_in * n_out)))) if experts else 0
+        if matrices * experts * n_in * n_out > 1e8:
+            experts = 1
+        c = _clip("", rng.randint(0, 4), rng.choice((8, 16, 32, 64)), rng.randint(1, 6), rng.randint(2, 32), experts, n_in if experts else 0,
+                  n_out if experts else 0, matrices, dtype, rng.choice((0.02, 0.5, 0.5, 2.0)))
+    del c["name"]
+    return c
+
+
+# --------------------------------------------------------------------------------------------------------- inputs
+def _gauss(seed, tag, shape, scale=1.0, dtype=torch.float32):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(int(seed) * 1000 + tag)
+    return torch.randn(shape, generator=gen, device="cuda", dtype=torch.float32).mul_(scale).to(dtype)
+
+
+def _degrees(lmax):
+    """Degree of each of the (lmax + 1)^2 planes."""
+    return torch.repeat_interleave(torch.arange(lmax + 1), 2 * torch.arange(lmax + 1) + 1)
+
+
+def _ragged(n, parts):
+    """parts + 1 offsets of n rows, lengths growing from part to part and some odd; the same for every seed."""
+    w = torch.arange(1, parts + 1, dtype=torch.float64) + 0.37 * (torch.arange(parts) % 3)
+    at = torch.floor(torch.cumsum(w, 0) / w.sum() * n).long()
+    at[-1] = n
+    return torch.cat([torch.zeros(1, dtype=torch.long), at])
+
+
+def _sizes(case):
+    """Rows and groups of a product."""
+    if case["lmax"] < 0:
+        return case["rows"], case["groups"]
+    return case["rows"] * (case["lmax"] + 1) ** 2, case["groups"] * (case["lmax"] + 1)
+
+
+def _shapes(case):
+    """Of the gradients: per layer three mixes by degree and the two matrices of the radial network, the readout's, the experts'."""
+    lmax, C, hidden = case["lmax"], case["channels"], 64
+    ls = range(lmax + 1)
+    paths = len([0 for a in ls for b in ls for c in ls if abs(a - b) <= c <= a + b and (a + b + c) % 2 == 0])
+    layer = [(lmax + 1, C, C)] * 3 + [(hidden, case["n_rbf"]), (paths * C, hidden)]
+    readout = [(lmax + 1, C, C)] * 2 + [(hidden, case["n_rbf"]), (paths * C, hidden), (13 * 13, C), (2, C), (C,)]
+    experts = [(case["experts"], case["n_out"], case["n_in"])] * case["matrices"] + [(case["experts"], case["n_out"])] * min(1, case["matrices"])
+    return layer * case["layers"] + readout + experts
+
+
+def _inputs(case, seed):
+    s = dict(case=case)
+    t = TYPES[case["dtype"]]
+    kind = case["kind"]
+    if kind.startswith("norm"):
+        n, C, dim = case["rows"], case["channels"], (case["lmax"] + 1) ** 2
+        shape = (n, dim, C)
+        degree = _degrees(case["lmax"]).cuda()
+        spread = (1.5 / (1.0 + degree.float()))[:, None]           # embeddings of higher degrees are smaller
+        s["x"] = _gauss(seed, 2, shape).mul_(spread).to(t)
+        s["r"] = _gauss(seed, 3, shape).mul_(0.5 * spread).to(t) if case["residual"] else None
+        s["gamma"] = _gauss(seed, 4, (case["lmax"] + 1, C), 0.3).add_(1.0)
+        s["degree"] = degree
+        if kind == "norm_train":
+            s["dy"] = _gauss(seed, 5, shape, 1e-2, t)
+            s["dh"] = _gauss(seed, 6, shape, 1e-2, t) if case["residual"] else None
+    elif kind == "quantise":
+        s["x"] = _gauss(seed, 2, (case["rows"], case["cols"])).mul_(torch.exp(_gauss(seed, 3, (case["rows"], 1)))).to(t)
+    elif kind == "quantise_w":
+        s["W"] = _gauss(seed, 2, (case["batch"], case["rows"], case["cols"]), case["cols"] ** -0.5, t)
+    elif kind == "linear8":
+        n, G = _sizes(case)
+        K, N = case["n_in"], case["n_out"]
+        s["q"], s["qs"] = _codes(_gauss(seed, 2, (n, K)))
+        s["w"], s["ws"] = _codes_of_matrices(_gauss(seed, 3, (G, N, K), K ** -0.5))
+        s["bias"] = _gauss(seed, 4, (G, N), 0.3)
+        s["ptr"] = s["perm"] = None
+        if G > 1:
+            if case["lmax"] < 0:
+                at = _ragged(n, G)
+                key = torch.repeat_interleave(torch.arange(G), at[1:] - at[:-1])
+            else:
+                at = _ragged(case["rows"], case["groups"])
+                species = torch.repeat_interleave(torch.arange(case["groups"]), at[1:] - at[:-1])
+                gen = torch.Generator()
+                gen.manual_seed(int(seed) * 1000 + 1)
+                species = species[torch.randperm(case["rows"], generator=gen)]
+                key = (species[:, None] * (case["lmax"] + 1) + _degrees(case["lmax"])[None, :]).reshape(-1)
+            if case["perm"] and case["lmax"] < 0:
+                gen = torch.Generator()
+                gen.manual_seed(int(seed) * 1000 + 1)
+                key = key[torch.randperm(n, generator=gen)]
+            key = key.cuda()
+            count = torch.bincount(key, minlength=G)
+            s["ptr"] = torch.cat([count.new_zeros(1), torch.cumsum(count, 0)]).to(torch.int32)
+            s["perm"] = torch.sort(key, stable=True).indices.to(torch.int32) if case["perm"] else None
+            s["most"] = int(count.max())
+    else:
+        shapes = _shapes(case)
+        # gradients of unlike sizes, as those of layers at different depths are; matrices in the type, vectors in fp32
+        s["g"] = [_gauss(seed, 10 + i, sh, 1e-3 * 2.0 ** (i % 5), t if len(sh) > 2 else torch.float32) for i, sh in enumerate(shapes)]
+        expected = math.sqrt(sum(math.prod(sh) * (1e-3 * 2.0 ** (i % 5)) ** 2 for i, sh in enumerate(shapes)))
+        s["most"] = case["share"] * expected
+    return s
+
+
+def prepare(case, seed):
+    s = _inputs(case, seed)
+    if own:
+        _keep(case, s)
+    return s
+
+
+def _keep(case, s):
+    """Context, outputs and workspace that a program keeps from call to call."""
+    from paper_2507_03840_amd import binding as B
+    s["lib"] = m = B.Egnn(max(0, case.get("lmax", 0)), 32, 16, 10.0, 200.0)
+    empty = lambda shape, t=torch.float32: torch.empty(shape, dtype=t, device="cuda")
+    kind, t = case["kind"], TYPES[case["dtype"]]
+    if kind.startswith("norm"):
+        n, C, dim = case["rows"], case["channels"], (case["lmax"] + 1) ** 2
+        s["h"] = torch.empty_like(s["x"]) if case["residual"] else None
+        if kind == "norm8":
+            s["q"], s["qs"] = B.empty_codes((n, dim, C))
+        else:
+            s["y"], s["dx"], s["rstd"] = torch.empty_like(s["x"]), torch.empty_like(s["x"]), empty((n, case["lmax"] + 1))
+            s["dgamma"] = torch.empty_like(s["gamma"])
+            s["room"] = empty(max(256, m.egnn_rms_norm_workspace_bytes(n, case["lmax"], C)), torch.uint8)
+    elif kind == "quantise":
+        s["q"], s["qs"] = B.empty_codes((case["rows"], case["cols"]))
+    elif kind == "quantise_w":
+        b, r, c = case["batch"], case["rows"], case["cols"]
+        s["q"], s["qs"] = B.empty_matrix_codes((b, r, c))
+        s["qt"], s["qts"] = B.empty_matrix_codes((b, c, r))
+    elif kind == "linear8":
+        s["y"] = empty((_sizes(case)[0], case["n_out"]), t)
+    else:
+        s["out"] = [torch.empty_like(g) for g in s["g"]]
+        s["list"] = B.TensorList(s["g"], s["out"])
+        s["norm"] = empty((2,))
+        s["room"] = empty(max(256, m.egnn_clip_gradients_workspace_bytes(s["list"])), torch.uint8)
+
+
+# ------------------------------------------------------------------------------------------------------ plain forms
+def _exponents(largest):
+    """e of the blocks' largest values, from the bits of a float: 448 = 0.875 * 2^9."""
+    mantissa, exponent = torch.frexp(largest)
+    e = exponent - 9 + (mantissa > 0.875).to(exponent.dtype)
+    return torch.where(largest > 0, e, torch.full_like(e, -127)).clamp(min=-127)
+
+
+def _blocked(v, dim=-1):
+    """The axis in blocks of 128, the last one filled up with zeros."""
+    n = v.shape[dim]
+    if n > BLOCK and n % BLOCK:
+        shape = list(v.shape)
+        shape[dim] = BLOCK - n % BLOCK
+        v = torch.cat([v, v.new_zeros(shape)], dim)
+    return v.unflatten(dim, (-1, min(n, BLOCK)))
+
+
+def _spread(e, dim, n):
+    """What a block has, for each of its values along an axis of n."""
+    return e.repeat_interleave(min(n, BLOCK), dim).narrow(dim, 0, n)
+
+
+def _scales(e):
+    return (e + 127).to(torch.uint8).view(torch.float8_e8m0fnu)
+
+
+def _pad(q):
+    """Rows of codes from multiples of 16 bytes on."""
+    K = q.shape[-1]
+    if K % 16 == 0:
+        return q.to(torch.float8_e4m3fn)
+    whole = torch.zeros((*q.shape[:-1], (K + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=q.device)
+    whole[..., :K] = q.to(torch.float8_e4m3fn)
+    return whole[..., :K]
+
+
+def _codes(y):
+    """(codes, scales) of rows, a scale for every 128 values."""
+    e = _exponents(_blocked(y.abs()).amax(-1))
+    return _pad(torch.ldexp(y, -_spread(e, -1, y.shape[-1]))), _scales(e)
+
+
+def _codes_of_matrices(W):
+    """(codes, scales) of matrices, a scale for every 128 x 128 values."""
+    e = _exponents(_blocked(_blocked(W.abs()).amax(-1), -2).amax(-2))
+    return _pad(torch.ldexp(W, -_spread(_spread(e, -1, W.shape[-1]), -2, W.shape[-2]))), _scales(e)
+
+
+def _norm_plain(s):
+    case = s["case"]
+    x, degree, lmax = s["x"], s["degree"], case["lmax"]
+    h = x if s["r"] is None else (x.float() + s["r"].float()).to(x.dtype)
+    v = h.float()
+    per = torch.nn.functional.one_hot(degree, lmax + 1).float()                 # planes of each degree
+    per = per / (per.sum(0) * case["channels"])
+    rstd = (v.square().sum(-1) @ per + EPS) ** -0.5
+    gain = s["gamma"][degree]
+    hat = v * rstd[:, degree, None]
+    y = hat * gain
+    out = dict(h=h) if s["r"] is not None else {}
+    if case["kind"] == "norm8":
+        out["q"], out["qs"] = _codes(y)
+        return out
+    dy = s["dy"].float()
+    d = dy * gain
+    along = ((d * hat).sum(-1) @ per)[:, degree, None]
+    dx = rstd[:, degree, None] * (d - hat * along)
+    if s["dh"] is not None:
+        dx = dx + s["dh"].float()
+    dgamma = torch.zeros_like(s["gamma"]).index_add(0, degree, (dy * hat).sum(0))
+    return dict(out, y=y.to(x.dtype), rstd=rstd, dx=dx.to(x.dtype), dgamma=dgamma)
+
+
+def _linear_plain(s):
+    case = s["case"]
+    n, G = _sizes(case)
+    K, N = case["n_in"], case["n_out"]
+    x = s["q"].float() * _spread(s["qs"].float(), -1, K)
+    W = s["w"].float() * _spread(_spread(s["ws"].float(), -1, K), -2, N)
+    if G == 1:
+        return (x @ W[0].t() + s["bias"][0]).to(TYPES[case["dtype"]])
+    at = s["ptr"][:-1, None] + torch.arange(s["most"], device=x.device)          # rows of the groups side by side, short ones filled up
+    there = at < s["ptr"][1:, None]
+    rows = at.clamp(max=n - 1).long()
+    rows = rows if s["perm"] is None else s["perm"].long()[rows]
+    each = torch.bmm(x[rows], W.transpose(1, 2).contiguous()) + s["bias"][:, None]
+    y = torch.empty((n, N), dtype=TYPES[case["dtype"]], device=x.device)
+    y[rows[there]] = each[there].to(y.dtype)
+    return y
+
+
+def _clip_plain(s):
+    norm = torch.cat([g.float().reshape(-1) for g in s["g"]]).square().sum().sqrt()
+    factor = (s["most"] / (norm + TINY)).clamp(max=1.0)
+    return dict(g=[(g.float() * factor).to(g.dtype) for g in s["g"]], norm=torch.stack([norm, factor]))
+
+
+# ------------------------------------------------------------------------------------------------------- operators
+def run(state):
+    s, case = state, state["case"]
+    kind = case["kind"]
+    if not own:
+        if kind.startswith("norm"):
+            return _norm_plain(s)
+        if kind == "quantise":
+            return dict(zip(("q", "qs"), _codes(s["x"].float())))
+        if kind == "quantise_w":
+            W = s["W"].float()
+            return dict(zip(("q", "qs", "qt", "qts"), _codes_of_matrices(W) + _codes_of_matrices(W.transpose(1, 2))))
+        return _linear_plain(s) if kind == "linear8" else _clip_plain(s)
+    m = s["lib"]
+    if kind == "norm8":
+        m.egnn_rms_norm(s["x"], s["gamma"], residual=s["r"], eps=EPS, y=False, h=s["h"], rstd=False, q=s["q"], scale=s["qs"])
+        return dict(dict(h=s["h"]) if case["residual"] else {}, q=s["q"], qs=s["qs"])
+    if kind == "norm_train":
+        m.egnn_rms_norm(s["x"], s["gamma"], residual=s["r"], eps=EPS, y=s["y"], h=s["h"], rstd=s["rstd"])
+        h = s["h"] if case["residual"] else s["x"]
+        m.egnn_rms_norm_backward(h, s["dy"], s["rstd"], s["gamma"], dh=s["dh"], dx=s["dx"], dgamma=s["dgamma"], ws=s["room"])
+        return dict(dict(h=h) if case["residual"] else {}, y=s["y"], rstd=s["rstd"], dx=s["dx"], dgamma=s["dgamma"])
+    if kind == "quantise":
+        m.egnn_quantise_rows(s["x"], q=s["q"], scale=s["qs"])
+        return dict(q=s["q"], qs=s["qs"])
+    if kind == "quantise_w":
+        m.egnn_quantise_matrices(s["W"], q=s["q"], scale=s["qs"], qt=s["qt"], scale_t=s["qts"])
+        return dict(q=s["q"], qs=s["qs"], qt=s["qt"], qts=s["qts"])
+    if kind == "linear8":
+        return m.egnn_scaled_linear(s["q"], s["qs"], s["w"], s["ws"], ptr=s["ptr"], perm=s["perm"], bias=s["bias"], y=s["y"])
+    m.egnn_clip_gradients(s["list"], s["most"], norm=s["norm"], ws=s["room"])
+    return dict(g=s["out"], norm=s["norm"])
+
+
+def work(case):
+    kind, size = case["kind"], SIZES[case["dtype"]]
+    if kind.startswith("norm"):
+        planes = case["rows"] * (case["lmax"] + 1) ** 2
+        n, extra = planes * case["channels"], 2 if case["residual"] else 0
+        if kind == "norm8":
+            return dict(bytes=n * (size * (1 + extra) + 1) + planes * -(-case["channels"] // BLOCK), flops=9 * n)
+        return dict(bytes=n * size * (4 + (3 if extra else 0)), flops=16 * n)
+    if kind == "quantise":
+        return dict(bytes=case["rows"] * (case["cols"] * (size + 1) + -(-case["cols"] // BLOCK)), flops=3 * case["rows"] * case["cols"])
+    if kind == "quantise_w":
+        n = case["batch"] * case["rows"] * case["cols"]
+        return dict(bytes=n * (size + 2), flops=3 * n)
+    if kind == "linear8":
+        n, G = _sizes(case)
+        K, N = case["n_in"], case["n_out"]
+        used = min(n, G)                                            # groups whose matrices are read, at most
+        return dict(bytes=n * (K + -(-K // BLOCK) + N * size) + used * N * (K + 4), flops=2 * n * K * N)
+    shapes = _shapes(case)
+    n = sum(math.prod(sh) for sh in shapes)
+    return dict(bytes=2 * sum(math.prod(sh) * (size if len(sh) > 2 else 4) for sh in shapes), flops=3 * n)
+
+
+# ------------------------------------------------------------------------------------------------------ in 64 bits
+def _codes64(y, blocks, shape):
+    """Values on the scale of their block before they are rounded to 8 bits, and the scales; blocks: number of the block of every value."""
+    count = int(blocks.max()) + 1
+    largest = torch.zeros(count, dtype=torch.float64, device=y.device).scatter_reduce(0, blocks.reshape(-1), y.abs().reshape(-1), "amax")
+    e = torch.ceil(torch.log2(torch.where(largest > 0, largest, torch.ones_like(largest)) / 448.0))
+    e = torch.where(torch.exp2(e - 1.0) * 448.0 >= largest, e - 1.0, e)          # log2 may be a step off beside a power of two
+    e = torch.where(torch.exp2(e) * 448.0 < largest, e + 1.0, e)
+    e = torch.where(largest > 0, e, torch.full_like(e, -127.0)).clamp(min=-127.0)
+    return y / torch.exp2(e)[blocks], torch.exp2(e).reshape(shape)
+
+
+def _row_blocks(rows, cols):
+    per = -(-cols // BLOCK)
+    return torch.arange(rows, device="cuda")[:, None] * per + torch.arange(cols, device="cuda")[None] // BLOCK, per
+
+
+def _matrix_blocks(batch, rows, cols):
+    nr, nc = -(-rows // BLOCK), -(-cols // BLOCK)
+    r, c = torch.arange(rows, device="cuda") // BLOCK, torch.arange(cols, device="cuda") // BLOCK
+    return (torch.arange(batch, device="cuda")[:, None, None] * nr + r[None, :, None]) * nc + c[None, None], nr, nc
+
+
+def _norm64(case, seed):
+    i = _inputs(case, seed)
+    n, C, lmax = case["rows"], case["channels"], case["lmax"]
+    dim = (lmax + 1) ** 2
+    x = i["x"].double()
+    h = x if i["r"] is None else (x + i["r"].double()).to(i["x"].dtype).double()     # the norm is of the sum as it is stored
+    train = case["kind"] == "norm_train"
+    leaf, gamma = h.clone().requires_grad_(train), i["gamma"].double().requires_grad_(train)
+    with torch.set_grad_enabled(train):
+        y, rstd = [], []
+        for l in range(lmax + 1):
+            part = leaf[:, l * l:(l + 1) ** 2]
+            r = 1.0 / torch.sqrt(part.square().mean((1, 2)) + EPS)
+            rstd.append(r)
+            y.append(part * r[:, None, None] * gamma[l])
+        y, rstd = torch.cat(y, 1), torch.stack(rstd, 1)
+    out = dict(h=h) if i["r"] is not None else {}
+    if not train:
+        blocks, per = _row_blocks(n * dim, C)
+        q, qs = _codes64(y.reshape(n * dim, C), blocks, (n, dim, per))
+        return dict(out, q=q.reshape(n, dim, C), qs=qs)
+    dx, dgamma = torch.autograd.grad(y, (leaf, gamma), i["dy"].double())
+    if i["dh"] is not None:
+        dx = dx + i["dh"].double()
+    return dict(out, y=y.detach(), rstd=rstd.detach(), dx=dx, dgamma=dgamma)
+
+
+def _linear64(case, seed):
+    i = _inputs(case, seed)
+    n, G = _sizes(case)
+    K, N = case["n_in"], case["n_out"]
+    blocks, per = _row_blocks(n, K)
+    x = i["q"].double() * i["qs"].double().reshape(-1)[blocks]
+    blocks, _, _ = _matrix_blocks(G, N, K)
+    W = i["w"].double() * i["ws"].double().reshape(-1)[blocks]
+    y = torch.empty((n, N), dtype=torch.float64, device="cuda")
+    at = [0, n] if G == 1 else i["ptr"].tolist()
+    for g in range(G):
+        rows = torch.arange(at[g], at[g + 1], device="cuda")
+        rows = rows if i["perm"] is None else i["perm"][rows].long()
+        y[rows] = torch.addmm(i["bias"][g].double(), x[rows], W[g].t())
+    return y
+
+
+def exact(case, seed):
+    kind = case["kind"]
+    if kind.startswith("norm"):
+        return _norm64(case, seed)
+    if kind == "linear8":
+        return _linear64(case, seed)
+    i = _inputs(case, seed)
+    if kind == "quantise":
+        blocks, per = _row_blocks(case["rows"], case["cols"])
+        q, qs = _codes64(i["x"].double(), blocks, (case["rows"], per))
+        return dict(q=q, qs=qs)
+    if kind == "quantise_w":
+        b, r, c = case["batch"], case["rows"], case["cols"]
+        blocks, nr, nc = _matrix_blocks(b, r, c)
+        q, qs = _codes64(i["W"].double(), blocks, (b, nr, nc))
+        return dict(q=q, qs=qs, qt=q.transpose(1, 2).contiguous(), qts=qs.transpose(1, 2).contiguous())
+    g = [v.double() for v in i["g"]]
+    norm = math.sqrt(sum(float(v.square().sum()) for v in g))
+    factor = min(1.0, i["most"] / (norm + TINY))
+    return dict(g=[v * factor for v in g], norm=torch.tensor([norm, factor], dtype=torch.float64))
