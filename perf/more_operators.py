@@ -246,7 +246,7 @@ def _keep(case, s):
         if kind == "norm8":
             s["q"], s["qs"] = B.empty_codes((n, dim, C))
         else:
-            s["y"], s["dx"], s["rstd"] = torch.empty_like(s["x"]), torch.empty_like(s["x"]), empty((n, case["lmax"] + 1))
+            s["y"], s["dx"] = torch.empty_like(s["x"]), torch.empty_like(s["x"])
             s["dgamma"] = torch.empty_like(s["gamma"])
             s["room"] = empty(max(256, m.egnn_rms_norm_workspace_bytes(n, case["lmax"], C)), torch.uint8)
     elif kind == "quantise":
@@ -335,7 +335,7 @@ def _norm_plain(s):
     if s["dh"] is not None:
         dx = dx + s["dh"].float()
     dgamma = torch.zeros_like(s["gamma"]).index_add(0, degree, (dy * hat).sum(0))
-    return dict(out, y=y.to(x.dtype), rstd=rstd, dx=dx.to(x.dtype), dgamma=dgamma)
+    return dict(out, y=y.to(x.dtype), dx=dx.to(x.dtype), dgamma=dgamma)
 
 
 def _linear_plain(s):
@@ -377,13 +377,13 @@ def run(state):
         return _linear_plain(s) if kind == "linear8" else _clip_plain(s)
     m = s["lib"]
     if kind == "norm8":
-        m.egnn_rms_norm(s["x"], s["gamma"], residual=s["r"], eps=EPS, y=False, h=s["h"], rstd=False, q=s["q"], scale=s["qs"])
+        m.egnn_rms_norm(s["x"], s["gamma"], residual=s["r"], eps=EPS, y=False, h=s["h"], q=s["q"], scale=s["qs"])
         return dict(dict(h=s["h"]) if case["residual"] else {}, q=s["q"], qs=s["qs"])
     if kind == "norm_train":
-        m.egnn_rms_norm(s["x"], s["gamma"], residual=s["r"], eps=EPS, y=s["y"], h=s["h"], rstd=s["rstd"])
+        m.egnn_rms_norm(s["x"], s["gamma"], residual=s["r"], eps=EPS, y=s["y"], h=s["h"])
         h = s["h"] if case["residual"] else s["x"]
-        m.egnn_rms_norm_backward(h, s["dy"], s["rstd"], s["gamma"], dh=s["dh"], dx=s["dx"], dgamma=s["dgamma"], ws=s["room"])
-        return dict(dict(h=h) if case["residual"] else {}, y=s["y"], rstd=s["rstd"], dx=s["dx"], dgamma=s["dgamma"])
+        m.egnn_rms_norm_backward(h, s["dy"], s["gamma"], dh=s["dh"], eps=EPS, dx=s["dx"], dgamma=s["dgamma"], ws=s["room"])
+        return dict(dict(h=h) if case["residual"] else {}, y=s["y"], dx=s["dx"], dgamma=s["dgamma"])
     if kind == "quantise":
         m.egnn_quantise_rows(s["x"], q=s["q"], scale=s["qs"])
         return dict(q=s["q"], qs=s["qs"])
@@ -451,13 +451,12 @@ def _norm64(case, seed):
     train = case["kind"] == "norm_train"
     leaf, gamma = h.clone().requires_grad_(train), i["gamma"].double().requires_grad_(train)
     with torch.set_grad_enabled(train):
-        y, rstd = [], []
+        y = []
         for l in range(lmax + 1):
             part = leaf[:, l * l:(l + 1) ** 2]
             r = 1.0 / torch.sqrt(part.square().mean((1, 2)) + EPS)
-            rstd.append(r)
             y.append(part * r[:, None, None] * gamma[l])
-        y, rstd = torch.cat(y, 1), torch.stack(rstd, 1)
+        y = torch.cat(y, 1)
     out = dict(h=h) if i["r"] is not None else {}
     if not train:
         blocks, per = _row_blocks(n * dim, C)
@@ -466,7 +465,7 @@ def _norm64(case, seed):
     dx, dgamma = torch.autograd.grad(y, (leaf, gamma), i["dy"].double())
     if i["dh"] is not None:
         dx = dx + i["dh"].double()
-    return dict(out, y=y.detach(), rstd=rstd.detach(), dx=dx, dgamma=dgamma)
+    return dict(out, y=y.detach(), dx=dx, dgamma=dgamma)
 
 
 def _linear64(case, seed):
