@@ -556,6 +556,69 @@ int egnn_muon_step(egnn_ctx* ctx, const float* W, const float* g, const float* m
                    float lr, float beta, float weight_decay, int32_t steps, float* W_out, float* m_out, void* ws,
                    size_t ws_bytes, void* stream);
 
+/* ---- a residual block in 8 bits and its training: root-mean-square norm with the residual's addition, quantising, products with scales,
+ *      clipping of the gradients (which norm the layers have, in how many bits their maps run and how steps are limited the paper leaves open) ----
+ * dtype, strides and workspaces as above.  Results do not depend on what else runs; the same inputs give the same bits.
+ *
+ * Codes: uint8 e4m3 (OCP: 4 exponent and 3 mantissa bits, largest value 448, 0x7f and 0xff are NaN), each the value 2^-e rounded to nearest even once,
+ *   and a byte e + 127 (e8m0) for every block of 128 values: e is the least integer for which the block's largest finite magnitude times 2^-e
+ *   is at most 448, but at least -127 (a block of zeros).  Values that are not finite become NaN and do not count for the scale.
+ *   Calls that read scales take bytes 0..254.
+ *   Rows of codes begin at multiples of 16 bytes (*_stride: bytes from one row to the next); the bytes from the last code to the next multiple
+ *   of 16 are zero: the calls that write codes write them, the call that reads codes takes them to be.
+ *   Rows of n_cols codes have ceil(n_cols / 128) scales, contiguous from row to row.  Matrices [batch][rows][cols] of codes (row stride
+ *   q_stride, matrices rows * q_stride apart) have a scale for every 128 x 128 values: [batch][ceil(rows / 128)][ceil(cols / 128)].
+ *
+ * egnn_rms_norm: rows of (lmax + 1)^2 * channels values, planes of channels as in a node tensor (lmax = 0: plain rows).  h = x + r rounded to
+ *   the dtype (r NULL: h is x); for each row and degree l, over its (2 l + 1) channels values,
+ *   y_{l,m,c} = h_{l,m,c} gamma_{l,c} / sqrt(mean h^2 + eps), gamma [lmax + 1][channels].  Outputs: h (NULL: not written; with r only), y of the
+ *   dtype (NULL: not written) and / or y in codes: q has a row for each plane, number row (lmax + 1)^2 + plane, of `channels` codes, and scale
+ *   its scales.  lmax in 0..15, channels in 1..65536.  h or y may be x or r (same stride).  A row with an infinite value of h gives 0 for its
+ *   finite values and NaN for the infinite ones, a row with a NaN all NaN.
+ * egnn_rms_norm_backward: dx = dh + J^T dy with h the sum that the forward call wrote (its x, without a residual) and dh, which may be NULL,
+ *   the gradient that reaches h besides; dx is the gradient of x and of r.  dgamma [lmax + 1][channels].  Both overwritten.  dx may be dy, dh or h
+ *   (same stride).  ws: egnn_rms_norm_workspace_bytes.
+ *
+ * egnn_quantise_rows: x [n_rows][n_cols] to codes and scales.  n_cols in 1..65536.
+ * egnn_quantise_matrices: W [batch][rows][cols] (contiguous) to codes and scales; qt, scale_t (both or neither): those of the transposed
+ *   matrices [batch][cols][rows], the same codes and scales in the other order.
+ * egnn_scaled_linear: y_r = W_g x_r + bias_g for every row r = perm[k], ptr[g] <= k < ptr[g+1], as egnn_grouped_linear, with x [n_rows][n_in]
+ *   and W [n_groups][n_out][n_in] in codes and y of the dtype; ptr NULL: one group of all rows in their order (n_groups 1, perm NULL).
+ *   fp32 and fp16 results: products of codes are exact, sums fp32.  bf16 results: the 8-bit matrix instructions add products eight at a time, cut off at
+ *   2^-13 of the largest of the eight (at most 2^-10 of the terms' magnitudes together; 1.5e-5 of a result's norm on normally distributed
+ *   values), and these sums in fp32.  Results in less than 2^-126 may be zero.  The adjoint is the same call with the codes of dy and
+ *   those of the transposed matrices (dx) and egnn_grouped_linear_backward without dx (dW, db).
+ *
+ * egnn_clip_gradients: norm[0] = sqrt of the sum of the squares of all values of all tensors, norm[1] = min(1, max_norm / (norm[0] + 1e-6)) (both device),
+ *   and every tensor times norm[1], rounded to its dtype, to its `out` (which may be its data).  A norm that is not finite in fp32 leaves
+ *   the values as they are and norm[1] = 0: there is no step to take.  max_norm > 0; infinite: nothing is scaled.  The list is
+ *   read during the call.  What is written must overlap nothing else of the list (EGNN_EINVAL: a tensor that is in it twice).
+ *   ws: egnn_clip_gradients_workspace_bytes, whatever the addresses. */
+typedef struct {
+  const void* data; /* n contiguous values of the dtype, aligned to one */
+  void* out;        /* data or another place */
+  int64_t n;        /* 0..2^40; 0: the addresses are not looked at */
+  int32_t dtype;
+  int32_t reserved;
+} egnn_tensor;
+int egnn_rms_norm(egnn_ctx* ctx, int32_t dtype, const void* x, int64_t x_stride, const void* r, int64_t r_stride, int64_t n_rows,
+                  int32_t lmax, int32_t channels, const float* gamma, float eps, void* h, int64_t h_stride, void* y, int64_t y_stride,
+                  void* q, int64_t q_stride, void* scale, void* stream);
+int egnn_rms_norm_workspace_bytes(const egnn_ctx* ctx, int64_t n_rows, int32_t lmax, int32_t channels, size_t* bytes);
+int egnn_rms_norm_backward(egnn_ctx* ctx, int32_t dtype, const void* h, int64_t h_stride, const void* dy, int64_t dy_stride, const void* dh,
+                           int64_t dh_stride, int64_t n_rows, int32_t lmax, int32_t channels, const float* gamma, float eps, void* dx,
+                           int64_t dx_stride, float* dgamma, void* ws, size_t ws_bytes, void* stream);
+int egnn_quantise_rows(egnn_ctx* ctx, int32_t dtype, const void* x, int64_t x_stride, int64_t n_rows, int32_t n_cols, void* q,
+                       int64_t q_stride, void* scale, void* stream);
+int egnn_quantise_matrices(egnn_ctx* ctx, int32_t dtype, const void* W, int32_t batch, int32_t rows, int32_t cols, void* q, int64_t q_stride,
+                           void* scale, void* qt, int64_t qt_stride, void* scale_t, void* stream);
+int egnn_scaled_linear(egnn_ctx* ctx, const void* q, int64_t q_stride, const void* q_scale, int64_t n_rows, int32_t n_in, int32_t n_out,
+                       const void* w, int64_t w_stride, const void* w_scale, const float* bias, const int32_t* ptr, const int32_t* perm,
+                       int32_t n_groups, int32_t dtype, void* y, int64_t y_stride, void* stream);
+int egnn_clip_gradients_workspace_bytes(const egnn_ctx* ctx, const egnn_tensor* tensors, int32_t n_tensors, size_t* bytes);
+int egnn_clip_gradients(egnn_ctx* ctx, const egnn_tensor* tensors, int32_t n_tensors, float max_norm, float* norm, void* ws, size_t ws_bytes,
+                        void* stream);
+
 /* ---- stage timing (measurement aid; follows the paper's protocol of timing the blocks of the forward
  *      pass separately, Sec. 4.4 / Fig. 6(c)) ----
  * egnn_timing_enable(ctx, max_calls > 0) creates HIP events; from then on every egnn_layer_forward /

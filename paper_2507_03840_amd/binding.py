@@ -36,6 +36,8 @@ SYMBOLS = [
     "egnn_group_norm_workspace_bytes", "egnn_group_norm", "egnn_group_norm_backward", "egnn_group_rows_workspace_bytes", "egnn_group_rows",
     "egnn_grouped_linear_workspace_bytes", "egnn_grouped_linear", "egnn_grouped_linear_backward",
     "egnn_orthogonalise_workspace_bytes", "egnn_orthogonalise", "egnn_muon_step",
+    "egnn_rms_norm", "egnn_rms_norm_workspace_bytes", "egnn_rms_norm_backward", "egnn_quantise_rows", "egnn_quantise_matrices",
+    "egnn_scaled_linear", "egnn_clip_gradients_workspace_bytes", "egnn_clip_gradients",
 ]
 
 DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}   # EGNN_F32, EGNN_F16, EGNN_BF16
@@ -53,6 +55,14 @@ _SIGNATURES = {
     "egnn_orthogonalise_workspace_bytes": "piiip",
     "egnn_orthogonalise": "pipiiiippzp",
     "egnn_muon_step": "ppppiiifffipppzp",
+    "egnn_rms_norm": "piplplliipfplplplpp",
+    "egnn_rms_norm_workspace_bytes": "pliip",
+    "egnn_rms_norm_backward": "piplplplliipfplppzp",
+    "egnn_quantise_rows": "piplliplpp",
+    "egnn_quantise_matrices": "pipiiiplpplpp",
+    "egnn_scaled_linear": "pplpliiplppppiiplp",
+    "egnn_clip_gradients_workspace_bytes": "ppip",
+    "egnn_clip_gradients": "ppifppzp",
 }
 _LETTERS = {"p": C.c_void_p, "i": C.c_int32, "l": C.c_int64, "f": C.c_float, "z": C.c_size_t}
 
@@ -68,6 +78,10 @@ class GraphDesc(C.Structure):
     _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("row_ptr", C.c_void_p), ("shift", C.c_void_p),
                 ("n_edges", C.c_int64), ("n_owned", C.c_int32), ("n_total", C.c_int32),
                 ("w_row", C.c_void_p), ("n_w_rows", C.c_int64), ("len_ptr", C.c_void_p), ("len_perm", C.c_void_p)]
+
+
+class TensorDesc(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
 
 
 class EgnnError(RuntimeError):
@@ -120,6 +134,92 @@ def _rows(t, n, length, dtype):
     if one != 1 and length > 1 or row < length and n > 1:
         raise ValueError(f"rows must be contiguous and must not overlap, not of strides {(row, one)}")
     return t.data_ptr(), max(row, length)
+
+
+def _here(*tensors):
+    """Refuses tensors of another device than the current one, on whose stream the kernels run."""
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+
+
+CODES, SCALES, BLOCK = torch.float8_e4m3fn, torch.float8_e8m0fnu, 128
+
+
+def _blocks(n):
+    return (n + BLOCK - 1) // BLOCK
+
+
+def empty_codes(shape, device="cuda"):
+    """(codes [...][n], scales [...][ceil(n / 128)]) for rows of n values: torch.float8_e4m3fn in rows from multiples of 16 bytes on, and
+    torch.float8_e8m0fnu."""
+    *rows, n = shape
+    return (torch.empty((*rows, (n + 15) // 16 * 16), dtype=CODES, device=device)[..., :n],
+            torch.empty((*rows, _blocks(n)), dtype=SCALES, device=device))
+
+
+def empty_matrix_codes(shape, device="cuda"):
+    """(codes [batch][rows][cols], scales [batch][ceil(rows / 128)][ceil(cols / 128)]) for matrices."""
+    batch, rows, cols = shape
+    return (torch.empty((batch, rows, (cols + 15) // 16 * 16), dtype=CODES, device=device)[..., :cols],
+            torch.empty((batch, _blocks(rows), _blocks(cols)), dtype=SCALES, device=device))
+
+
+def _code_rows(q, scale, shape):
+    """(address, bytes from row to row, address of the scales) of codes of this shape whose rows of the last axis follow one another."""
+    if not (q.is_cuda and q.dtype == CODES and tuple(q.shape) == tuple(shape)):
+        raise ValueError(f"{CODES} device tensor of shape {tuple(shape)} required, not {q.dtype} {tuple(q.shape)} on {q.device}")
+    n, stride = shape[-1], q.stride()
+    row, wide = None, 1                       # of the rows, from the innermost axis with several of them on
+    for size, step in zip(reversed(shape[:-1]), reversed(stride[:-1])):
+        if size == 1:
+            continue
+        row = step if row is None else row
+        if step != row * wide:
+            raise ValueError(f"rows of codes must follow one another, not with strides {stride}")
+        wide *= size
+    row = (n + 15) // 16 * 16 if row is None or 0 in shape[:-1] else row
+    if stride[-1] != 1 and n > 1 or row < n:
+        raise ValueError(f"rows of codes must be contiguous and must not overlap, not of strides {stride}")
+    if n % 16 and q.numel() and q.untyped_storage().nbytes() < q.storage_offset() + (q.numel() // n - 1) * row + (n + 15) // 16 * 16:
+        raise ValueError("the last row of codes has no room up to a multiple of 16 bytes")
+    return q.data_ptr(), row, _at(scale, (*shape[:-1], _blocks(n)), SCALES)
+
+
+def _matrix_code_rows(q, scale, shape):
+    """The same for matrices of codes, which have fewer scales."""
+    batch, rows, cols = shape
+    at, row, _ = _code_rows(q, None, shape)
+    return at, row, _at(scale, (batch, _blocks(rows), _blocks(cols)), SCALES)
+
+
+def _planes(t, shape, dtype):
+    """(address, row stride) of rows of planes of channels; contiguous inside a row."""
+    if t is None:
+        return None, 0
+    n, dim, c = shape
+    if t.dim() == 3 and tuple(t.shape) == tuple(shape) and t.is_cuda and t.dtype == dtype:
+        row, plane, one = t.stride()
+        if (one == 1 or c == 1) and (plane == c or dim == 1) and (row >= dim * c or n <= 1):
+            return t.data_ptr(), max(row, dim * c)
+        raise ValueError(f"rows must be contiguous and must not overlap, not of strides {t.stride()}")
+    raise ValueError(f"{dtype} device tensor of shape {tuple(shape)} required, not {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+class TensorList:
+    """Contiguous device tensors, each with the place its result goes to (itself where `out` is left out), as egnn_clip_gradients takes them.
+    Keeps them alive; made once for tensors that stay where they are."""
+
+    def __init__(self, tensors, out=None):
+        self.tensors, self.out = list(tensors), list(tensors if out is None else out)
+        if len(self.out) != len(self.tensors):
+            raise ValueError(f"{len(self.tensors)} tensors, but {len(self.out)} places for results")
+        self.desc = (TensorDesc * max(1, len(self.tensors)))()
+        for d, t, o in zip(self.desc, self.tensors, self.out):
+            if t.dtype not in DTYPES:
+                raise ValueError(f"float32, float16 or bfloat16 required, not {t.dtype}")
+            d.data, d.out, d.n, d.dtype = _at(t, t.shape, t.dtype), _at(o, t.shape, t.dtype), t.numel(), DTYPES[t.dtype]
+        _here(*self.tensors, *self.out)
 
 
 def _f3(a):
@@ -811,6 +911,106 @@ class Egnn:
             self.ctx, _at(W, W.shape), _at(g, W.shape), _at(momentum, W.shape), batch, rows, cols, lr, beta, weight_decay, steps,
             _at(W_out, W.shape), _at(momentum_out, W.shape), at, size, _stream()))
         return W_out, momentum_out
+
+    # ---- a residual block in 8 bits and its training: root-mean-square norm, codes with scales, clipping
+    def egnn_rms_norm(self, x, gamma, residual=None, eps=1e-5, y=None, h=None, q=False, scale=None):
+        """h = x + residual and its root-mean-square norm by degree; x [n][(lmax + 1)^2][channels], gamma [lmax + 1][channels] (lmax = 0 with x [n][1][channels]).
+        Returns (y, h, q, scale).  y = False: it is not computed.  h = False: the sum is not kept (h is x without a residual).  q = None: y also in
+        codes with their scales, to new tensors; q and scale: to these.  What is not computed is None in the result."""
+        _here(x, gamma, residual, y, h, q, scale)
+        code, shape, (degrees, c) = self._dtype(x), tuple(x.shape), gamma.shape
+        if len(shape) != 3 or shape[1:] != (degrees * degrees, c):
+            raise ValueError(f"x of shape (n, {degrees * degrees}, {c}) required for gamma {tuple(gamma.shape)}, not {shape}")
+        n = shape[0]
+        y = None if y is False else torch.empty(shape, dtype=x.dtype, device=x.device) if y is None else y
+        if residual is None and h is not None and h is not False:
+            raise ValueError("h is the sum with a residual")
+        h = None if h is False or residual is None else torch.empty(shape, dtype=x.dtype, device=x.device) if h is None else h
+        if q is None:
+            q, scale = empty_codes(shape, x.device)
+        q_at, q_row, s_at = (None, 0, None) if q is False else _code_rows(q, scale, shape)
+        if q is not False and scale is None:
+            raise ValueError("codes and scales go together")
+        self._check(self.lib.egnn_rms_norm(
+            self.ctx, code, *_planes(x, shape, x.dtype), *_planes(residual, shape, x.dtype), n, degrees - 1, c, _at(gamma, (degrees, c)), eps,
+            *_planes(h, shape, x.dtype), *_planes(y, shape, x.dtype), q_at, q_row, s_at, _stream()))
+        return y, (x if residual is None else h), (None if q is False else q), (None if q is False else scale)
+
+    def egnn_rms_norm_workspace_bytes(self, n_rows, lmax, channels):
+        return self._bytes(self.lib.egnn_rms_norm_workspace_bytes, n_rows, lmax, channels)
+
+    def egnn_rms_norm_backward(self, h, dy, gamma, dh=None, eps=1e-5, dx=None, dgamma=None, ws=None):
+        """Adjoint of egnn_rms_norm at the h it returned; dh: what reaches h besides.  Returns (dx, dgamma); dx is also the residual's."""
+        _here(h, dy, gamma, dh, dx, dgamma, ws)
+        code, shape, (degrees, c) = self._dtype(h), tuple(h.shape), gamma.shape
+        if len(shape) != 3 or shape[1:] != (degrees * degrees, c):
+            raise ValueError(f"h of shape (n, {degrees * degrees}, {c}) required for gamma {tuple(gamma.shape)}, not {shape}")
+        dx = torch.empty(shape, dtype=h.dtype, device=h.device) if dx is None else dx
+        dgamma = torch.empty((degrees, c), dtype=torch.float32, device=h.device) if dgamma is None else dgamma
+        ws, at, size = self._room(ws, self.lib.egnn_rms_norm_workspace_bytes, shape[0], degrees - 1, c)
+        self._check(self.lib.egnn_rms_norm_backward(
+            self.ctx, code, *_planes(h, shape, h.dtype), *_planes(dy, shape, h.dtype), *_planes(dh, shape, h.dtype), shape[0], degrees - 1, c,
+            _at(gamma, (degrees, c)), eps, *_planes(dx, shape, h.dtype), _at(dgamma, (degrees, c)), at, size, _stream()))
+        return dx, dgamma
+
+    def egnn_quantise_rows(self, x, q=None, scale=None):
+        """Rows x [n][cols] in codes: (q, scale)."""
+        _here(x, q, scale)
+        code, (n, cols) = self._dtype(x), x.shape
+        if (q is None) != (scale is None):
+            raise ValueError("codes and scales go together")
+        q, scale = empty_codes((n, cols), x.device) if q is None else (q, scale)
+        q_at, q_row, s_at = _code_rows(q, scale, (n, cols))
+        self._check(self.lib.egnn_quantise_rows(self.ctx, code, *_rows(x, n, cols, x.dtype), n, cols, q_at, q_row, s_at, _stream()))
+        return q, scale
+
+    def egnn_quantise_matrices(self, W, q=None, scale=None, qt=False, scale_t=None):
+        """Matrices W [batch][rows][cols] in codes: (q, scale, qt, scale_t); qt = None: those of the transposed matrices too, to new tensors; qt
+        and scale_t: to these."""
+        _here(W, q, scale, qt, scale_t)
+        code, (batch, rows, cols) = self._dtype(W), W.shape
+        if (q is None) != (scale is None) or (qt is None or qt is False) != (scale_t is None):
+            raise ValueError("codes and scales go together")
+        q, scale = empty_matrix_codes((batch, rows, cols), W.device) if q is None else (q, scale)
+        if qt is None:
+            qt, scale_t = empty_matrix_codes((batch, cols, rows), W.device)
+        q_at, q_row, s_at = _matrix_code_rows(q, scale, (batch, rows, cols))
+        t_at, t_row, ts_at = (None, 0, None) if qt is False else _matrix_code_rows(qt, scale_t, (batch, cols, rows))
+        self._check(self.lib.egnn_quantise_matrices(self.ctx, code, _at(W, W.shape, W.dtype), batch, rows, cols, q_at, q_row, s_at, t_at, t_row, ts_at,
+                                                    _stream()))
+        return q, scale, (None if qt is False else qt), (None if qt is False else scale_t)
+
+    def egnn_scaled_linear(self, q, scale, w, w_scale, ptr=None, perm=None, bias=None, y=None, dtype=torch.float32):
+        """y = W_g x + bias_g for the rows of every group, x [n][n_in] and W [groups][n_out][n_in] in codes with their scales (rows of codes of more
+        axes are taken as one row after the other); without ptr one group of all rows.  y, or a new tensor of `dtype` [n][n_out]."""
+        _here(q, scale, w, w_scale, ptr, perm, bias, y)
+        groups, n_out, n_in = w.shape
+        q_at, q_row, s_at = _code_rows(q, scale, (*q.shape[:-1], n_in))
+        w_at, w_row, ws_at = _matrix_code_rows(w, w_scale, (groups, n_out, n_in))
+        n = q.numel() // n_in
+        y = torch.empty((n, n_out), dtype=dtype, device=q.device) if y is None else y
+        if s_at is None or ws_at is None:
+            raise ValueError("codes and scales go together")
+        self._check(self.lib.egnn_scaled_linear(
+            self.ctx, q_at, q_row, s_at, n, n_in, n_out, w_at, w_row, ws_at, _at(bias, (groups, n_out)), _at(ptr, (groups + 1,), torch.int32),
+            _at(perm, (n,), torch.int32), groups, self._dtype(y), *_rows(y, n, n_out, y.dtype), _stream()))
+        return y
+
+    def egnn_clip_gradients_workspace_bytes(self, tensors):
+        t = tensors if isinstance(tensors, TensorList) else TensorList(tensors)
+        return self._bytes(self.lib.egnn_clip_gradients_workspace_bytes, C.addressof(t.desc), len(t.tensors))
+
+    def egnn_clip_gradients(self, tensors, max_norm, out=None, norm=None, ws=None):
+        """Gradients (a list of contiguous device tensors, or a TensorList) scaled in place, or to `out`, so that their common norm is at most max_norm;
+        returns norm [2]: the norm before, and the factor (0 where the norm is not finite; nothing is scaled then)."""
+        if isinstance(tensors, TensorList) and out is not None:
+            raise ValueError("a TensorList says itself where results go")
+        t = tensors if isinstance(tensors, TensorList) else TensorList(tensors, out)
+        norm = torch.empty(2, dtype=torch.float32, device="cuda") if norm is None else norm
+        _here(norm, ws)
+        ws, at, size = self._room(ws, self.lib.egnn_clip_gradients_workspace_bytes, C.addressof(t.desc), len(t.tensors))
+        self._check(self.lib.egnn_clip_gradients(self.ctx, C.addressof(t.desc), len(t.tensors), max_norm, _at(norm, (2,)), at, size, _stream()))
+        return norm
 
     # ---- stage timing
     def egnn_timing_enable(self, max_calls):
