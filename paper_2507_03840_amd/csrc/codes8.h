@@ -46,6 +46,35 @@ __device__ __forceinline__ double c8_wave_sum(double v, int lanes) {
   return v;
 }
 
+// Codes of N x V values of one block, which `lanes` neighbouring lanes hold together (lanes a power of two, the same for all of the wave; a lane without
+// values holds zeros): returns the scale byte, v becomes the values on the scale.  What is not finite is looked at apart, where there is any.
+template <int N>
+__device__ __forceinline__ int c8_to_scale(float (&v)[N], int lanes) {
+  unsigned m = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+  if (__any(m >= 0x7f800000u)) {
+    m = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      m = max(m, c8_magnitude(v[i]));
+      v[i] = c8_scaled(v[i], 1.0f);
+    }
+  }
+  const int byte = c8_scale_byte(c8_wave_max(m, lanes));
+  const float inverse = c8_inverse(byte);
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] *= inverse;
+  return byte;
+}
+// V codes to an address of a multiple of V
+template <int V>
+__device__ __forceinline__ void c8_store(uint8_t* q, const float (&v)[V]) {
+  static_assert(V == 4 || V == 8, "a word or two");
+  if constexpr (V == 4) *(unsigned*)q = c8_four(v[0], v[1], v[2], v[3]);
+  else *(uint2*)q = make_uint2(c8_four(v[0], v[1], v[2], v[3]), c8_four(v[4], v[5], v[6], v[7]));
+}
+
 // A block of up to 128 values of one row, two a lane of a whole wave (columns c0 + lane and c0 + 64 + lane of n): codes, zeros up to the next
 // multiple of 16 columns behind the last, and the scale.
 __device__ __forceinline__ void c8_store_block(float v0, float v1, int c0, int n, int lane, uint8_t* q, uint8_t* scale) {

@@ -9,14 +9,25 @@
 // Sums over a row are fp64: squares of any fp32 value stay finite, and the two terms of dx, which cancel in short rows (for one value all but
 // eps rho^2 of them), are subtracted in fp64 from a rho that is made again from h.
 #include "codes8.h"
+#include "row_vectors.h"
 
 namespace {
+
+constexpr int RN_WIDE_ROWS = 1024;    // from so many rows on a wave takes a row of up to 512 vectors, below it a workgroup
+constexpr int RN_THREADS = 256, RN_WAVES = RN_THREADS / 64;
 
 struct RnShape {
   long n;               // rows
   int C, lmax;
   float eps;
+  int lanes;            // of a row, where a wave takes several
 };
+
+// 1 / sqrt(v): the instruction's, made exact to fp64 by a Newton step
+__device__ __forceinline__ double rn_rsqrt(double v) {
+  const double r = __builtin_amdgcn_rsq(v);
+  return r > 0.0 ? r * (1.5 - 0.5 * v * r * r) : r;       // (0 for an infinite v, where the step would be 0 * infinity; NaN stays)
+}
 
 template <class T>
 struct RnForward {
@@ -27,7 +38,116 @@ struct RnForward {
   const float* gamma;
 };
 
-constexpr int RN_WAVES = 4;   // a wave for each (row, degree), so many to a workgroup
+// Sum over the `lanes` lanes of a row, to all of them
+template <bool WIDE>
+__device__ __forceinline__ double rn_row_sum(double v, int lanes, double* lds) {
+  if constexpr (!WIDE) return c8_wave_sum(v, lanes);
+  v = c8_wave_sum(v, 64);
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = lds[0];
+#pragma unroll
+  for (int w = 1; w < RN_WAVES; ++w) v += lds[w];
+  return v;
+}
+
+// U rows at a time of one degree, PL planes each, by `lanes` lanes with NV vectors of a plane each (WIDE: by the workgroup).  All of them are
+// read before anything is written.
+template <class T, bool EVEN, int PL, int U, int NV, bool WIDE>
+__device__ __forceinline__ void rn_write(const RnShape& p, const RnForward<T>& a, int l) {
+  typedef Rv<T, EVEN> R;
+  constexpr int V = R::V, BL = C8_BLOCK / V;
+  __shared__ double lds[RN_WAVES];
+  const int lanes = WIDE ? RN_THREADS : p.lanes, lane = threadIdx.x & (lanes - 1), groups = RN_THREADS / lanes, C = p.C;
+  const int dim = (p.lmax + 1) * (p.lmax + 1), vecs = (C + V - 1) / V, blocks = (C + C8_BLOCK - 1) / C8_BLOCK;
+  const long row0 = (long)blockIdx.x * groups * U + threadIdx.x / lanes;
+  typename R::vec h[U][PL][NV];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int m = 0; m < PL; ++m)
+#pragma unroll
+      for (int k = 0; k < NV; ++k) h[u][m][k] = R::load(a.x + min(row0 + u * groups, p.n - 1) * a.xs + (l * l + m) * C, lane + k * lanes, C);
+  if (a.r) {
+    typename R::vec r[U][PL][NV];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int m = 0; m < PL; ++m)
+#pragma unroll
+        for (int k = 0; k < NV; ++k) r[u][m][k] = R::load(a.r + min(row0 + u * groups, p.n - 1) * a.rs + (l * l + m) * C, lane + k * lanes, C);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int m = 0; m < PL; ++m)
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+          for (int i = 0; i < V; ++i) h[u][m][k][i] = (T)((float)h[u][m][k][i] + (float)r[u][m][k][i]);
+  }
+  float gain[NV][V];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) R::load_floats(a.gamma + l * C, lane + k * lanes, C, gain[k]);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const long row = row0 + u * groups;
+    const bool there = row < p.n;
+    double sum = 0.0;
+#pragma unroll
+    for (int m = 0; m < PL; ++m)
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        if (a.h && there) R::store(a.h + row * a.hs + (l * l + m) * C, lane + k * lanes, C, h[u][m][k]);
+        if (lane + k * lanes < vecs)
+#pragma unroll
+          for (int i = 0; i < V; ++i) sum += (double)(float)h[u][m][k][i] * (double)(float)h[u][m][k][i];
+      }
+    const double rho = rn_rsqrt(rn_row_sum<WIDE>(sum, lanes, lds) / ((double)PL * C) + (double)p.eps);
+    // (a rho that fp32 holds with fewer bits: of rows of more than 2^64)
+    const bool large = rho < 0x1p-64;
+    const float by = (float)(large ? rho * 0x1p64 : rho), down = large ? 0x1p-64f : 1.0f;
+#pragma unroll
+    for (int m = 0; m < PL; ++m)
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int j = lane + k * lanes;
+        float v[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = (float)h[u][m][k][i] * down * by * gain[k][i];
+        if (a.y && there) {
+          typename R::vec y;
+#pragma unroll
+          for (int i = 0; i < V; ++i) y[i] = (T)v[i];
+          R::store(a.y + row * a.ys + (l * l + m) * C, j, C, y);
+        }
+        if (!a.q) continue;
+        const int byte = c8_to_scale(v, WIDE || lanes > BL ? BL : lanes);
+        const long out = row * dim + l * l + m;
+        if (!there) continue;
+        if (j < vecs) c8_store(a.q + out * a.qs + j * V, v);
+        if (j < vecs && j % BL == 0) a.scale[out * blocks + j / BL] = (uint8_t)byte;
+        const float none[V] = {};
+        if (j == 0)
+          for (int c = vecs * V; c < ((C + 15) & ~15); c += V) c8_store(a.q + out * a.qs + c, none);
+      }
+  }
+}
+
+template <class T, bool EVEN, int NV>
+__global__ void __launch_bounds__(RN_THREADS) rn_rows_kernel(RnShape p, RnForward<T> a) { rn_write<T, EVEN, 1, NV == 1 ? 4 : 1, NV, false>(p, a, 0); }
+template <class T, bool EVEN, int NV>
+__global__ void __launch_bounds__(RN_THREADS) rn_wide_kernel(RnShape p, RnForward<T> a) { rn_write<T, EVEN, 1, 1, NV, true>(p, a, 0); }
+// a degree for each blockIdx.y, the longest first
+template <class T, bool EVEN>
+__global__ void __launch_bounds__(RN_THREADS) rn_degrees_kernel(RnShape p, RnForward<T> a) {
+  switch (p.lmax - blockIdx.y) {
+    case 0: rn_write<T, EVEN, 1, 1, 1, false>(p, a, 0); break;
+    case 1: rn_write<T, EVEN, 3, 1, 1, false>(p, a, 1); break;
+    case 2: rn_write<T, EVEN, 5, 1, 1, false>(p, a, 2); break;
+    case 3: rn_write<T, EVEN, 7, 1, 1, false>(p, a, 3); break;
+    default: rn_write<T, EVEN, 9, 1, 1, false>(p, a, 4);
+  }
+}
 
 template <class T>
 __device__ __forceinline__ float rn_sum(const RnForward<T>& a, long row, int at) {
@@ -81,6 +201,130 @@ struct RnAdjoint {
   const float* gamma;
 };
 
+// The rows of a chunk, in the layout of rn_write; the gradient of gamma stays in registers until the last of them.
+template <class T, bool EVEN, int PL, int U, int NV, bool WIDE>
+__device__ __forceinline__ void rn_adjoint(const RnShape& p, const RnAdjoint<T>& a, int l, double* lds) {
+  typedef Rv<T, EVEN> R;
+  constexpr int V = R::V;
+  const int lanes = WIDE ? RN_THREADS : p.lanes, lane = threadIdx.x & (lanes - 1), groups = RN_THREADS / lanes, C = p.C;
+  const int vecs = (C + V - 1) / V;
+  const long begin = (long)blockIdx.x * a.rows, end = min(begin + a.rows, p.n);
+  float gain[NV][V];
+  double dg[NV][V];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    R::load_floats(a.gamma + l * C, lane + k * lanes, C, gain[k]);
+#pragma unroll
+    for (int i = 0; i < V; ++i) dg[k][i] = 0.0;
+  }
+  for (long r0 = begin + threadIdx.x / lanes, turn = begin; turn < end; r0 += groups * U, turn += groups * U) {
+    typename R::vec h[U][PL][NV], dy[U][PL][NV], dh[U][PL][NV];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int m = 0; m < PL; ++m)
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          const long row = min(r0 + u * groups, p.n - 1);
+          h[u][m][k] = R::load(a.h + row * a.hs + (l * l + m) * C, lane + k * lanes, C);
+          dy[u][m][k] = R::load(a.dy + row * a.dys + (l * l + m) * C, lane + k * lanes, C);
+        }
+    if (a.dh) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int m = 0; m < PL; ++m)
+#pragma unroll
+          for (int k = 0; k < NV; ++k) dh[u][m][k] = R::load(a.dh + min(r0 + u * groups, p.n - 1) * a.dhs + (l * l + m) * C, lane + k * lanes, C);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long row = r0 + u * groups;
+      const bool there = row < end;
+      double sum = 0.0, along = 0.0;
+#pragma unroll
+      for (int m = 0; m < PL; ++m)
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+          if (lane + k * lanes < vecs)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+              const double v = (double)(float)h[u][m][k][i];
+              sum += v * v;
+              along += v * (double)((float)dy[u][m][k][i] * gain[k][i]);
+            }
+      sum = rn_row_sum<WIDE>(sum, lanes, lds);
+      if constexpr (WIDE) __syncthreads();
+      along = rn_row_sum<WIDE>(along, lanes, lds);
+      if constexpr (WIDE) __syncthreads();
+      const double rho = rn_rsqrt(sum / ((double)PL * C) + (double)p.eps), back = along / ((double)PL * C) * rho * rho;
+      if (!there) continue;
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int m = 0; m < PL; ++m) {
+          typename R::vec dx;
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            const double v = (double)(float)h[u][m][k][i];
+            const float d = (float)dy[u][m][k][i];
+            dg[k][i] += (double)d * (v * rho);
+            double g = rho * ((double)(d * gain[k][i]) - v * back);
+            if (a.dh) g += (double)(float)dh[u][m][k][i];
+            dx[i] = (T)(float)g;
+          }
+          R::store(a.dx + row * a.dxs + (l * l + m) * C, lane + k * lanes, C, dx);
+        }
+    }
+  }
+  float* out = a.part + ((long)blockIdx.x * (p.lmax + 1) + l) * C;
+  if constexpr (WIDE) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if ((lane + k * lanes) * V + i < C) out[(lane + k * lanes) * V + i] = (float)dg[k][i];
+  } else {
+    const int width = vecs * V;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        for (int at = lanes; at < 64; at <<= 1) dg[k][i] += __shfl_xor(dg[k][i], at);
+        if ((threadIdx.x & 63) < lanes && lane + k * lanes < vecs) lds[(threadIdx.x >> 6) * width + (lane + k * lanes) * V + i] = dg[k][i];
+      }
+    __syncthreads();
+    for (int c = threadIdx.x; c < C; c += RN_THREADS) {
+      double sum = lds[c];
+#pragma unroll
+      for (int w = 1; w < RN_WAVES; ++w) sum += lds[w * width + c];
+      out[c] = (float)sum;
+    }
+  }
+}
+
+template <class T, bool EVEN, int NV>
+__global__ void __launch_bounds__(RN_THREADS) rn_rows_adjoint_kernel(RnShape p, RnAdjoint<T> a) {
+  extern __shared__ double rn_lds[];
+  rn_adjoint<T, EVEN, 1, NV == 1 ? 2 : 1, NV, false>(p, a, 0, rn_lds);
+}
+template <class T, bool EVEN, int NV>
+__global__ void __launch_bounds__(RN_THREADS) rn_wide_adjoint_kernel(RnShape p, RnAdjoint<T> a) {
+  extern __shared__ double rn_lds[];
+  rn_adjoint<T, EVEN, 1, 1, NV, true>(p, a, 0, rn_lds);
+}
+template <class T, bool EVEN>
+__global__ void __launch_bounds__(RN_THREADS) rn_degrees_adjoint_kernel(RnShape p, RnAdjoint<T> a) {
+  extern __shared__ double rn_lds[];
+  switch (p.lmax - blockIdx.y) {
+    case 0: rn_adjoint<T, EVEN, 1, 1, 1, false>(p, a, 0, rn_lds); break;
+    case 1: rn_adjoint<T, EVEN, 3, 1, 1, false>(p, a, 1, rn_lds); break;
+    case 2: rn_adjoint<T, EVEN, 5, 1, 1, false>(p, a, 2, rn_lds); break;
+    case 3: rn_adjoint<T, EVEN, 7, 1, 1, false>(p, a, 3, rn_lds); break;
+    default: rn_adjoint<T, EVEN, 9, 1, 1, false>(p, a, 4, rn_lds);
+  }
+}
+
 // A workgroup for a chunk of rows and a degree: its waves take the rows in turn.  The gradient of gamma is added in LDS a row after the other by
 // the wave whose turn it is.
 template <class T>
@@ -120,21 +364,32 @@ __global__ void __launch_bounds__(RN_WAVES * 64) rn_any_adjoint_kernel(RnShape p
   }
 }
 
-__global__ void rn_join_kernel(const float* part, long chunks, long n, float* out) {
-  const long i = (long)blockIdx.x * blockDim.x + threadIdx.x;
-  if (i >= n) return;
+// Adds the chunks' gradients of gamma: 16 columns a workgroup, each by 16 threads that take the chunks in turn
+__global__ void __launch_bounds__(256) rn_join_kernel(const float* part, int chunks, long n, float* out) {
+  __shared__ double lds[16][17];
+  const long at = (long)blockIdx.x * 16 + (threadIdx.x & 15);
   double sum = 0.0;
-  for (long k = 0; k < chunks; ++k) sum += (double)part[k * n + i];
-  out[i] = (float)sum;
+  if (at < n)
+    for (int k = threadIdx.x >> 4; k < chunks; k += 16) sum += (double)part[k * n + at];
+  lds[threadIdx.x >> 4][threadIdx.x & 15] = sum;
+  __syncthreads();
+  if (threadIdx.x >= 16 || at >= n) return;
+  for (int k = 1; k < 16; ++k) sum += lds[k][threadIdx.x];
+  out[at] = (float)sum;
 }
 
+// Chunks of rows of the adjoint, the same for every type: about 2,048 workgroups, and no fewer than 16,384 values each, so that the chunks' gradients
+// of gamma are a small part of what is read
 struct RnSplit { long rows; int chunks; size_t bytes; };
 RnSplit rn_split(int64_t n, int lmax, int C) {
   RnSplit s;
-  s.rows = (n + 511) / 512;
-  if (s.rows < RN_WAVES) s.rows = RN_WAVES;
+  const long target = 2048 / (lmax + 1), least = 16384 / ((long)C * (lmax + 1));
+  s.rows = (n + target - 1) / target;
+  if (s.rows < least) s.rows = least;
+  s.rows = s.rows < 16 ? s.rows : (s.rows + 15) / 16 * 16;
+  if (s.rows < 1) s.rows = 1;
   s.chunks = n ? (int)((n + s.rows - 1) / s.rows) : 1;
-  s.bytes = (size_t)s.chunks * (lmax + 1) * C * sizeof(float);
+  s.bytes = s.chunks > 1 ? (size_t)s.chunks * (lmax + 1) * C * sizeof(float) : 0;
   return s;
 }
 
@@ -148,19 +403,85 @@ int rn_check(egnn_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32_t l
   return EGNN_OK;
 }
 
+// Lanes of a row: the least power of two with a vector of a plane each, or a wave
+int rn_lanes(int vecs) {
+  int lanes = 1;
+  while (lanes < vecs && lanes < 64) lanes *= 2;
+  return lanes;
+}
+
+template <class T, bool EVEN>
+bool rn_forward_vectors(const RnShape& p, const RnForward<T>& a, int vecs, hipStream_t st) {
+  auto rows = [&](int groups) { return dim3((unsigned)((p.n + groups - 1) / groups), p.lmax + 1); };
+  const dim3 block(RN_THREADS);
+  const int groups = RN_THREADS / p.lanes;
+  if (p.lmax) {
+    if (p.lmax > 4 || vecs > 64) return false;
+    hipLaunchKernelGGL((rn_degrees_kernel<T, EVEN>), rows(groups), block, 0, st, p, a);
+  } else if (vecs <= 64) {
+    hipLaunchKernelGGL((rn_rows_kernel<T, EVEN, 1>), rows(groups * 4), block, 0, st, p, a);
+  } else if (vecs <= 512 && p.n >= RN_WIDE_ROWS) {
+    if (vecs <= 128) hipLaunchKernelGGL((rn_rows_kernel<T, EVEN, 2>), rows(groups), block, 0, st, p, a);
+    else if (vecs <= 256) hipLaunchKernelGGL((rn_rows_kernel<T, EVEN, 4>), rows(groups), block, 0, st, p, a);
+    else hipLaunchKernelGGL((rn_rows_kernel<T, EVEN, 8>), rows(groups), block, 0, st, p, a);
+  } else if (vecs <= 2 * RN_THREADS) {
+    hipLaunchKernelGGL((rn_wide_kernel<T, EVEN, 2>), rows(1), block, 0, st, p, a);
+  } else if (vecs <= 8 * RN_THREADS) {
+    hipLaunchKernelGGL((rn_wide_kernel<T, EVEN, 8>), rows(1), block, 0, st, p, a);
+  } else {
+    return false;
+  }
+  return true;
+}
+
 template <class T>
-int rn_forward(egnn_ctx* ctx, const RnShape& p, const RnForward<T>& a, hipStream_t st) {
-  const long items = p.n * (p.lmax + 1);
-  hipLaunchKernelGGL(rn_any_kernel<T>, dim3((unsigned)((items + RN_WAVES - 1) / RN_WAVES)), dim3(RN_WAVES * 64), 0, st, p, a);
+int rn_forward(egnn_ctx* ctx, RnShape p, const RnForward<T>& a, hipStream_t st) {
+  const int vecs = (p.C + RvWidth<T>::V - 1) / RvWidth<T>::V, size = sizeof(T);
+  p.lanes = rn_lanes(vecs);
+  const bool even = p.C % RvWidth<T>::V == 0 && rv_aligned({a.x, a.r, a.h, a.y, a.gamma}, {a.xs * size, a.r ? a.rs * size : 0, a.h ? a.hs * size : 0, a.y ? a.ys * size : 0});
+  if (!(even ? rn_forward_vectors<T, true>(p, a, vecs, st) : rn_forward_vectors<T, false>(p, a, vecs, st))) {
+    const long items = p.n * (p.lmax + 1);
+    hipLaunchKernelGGL(rn_any_kernel<T>, dim3((unsigned)((items + RN_WAVES - 1) / RN_WAVES)), dim3(RN_THREADS), 0, st, p, a);
+  }
   EGNN_LAUNCH_CHECK(ctx, "rms_norm");
   return EGNN_OK;
 }
 
+template <class T, bool EVEN>
+bool rn_backward_vectors(const RnShape& p, const RnAdjoint<T>& a, int vecs, int chunks, hipStream_t st) {
+  constexpr int V = RvWidth<T>::V;
+  const dim3 grid(chunks, p.lmax + 1), block(RN_THREADS);
+  const size_t lds = (size_t)RN_WAVES * vecs * V * sizeof(double);
+  if (p.lmax) {
+    if (p.lmax > 4 || vecs > 64) return false;
+    hipLaunchKernelGGL((rn_degrees_adjoint_kernel<T, EVEN>), grid, block, lds, st, p, a);
+  } else if (vecs <= 64) {
+    hipLaunchKernelGGL((rn_rows_adjoint_kernel<T, EVEN, 1>), grid, block, lds, st, p, a);
+  } else if (vecs <= 128) {
+    hipLaunchKernelGGL((rn_rows_adjoint_kernel<T, EVEN, 2>), grid, block, lds, st, p, a);
+  } else if (vecs <= 2 * RN_THREADS) {
+    hipLaunchKernelGGL((rn_wide_adjoint_kernel<T, EVEN, 2>), grid, block, RN_WAVES * sizeof(double), st, p, a);
+  } else if (vecs <= 4 * RN_THREADS) {
+    hipLaunchKernelGGL((rn_wide_adjoint_kernel<T, EVEN, 4>), grid, block, RN_WAVES * sizeof(double), st, p, a);
+  } else if (V == 4 && vecs <= 8 * RN_THREADS) {
+    if constexpr (V == 4) hipLaunchKernelGGL((rn_wide_adjoint_kernel<T, EVEN, 8>), grid, block, RN_WAVES * sizeof(double), st, p, a);
+  } else {
+    return false;
+  }
+  return true;
+}
+
 template <class T>
-int rn_backward(egnn_ctx* ctx, const RnShape& p, const RnAdjoint<T>& a, const RnSplit& s, float* dgamma, hipStream_t st) {
+int rn_backward(egnn_ctx* ctx, RnShape p, RnAdjoint<T> a, const RnSplit& s, float* dgamma, hipStream_t st) {
   const long n = (long)(p.lmax + 1) * p.C;
-  if (p.n) hipLaunchKernelGGL(rn_any_adjoint_kernel<T>, dim3((unsigned)s.chunks, p.lmax + 1), dim3(RN_WAVES * 64), 0, st, p, a);
-  hipLaunchKernelGGL(rn_join_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, (const float*)a.part, p.n ? (long)s.chunks : 0l, n, dgamma);
+  const int vecs = (p.C + RvWidth<T>::V - 1) / RvWidth<T>::V, size = sizeof(T);
+  p.lanes = rn_lanes(vecs);
+  if (s.chunks == 1) a.part = dgamma;
+  const bool even = p.C % RvWidth<T>::V == 0 && rv_aligned({a.h, a.dy, a.dh, a.dx, a.gamma}, {a.hs * size, a.dys * size, a.dh ? a.dhs * size : 0, a.dxs * size});
+  if (p.n && !(even ? rn_backward_vectors<T, true>(p, a, vecs, s.chunks, st) : rn_backward_vectors<T, false>(p, a, vecs, s.chunks, st)))
+    hipLaunchKernelGGL(rn_any_adjoint_kernel<T>, dim3((unsigned)s.chunks, p.lmax + 1), dim3(RN_THREADS), 0, st, p, a);
+  if (!p.n || s.chunks > 1)
+    hipLaunchKernelGGL(rn_join_kernel, dim3((unsigned)((n + 15) / 16)), dim3(256), 0, st, (const float*)a.part, p.n ? s.chunks : 0, n, dgamma);
   EGNN_LAUNCH_CHECK(ctx, "rms_norm_backward");
   return EGNN_OK;
 }
@@ -183,7 +504,7 @@ extern "C" int egnn_rms_norm(egnn_ctx* ctx, int32_t dtype, const void* x, int64_
   if (q && (q_stride < channels || q_stride % 16 || (uintptr_t)q % 16))
     return egnn_fail(ctx, EGNN_EINVAL, "rms_norm: rows of codes begin at multiples of 16 bytes");
   if (n_rows == 0) return EGNN_OK;
-  const RnShape p{n_rows, channels, lmax, eps};
+  const RnShape p{n_rows, channels, lmax, eps, 1};
   hipStream_t st = (hipStream_t)stream;
 #define RN_CALL(T) return rn_forward<T>(ctx, p, {(const T*)x, (const T*)r, (T*)h, (T*)y, (uint8_t*)q, (uint8_t*)scale, x_stride, r_stride, h_stride, y_stride, q_stride, gamma}, st)
   if (dtype == EGNN_F32) RN_CALL(float);
@@ -209,9 +530,9 @@ extern "C" int egnn_rms_norm_backward(egnn_ctx* ctx, int32_t dtype, const void* 
   if (h_stride < row || dy_stride < row || (dh && dh_stride < row) || dx_stride < row)
     return egnn_fail(ctx, EGNN_EINVAL, "rms_norm_backward: a row stride below the row's length");
   const RnSplit s = rn_split(n_rows, lmax, channels);
-  if (!ws || (uintptr_t)ws % 256 || ws_bytes < s.bytes)
+  if (s.bytes && (!ws || (uintptr_t)ws % 256 || ws_bytes < s.bytes))
     return egnn_fail(ctx, EGNN_EWS, "rms_norm_backward: workspace too small or not 256-byte aligned");
-  const RnShape p{n_rows, channels, lmax, eps};
+  const RnShape p{n_rows, channels, lmax, eps, 1};
   hipStream_t st = (hipStream_t)stream;
 #define RN_CALL(T) return rn_backward<T>(ctx, p, {(const T*)h, (const T*)dy, (const T*)dh, (T*)dx, (float*)ws, h_stride, dy_stride, dh_stride, dx_stride, s.rows, gamma}, s, dgamma, st)
   if (dtype == EGNN_F32) RN_CALL(float);
