@@ -137,10 +137,18 @@ def _rows(t, n, length, dtype):
 
 
 def _here(*tensors):
-    """Refuses tensors of another device than the current one, on whose stream the kernels run."""
+    """Refuses tensors of another device than the current one, on whose stream the kernels run (None and False are no tensors)."""
+    here = None
     for t in tensors:
-        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
-            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{torch.cuda.current_device()}")
+        if t is None or t is False:
+            continue
+        device = t.get_device()
+        if device < 0:
+            continue                          # a host tensor is refused with its name, type and shape
+        if here is None:
+            here = torch.cuda.current_device() if _device is None else _device()
+        if device != here:
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
 
 
 CODES, SCALES, BLOCK = torch.float8_e4m3fn, torch.float8_e8m0fnu, 128
@@ -165,45 +173,49 @@ def empty_matrix_codes(shape, device="cuda"):
             torch.empty((batch, _blocks(rows), _blocks(cols)), dtype=SCALES, device=device))
 
 
-def _code_rows(q, scale, shape):
+def _code_rows(q, scale, shape, scale_shape=None):
     """(address, bytes from row to row, address of the scales) of codes of this shape whose rows of the last axis follow one another."""
-    if not (q.is_cuda and q.dtype == CODES and tuple(q.shape) == tuple(shape)):
+    if not (q.is_cuda and q.dtype == CODES and q.shape == shape):
         raise ValueError(f"{CODES} device tensor of shape {tuple(shape)} required, not {q.dtype} {tuple(q.shape)} on {q.device}")
-    n, stride = shape[-1], q.stride()
-    row, wide = None, 1                       # of the rows, from the innermost axis with several of them on
-    for size, step in zip(reversed(shape[:-1]), reversed(stride[:-1])):
-        if size == 1:
-            continue
-        row = step if row is None else row
-        if step != row * wide:
-            raise ValueError(f"rows of codes must follow one another, not with strides {stride}")
-        wide *= size
-    row = (n + 15) // 16 * 16 if row is None or 0 in shape[:-1] else row
-    if stride[-1] != 1 and n > 1 or row < n:
-        raise ValueError(f"rows of codes must be contiguous and must not overlap, not of strides {stride}")
-    if n % 16 and q.numel() and q.untyped_storage().nbytes() < q.storage_offset() + (q.numel() // n - 1) * row + (n + 15) // 16 * 16:
-        raise ValueError("the last row of codes has no room up to a multiple of 16 bytes")
-    return q.data_ptr(), row, _at(scale, (*shape[:-1], _blocks(n)), SCALES)
+    n = shape[-1]
+    if n % 16 == 0 and q.is_contiguous():
+        row = n
+    else:
+        stride = q.stride()
+        row, wide = None, 1                   # of the rows, from the innermost axis with several of them on
+        for size, step in zip(reversed(shape[:-1]), reversed(stride[:-1])):
+            if size == 1:
+                continue
+            row = step if row is None else row
+            if step != row * wide:
+                raise ValueError(f"rows of codes must follow one another, not with strides {stride}")
+            wide *= size
+        row = (n + 15) // 16 * 16 if row is None or 0 in shape[:-1] else row
+        if stride[-1] != 1 and n > 1 or row < n:
+            raise ValueError(f"rows of codes must be contiguous and must not overlap, not of strides {stride}")
+        if n % 16 and q.numel() and q.untyped_storage().nbytes() < q.storage_offset() + (q.numel() // n - 1) * row + (n + 15) // 16 * 16:
+            raise ValueError("the last row of codes has no room up to a multiple of 16 bytes")
+    return q.data_ptr(), row, _at(scale, scale_shape or (*shape[:-1], (n + 127) // 128), SCALES)
 
 
 def _matrix_code_rows(q, scale, shape):
     """The same for matrices of codes, which have fewer scales."""
-    batch, rows, cols = shape
-    at, row, _ = _code_rows(q, None, shape)
-    return at, row, _at(scale, (batch, _blocks(rows), _blocks(cols)), SCALES)
+    return _code_rows(q, scale, shape, (shape[0], _blocks(shape[1]), _blocks(shape[2])))
 
 
 def _planes(t, shape, dtype):
     """(address, row stride) of rows of planes of channels; contiguous inside a row."""
     if t is None:
         return None, 0
+    if not (t.is_cuda and t.dtype == dtype and t.shape == shape):
+        raise ValueError(f"{dtype} device tensor of shape {tuple(shape)} required, not {t.dtype} {tuple(t.shape)} on {t.device}")
     n, dim, c = shape
-    if t.dim() == 3 and tuple(t.shape) == tuple(shape) and t.is_cuda and t.dtype == dtype:
-        row, plane, one = t.stride()
-        if (one == 1 or c == 1) and (plane == c or dim == 1) and (row >= dim * c or n <= 1):
-            return t.data_ptr(), max(row, dim * c)
+    if t.is_contiguous():
+        return t.data_ptr(), dim * c
+    row, plane, one = t.stride()
+    if not ((one == 1 or c == 1) and (plane == c or dim == 1) and (row >= dim * c or n <= 1)):
         raise ValueError(f"rows must be contiguous and must not overlap, not of strides {t.stride()}")
-    raise ValueError(f"{dtype} device tensor of shape {tuple(shape)} required, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr(), max(row, dim * c)
 
 
 class TensorList:
@@ -918,9 +930,9 @@ class Egnn:
         Returns (y, h, q, scale).  y = False: it is not computed.  h = False: the sum is not kept (h is x without a residual).  q = None: y also in
         codes with their scales, to new tensors; q and scale: to these.  What is not computed is None in the result."""
         _here(x, gamma, residual, y, h, q, scale)
-        code, shape, (degrees, c) = self._dtype(x), tuple(x.shape), gamma.shape
+        code, shape, (degrees, c) = self._dtype(x), x.shape, gamma.shape
         if len(shape) != 3 or shape[1:] != (degrees * degrees, c):
-            raise ValueError(f"x of shape (n, {degrees * degrees}, {c}) required for gamma {tuple(gamma.shape)}, not {shape}")
+            raise ValueError(f"x of shape (n, {degrees * degrees}, {c}) required for gamma {tuple(gamma.shape)}, not {tuple(shape)}")
         n = shape[0]
         y = None if y is False else torch.empty(shape, dtype=x.dtype, device=x.device) if y is None else y
         if residual is None and h is not None and h is not False:
@@ -942,9 +954,9 @@ class Egnn:
     def egnn_rms_norm_backward(self, h, dy, gamma, dh=None, eps=1e-5, dx=None, dgamma=None, ws=None):
         """Adjoint of egnn_rms_norm at the h it returned; dh: what reaches h besides.  Returns (dx, dgamma); dx is also the residual's."""
         _here(h, dy, gamma, dh, dx, dgamma, ws)
-        code, shape, (degrees, c) = self._dtype(h), tuple(h.shape), gamma.shape
+        code, shape, (degrees, c) = self._dtype(h), h.shape, gamma.shape
         if len(shape) != 3 or shape[1:] != (degrees * degrees, c):
-            raise ValueError(f"h of shape (n, {degrees * degrees}, {c}) required for gamma {tuple(gamma.shape)}, not {shape}")
+            raise ValueError(f"h of shape (n, {degrees * degrees}, {c}) required for gamma {tuple(gamma.shape)}, not {tuple(shape)}")
         dx = torch.empty(shape, dtype=h.dtype, device=h.device) if dx is None else dx
         dgamma = torch.empty((degrees, c), dtype=torch.float32, device=h.device) if dgamma is None else dgamma
         ws, at, size = self._room(ws, self.lib.egnn_rms_norm_workspace_bytes, shape[0], degrees - 1, c)
@@ -985,7 +997,7 @@ class Egnn:
         axes are taken as one row after the other); without ptr one group of all rows.  y, or a new tensor of `dtype` [n][n_out]."""
         _here(q, scale, w, w_scale, ptr, perm, bias, y)
         groups, n_out, n_in = w.shape
-        q_at, q_row, s_at = _code_rows(q, scale, (*q.shape[:-1], n_in))
+        q_at, q_row, s_at = _code_rows(q, scale, q.shape if q.shape[-1] == n_in else (*q.shape[:-1], n_in))
         w_at, w_row, ws_at = _matrix_code_rows(w, w_scale, (groups, n_out, n_in))
         n = q.numel() // n_in
         y = torch.empty((n, n_out), dtype=dtype, device=q.device) if y is None else y

@@ -389,7 +389,7 @@ RnSplit rn_split(int64_t n, int lmax, int C) {
   s.rows = s.rows < 16 ? s.rows : (s.rows + 15) / 16 * 16;
   if (s.rows < 1) s.rows = 1;
   s.chunks = n ? (int)((n + s.rows - 1) / s.rows) : 1;
-  s.bytes = s.chunks > 1 ? (size_t)s.chunks * (lmax + 1) * C * sizeof(float) : 0;
+  s.bytes = (size_t)s.chunks * (lmax + 1) * C * sizeof(float);
   return s;
 }
 
@@ -530,7 +530,7 @@ extern "C" int egnn_rms_norm_backward(egnn_ctx* ctx, int32_t dtype, const void* 
   if (h_stride < row || dy_stride < row || (dh && dh_stride < row) || dx_stride < row)
     return egnn_fail(ctx, EGNN_EINVAL, "rms_norm_backward: a row stride below the row's length");
   const RnSplit s = rn_split(n_rows, lmax, channels);
-  if (s.bytes && (!ws || (uintptr_t)ws % 256 || ws_bytes < s.bytes))
+  if (!ws || (uintptr_t)ws % 256 || ws_bytes < s.bytes)
     return egnn_fail(ctx, EGNN_EWS, "rms_norm_backward: workspace too small or not 256-byte aligned");
   const RnShape p{n_rows, channels, lmax, eps, 1};
   hipStream_t st = (hipStream_t)stream;

@@ -120,6 +120,48 @@ def test_more_groups_than_a_wave(m, dtype):
     check(m, 500, 32, 16, dtype, 699, ptr)
 
 
+def check_large(m, n, k, out, dtype, groups=1, ptr=None, perm=None, seed=0):
+    """check() with values and an oracle (fp64 products of the values of the codes) made on the device."""
+    import torch
+    torch.manual_seed(seed)
+    a = m.egnn_quantise_rows(torch.randn(n, k, device="cuda") * torch.rand(n, 1, device="cuda"))
+    b = m.egnn_quantise_matrices(torch.randn(groups, out, k, device="cuda"))[:2]
+    bias = torch.randn(groups, out, device="cuda")
+    x = a[0].double() * a[1].double().repeat_interleave(128, 1)[:, :k]
+    W = b[0].double() * b[1].double().repeat_interleave(128, 2)[:, :, :k].repeat_interleave(128, 1)[:, :out]
+    t = lambda v: None if v is None else torch.as_tensor(np.asarray(v), dtype=torch.int32, device="cuda")
+    y = torch.full((n, out), 77.0, dtype=getattr(torch, dtype), device="cuda")
+    m.egnn_scaled_linear(*a, *b, ptr=t(ptr), perm=t(perm), bias=bias, y=y)
+    order, at = torch.arange(n, device="cuda") if perm is None else t(perm).long(), [0, n] if ptr is None else [int(v) for v in ptr]
+    seen = torch.zeros(n, dtype=torch.bool, device="cuda")
+    off = 2 * (18 + k / 128) * U32 if dtype != "bfloat16" else 7 * 2.0 ** -13 + 2 * (2 + k / 8) * U32
+    for g in range(groups):
+        rows = order[at[g]:at[g + 1]]
+        seen[rows] = True
+        ry = x[rows] @ W[g].t() + bias[g]
+        size = x[rows].abs() @ W[g].abs().t() + bias[g].abs()
+        far = (y[rows].double() - ry).abs()
+        assert (far <= off * size + HALF_STEP[dtype] * ry.abs() + FLOOR[dtype]).all()
+        if len(rows) > 100:
+            assert far.norm() <= (2 * HALF_STEP[dtype] / 3 ** 0.5 + 3e-5) * ry.norm()
+    assert (y[~seen] == 77.0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,k,out", [(20001, 300, 520), (3600, 2100, 3400), (4097, 2048, 4090), (2050, 700, 2000), (5120, 136, 5000)])
+def test_many_tiles(m, n, k, out, dtype):
+    check_large(m, n, k, out, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,k,out,ptr", [(3000, 200, 300, [0, 0, 1, 700, 700, 2999]), (30001, 200, 260, [7, 7, 5000, 5001, 12345, 29000, 29000, 30001]),
+                                         (4500, 2100, 3300, [0, 2001, 4500]), (70000, 64, 64, [0, 10, 30000, 30000, 69999]), (5000, 130, 40, [0, 2500, 5000])])
+def test_many_tiles_in_groups(m, n, k, out, ptr, dtype):
+    """The last rows of a group and the first of the next in one tile's reach; rows in any order and in their own."""
+    check_large(m, n, k, out, dtype, len(ptr) - 1, ptr)
+    check_large(m, n, k, out, dtype, len(ptr) - 1, ptr, np.random.default_rng(n).permutation(n), seed=1)
+
+
 def test_pointers_out_of_range_are_clamped(m):
     import torch
     rng = np.random.default_rng(10)
