@@ -8,14 +8,14 @@
 // same order, and scales its pieces.  No atomics: the same bits every time.  The tensors' addresses travel as kernel arguments, so that a call
 // copies nothing from host memory and can be captured; CG_TENSORS of them at a time.
 #include <algorithm>
-#include "row_types.h"
+#include "row_vectors.h"
 
 namespace {
 
 constexpr int CG_TENSORS = 96;        // of 40 bytes each: kernel arguments of just under 4 KB
 constexpr int CG_THREADS = 256;
-constexpr int CG_PIECE = 16384;       // values of a piece
 constexpr int CG_SLOTS = 1024;        // workgroups of a launch at most
+constexpr int CG_AHEAD = 4;           // vectors of a thread under way at once
 
 struct CgTensor {
   const void* data;
@@ -25,23 +25,44 @@ struct CgTensor {
 };
 struct CgTable {
   CgTensor t[CG_TENSORS];
-  int count;
+  int count, piece;                   // piece: values of a piece
   long pieces;
 };
 
-// calls f(tensor, first value, values) for the pieces of this workgroup
+// calls f(tensor, first value, values) for the run of pieces of workgroup `block`; backwards: the last first
 template <class F>
-__device__ __forceinline__ void cg_pieces(const CgTable& p, const F& f) {
-  for (long k = blockIdx.x; k < p.pieces; k += gridDim.x) {
-    int lo = 0, hi = p.count - 1;     // the last tensor that begins at k or before (tensors of no values have no pieces and are not in the table)
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (p.t[mid].first <= k) lo = mid; else hi = mid - 1;
-    }
-    const CgTensor& t = p.t[lo];
-    const long at = (k - t.first) * CG_PIECE;
-    f(t, at, (int)min((long)CG_PIECE, t.n - at));
+__device__ __forceinline__ void cg_pieces(const CgTable& p, long block, bool backwards, const F& f) {
+  const long each = (p.pieces + gridDim.x - 1) / gridDim.x, begin = block * each, end = min(begin + each, p.pieces);
+  if (begin >= end) return;
+  const long from = backwards ? end - 1 : begin;
+  int at = 0;                         // the last tensor that begins at `from` or before (tensors of no values are not in the table)
+  for (int step = 64; step; step >>= 1)
+    if (at + step < p.count && p.t[at + step].first <= from) at += step;
+  for (long k = from; k >= begin && k < end; k += backwards ? -1 : 1) {
+    while (at + 1 < p.count && p.t[at + 1].first <= k) ++at;
+    while (p.t[at].first > k) --at;
+    const CgTensor& t = p.t[at];
+    const long first = (k - t.first) * p.piece;
+    f(t, first, (int)min((long)p.piece, t.n - first));
   }
+}
+
+// calls f(first value, vector) for the vectors of a thread among n values at `data`, CG_AHEAD of them loaded at a time, and g(value) for the last values
+// of the n that make no vector
+template <class T, class F, class G>
+__device__ __forceinline__ void cg_vectors(const T* data, int n, const F& f, const G& g) {
+  typedef Rv<T, false> R;
+  constexpr int V = R::V;
+  const int vecs = n / V;
+  for (int i = threadIdx.x; i < vecs; i += CG_THREADS * CG_AHEAD) {
+    typename R::vec v[CG_AHEAD];
+#pragma unroll
+    for (int u = 0; u < CG_AHEAD; ++u) v[u] = *(const typename R::loose*)(data + min(i + u * CG_THREADS, vecs - 1) * V);
+#pragma unroll
+    for (int u = 0; u < CG_AHEAD; ++u)
+      if (i + u * CG_THREADS < vecs) f((i + u * CG_THREADS) * V, v[u]);
+  }
+  if ((int)threadIdx.x < n - vecs * V) g(vecs * V + threadIdx.x);
 }
 
 __device__ __forceinline__ double cg_block_sum(double v) {
@@ -56,32 +77,38 @@ __device__ __forceinline__ double cg_block_sum(double v) {
 }
 
 template <class T>
-__device__ __forceinline__ double cg_square(const void* data, long at, int n) {
-  const T* g = (const T*)data + at;
+__device__ __forceinline__ double cg_square(const CgTensor& t, long at, int n) {
+  const T* g = (const T*)t.data + at;
   double sum = 0.0;
-  for (int i = threadIdx.x; i < n; i += CG_THREADS) {
-    const double v = (double)(float)g[i];
-    sum += v * v;
-  }
+  auto add = [&](T v) { sum += (double)(float)v * (double)(float)v; };
+  cg_vectors(g, n, [&](int, const typename Rv<T, false>::vec& v) {
+#pragma unroll
+    for (int i = 0; i < Rv<T, false>::V; ++i) add(v[i]);
+  }, [&](int i) { add(g[i]); });
   return sum;
 }
 
 __global__ void __launch_bounds__(CG_THREADS) cg_square_kernel(CgTable p, double* slot) {
   double sum = 0.0;
-  cg_pieces(p, [&](const CgTensor& t, long at, int n) {
-    sum += t.dtype == EGNN_F32 ? cg_square<float>(t.data, at, n) : t.dtype == EGNN_F16 ? cg_square<_Float16>(t.data, at, n) : cg_square<__bf16>(t.data, at, n);
+  cg_pieces(p, blockIdx.x, false, [&](const CgTensor& t, long at, int n) {
+    sum += t.dtype == EGNN_F32 ? cg_square<float>(t, at, n) : t.dtype == EGNN_F16 ? cg_square<_Float16>(t, at, n) : cg_square<__bf16>(t, at, n);
   });
   sum = cg_block_sum(sum);
   if (threadIdx.x == 0) slot[blockIdx.x] = sum;
 }
 
 template <class T>
-__device__ __forceinline__ void cg_scale(const CgTensor& t, long at, int n, float factor) {
+__device__ __forceinline__ void cg_scale(const CgTensor& t, long at, int n, float by) {
   const T* g = (const T*)t.data + at;
   T* out = (T*)t.out + at;
-  for (int i = threadIdx.x; i < n; i += CG_THREADS) out[i] = (T)((float)g[i] * factor);
+  cg_vectors(g, n, [&](int i, typename Rv<T, false>::vec v) {
+#pragma unroll
+    for (int k = 0; k < Rv<T, false>::V; ++k) v[k] = (T)((float)v[k] * by);
+    *(typename Rv<T, false>::loose*)(out + i) = v;
+  }, [&](int i) { out[i] = (T)((float)g[i] * by); });
 }
 
+// The second pass begins with what the first one read last, which the caches still hold.
 __global__ void __launch_bounds__(CG_THREADS) cg_scale_kernel(CgTable p, const double* slot, int slots, float most, float* norm, bool tell) {
   double sum = 0.0;
   for (int i = threadIdx.x; i < slots; i += CG_THREADS) sum += slot[i];
@@ -93,7 +120,7 @@ __global__ void __launch_bounds__(CG_THREADS) cg_scale_kernel(CgTable p, const d
     norm[1] = factor;
   }
   const float by = finite ? factor : 1.0f;
-  cg_pieces(p, [&](const CgTensor& t, long at, int n) {
+  cg_pieces(p, gridDim.x - 1 - blockIdx.x, true, [&](const CgTensor& t, long at, int n) {
     if (by == 1.0f && t.out == t.data) return;
     if (t.dtype == EGNN_F32) cg_scale<float>(t, at, n, by);
     else if (t.dtype == EGNN_F16) cg_scale<_Float16>(t, at, n, by);
@@ -138,17 +165,24 @@ bool cg_overlaps(const egnn_tensor* t, int32_t count) {
   return false;
 }
 
-// Tables of up to CG_TENSORS tensors that have values, one after the other
+// Tables of up to CG_TENSORS tensors that have values, one after the other.  A piece is what a workgroup reads at once, 4,096 to 16,384 values: fewer where all
+// values make few workgroups.
 struct CgWalk {
   const egnn_tensor* t;
-  int32_t count, at = 0;
+  int32_t count, at = 0, piece = 0;
   bool next(CgTable& p) {
+    if (!piece) {
+      int64_t all = 0;
+      for (int32_t i = 0; i < count; ++i) all += t[i].n;
+      for (piece = 16384; piece > 4096 && all / piece < CG_SLOTS; piece /= 2) {}
+    }
     p.count = 0;
     p.pieces = 0;
+    p.piece = piece;
     for (; at < count && p.count < CG_TENSORS; ++at) {
       if (!t[at].n) continue;
       p.t[p.count++] = {t[at].data, t[at].out, (long)t[at].n, p.pieces, t[at].dtype};
-      p.pieces += (long)((t[at].n + CG_PIECE - 1) / CG_PIECE);
+      p.pieces += (long)((t[at].n + piece - 1) / piece);
     }
     return p.count > 0;
   }

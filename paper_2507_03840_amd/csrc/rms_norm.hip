@@ -364,17 +364,25 @@ __global__ void __launch_bounds__(RN_WAVES * 64) rn_any_adjoint_kernel(RnShape p
   }
 }
 
-// Adds the chunks' gradients of gamma: 16 columns a workgroup, each by 16 threads that take the chunks in turn
-__global__ void __launch_bounds__(256) rn_join_kernel(const float* part, int chunks, long n, float* out) {
-  __shared__ double lds[16][17];
-  const long at = (long)blockIdx.x * 16 + (threadIdx.x & 15);
+// Adds the chunks' gradients of gamma: 16 columns a workgroup, each by 32 threads that take the chunks in turn, four of them under way
+constexpr int RN_JOIN = 512, RN_JOIN_TURNS = RN_JOIN / 16;
+__global__ void __launch_bounds__(RN_JOIN) rn_join_kernel(const float* part, int chunks, long n, float* out) {
+  __shared__ double lds[RN_JOIN_TURNS][17];
+  const long at = min((long)blockIdx.x * 16 + (threadIdx.x & 15), n - 1);
+  const int turn = threadIdx.x >> 4;
   double sum = 0.0;
-  if (at < n)
-    for (int k = threadIdx.x >> 4; k < chunks; k += 16) sum += (double)part[k * n + at];
-  lds[threadIdx.x >> 4][threadIdx.x & 15] = sum;
+  for (int k = turn; k < chunks; k += 4 * RN_JOIN_TURNS) {
+    float v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = part[min(k + u * RN_JOIN_TURNS, chunks - 1) * n + at];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (k + u * RN_JOIN_TURNS < chunks) sum += (double)v[u];
+  }
+  lds[turn][threadIdx.x & 15] = sum;
   __syncthreads();
-  if (threadIdx.x >= 16 || at >= n) return;
-  for (int k = 1; k < 16; ++k) sum += lds[k][threadIdx.x];
+  if (threadIdx.x >= 16 || (long)blockIdx.x * 16 + threadIdx.x >= n) return;
+  for (int k = 1; k < RN_JOIN_TURNS; ++k) sum += lds[k][threadIdx.x];
   out[at] = (float)sum;
 }
 
@@ -481,7 +489,7 @@ int rn_backward(egnn_ctx* ctx, RnShape p, RnAdjoint<T> a, const RnSplit& s, floa
   if (p.n && !(even ? rn_backward_vectors<T, true>(p, a, vecs, s.chunks, st) : rn_backward_vectors<T, false>(p, a, vecs, s.chunks, st)))
     hipLaunchKernelGGL(rn_any_adjoint_kernel<T>, dim3((unsigned)s.chunks, p.lmax + 1), dim3(RN_THREADS), 0, st, p, a);
   if (!p.n || s.chunks > 1)
-    hipLaunchKernelGGL(rn_join_kernel, dim3((unsigned)((n + 15) / 16)), dim3(256), 0, st, (const float*)a.part, p.n ? s.chunks : 0, n, dgamma);
+    hipLaunchKernelGGL(rn_join_kernel, dim3((unsigned)((n + 15) / 16)), dim3(RN_JOIN), 0, st, (const float*)a.part, p.n ? s.chunks : 0, n, dgamma);
   EGNN_LAUNCH_CHECK(ctx, "rms_norm_backward");
   return EGNN_OK;
 }
