@@ -6,14 +6,16 @@
 // No mean is subtracted and gamma is the same for all m of a degree, so the norm commutes with rotations.  y is that of the stored, rounded sum:
 // the adjoint, which reads h, is then the adjoint of what was computed.  With d = gamma dy:
 //   dx = dh + rho (d - h rho^2 sum(d h) / L),  dgamma_{l,c} = sum over rows and m of dy h rho.
-// Sums over a row are fp64: squares of any fp32 value stay finite, and the two terms of dx, which cancel in short rows (for one value all but
-// eps rho^2 of them), are subtracted in fp64 from a rho that is made again from h.
+// Sums over a row are fp64: squares of any fp32 value stay finite.  The two terms of dx, which cancel in short rows (for one value all but
+// eps rho^2 of them), are subtracted in fp64 in rows of up to 32 values, from a rho that is made again from h; in longer ones in fp32.
+#include <algorithm>
 #include "codes8.h"
 #include "row_vectors.h"
 
 namespace {
 
 constexpr int RN_WIDE_ROWS = 1024;    // from so many rows on a wave takes a row of up to 512 vectors, below it a workgroup
+constexpr int RN_SHORT = 32;           // up to so many values the adjoint's differences are fp64
 constexpr int RN_THREADS = 256, RN_WAVES = RN_THREADS / 64;
 
 struct RnShape {
@@ -51,6 +53,9 @@ __device__ __forceinline__ double rn_row_sum(double v, int lanes, double* lds) {
   return v;
 }
 
+// Degree of a workgroup: workgroups go through the degrees of a run of rows, the longest first, before the next rows, so that short ones run beside long ones
+__device__ __forceinline__ int rn_degree(const RnShape& p) { return p.lmax - (int)(blockIdx.x % (p.lmax + 1)); }
+
 // U rows at a time of one degree, PL planes each, by `lanes` lanes with NV vectors of a plane each (WIDE: by the workgroup).  All of them are
 // read before anything is written.
 template <class T, bool EVEN, int PL, int U, int NV, bool WIDE>
@@ -60,7 +65,7 @@ __device__ __forceinline__ void rn_write(const RnShape& p, const RnForward<T>& a
   __shared__ double lds[RN_WAVES];
   const int lanes = WIDE ? RN_THREADS : p.lanes, lane = threadIdx.x & (lanes - 1), groups = RN_THREADS / lanes, C = p.C;
   const int dim = (p.lmax + 1) * (p.lmax + 1), vecs = (C + V - 1) / V, blocks = (C + C8_BLOCK - 1) / C8_BLOCK;
-  const long row0 = (long)blockIdx.x * groups * U + threadIdx.x / lanes;
+  const long row0 = (long)(blockIdx.x / (p.lmax + 1)) * groups * U + threadIdx.x / lanes;
   typename R::vec h[U][PL][NV];
 #pragma unroll
   for (int u = 0; u < U; ++u)
@@ -137,10 +142,9 @@ template <class T, bool EVEN, int NV>
 __global__ void __launch_bounds__(RN_THREADS) rn_rows_kernel(RnShape p, RnForward<T> a) { rn_write<T, EVEN, 1, NV == 1 ? 4 : 1, NV, false>(p, a, 0); }
 template <class T, bool EVEN, int NV>
 __global__ void __launch_bounds__(RN_THREADS) rn_wide_kernel(RnShape p, RnForward<T> a) { rn_write<T, EVEN, 1, 1, NV, true>(p, a, 0); }
-// a degree for each blockIdx.y, the longest first
 template <class T, bool EVEN>
 __global__ void __launch_bounds__(RN_THREADS) rn_degrees_kernel(RnShape p, RnForward<T> a) {
-  switch (p.lmax - blockIdx.y) {
+  switch (rn_degree(p)) {
     case 0: rn_write<T, EVEN, 1, 1, 1, false>(p, a, 0); break;
     case 1: rn_write<T, EVEN, 3, 1, 1, false>(p, a, 1); break;
     case 2: rn_write<T, EVEN, 5, 1, 1, false>(p, a, 2); break;
@@ -192,23 +196,36 @@ __global__ void __launch_bounds__(RN_WAVES * 64) rn_any_kernel(RnShape p, RnForw
     }
 }
 
+// Chunks of rows of the adjoint, the same for every type and degree: as many workgroups as run at once (1,024, or 2,048 with degrees, whose workgroups are of
+// unlike length), and no fewer than 4,096 values of a plane in each, so that the chunks' gradients of gamma are a small part of what is read.
+struct RnSplit { long rows; int chunks; };
+RnSplit rn_split(int64_t n, int lmax, int C) {
+  const long most = lmax ? 2048l / (lmax + 1) : 1024;
+  RnSplit s;
+  s.rows = std::max<long>(std::max<long>((n + most - 1) / most, 4096l / C), 1);
+  if (s.rows > 16) s.rows = (s.rows + 15) / 16 * 16;
+  s.chunks = n ? (int)((n + s.rows - 1) / s.rows) : 1;
+  return s;
+}
+
 template <class T>
 struct RnAdjoint {
   const T *h, *dy, *dh;   // dh may be NULL
   T* dx;
-  float* part;            // [chunks][lmax + 1][C]
-  long hs, dys, dhs, dxs, rows;   // rows of a chunk
+  float* part;            // [chunks][lmax + 1][C], the highest degree first
+  long hs, dys, dhs, dxs;
   const float* gamma;
 };
 
-// The rows of a chunk, in the layout of rn_write; the gradient of gamma stays in registers until the last of them.
-template <class T, bool EVEN, int PL, int U, int NV, bool WIDE>
-__device__ __forceinline__ void rn_adjoint(const RnShape& p, const RnAdjoint<T>& a, int l, double* lds) {
-  typedef Rv<T, EVEN> R;
-  constexpr int V = R::V;
+// The rows of a chunk, in the layout of rn_write; the gradient of gamma stays in registers until the last of them.  Where a turn's rows are few registers,
+// the next turn's are on their way meanwhile.
+template <class T, bool EVEN, int PL, int U, int NV, bool WIDE, int V>
+__device__ __forceinline__ void rn_adjoint(const RnShape& p, const RnSplit& s, const RnAdjoint<T>& a, int l, double* lds) {
+  typedef Rv<T, EVEN, V> R;
+  constexpr bool EARLY = PL * U * NV <= 2;
   const int lanes = WIDE ? RN_THREADS : p.lanes, lane = threadIdx.x & (lanes - 1), groups = RN_THREADS / lanes, C = p.C;
   const int vecs = (C + V - 1) / V;
-  const long begin = (long)blockIdx.x * a.rows, end = min(begin + a.rows, p.n);
+  const long begin = (long)(blockIdx.x / (p.lmax + 1)) * s.rows, end = min(begin + s.rows, p.n);
   float gain[NV][V];
   double dg[NV][V];
 #pragma unroll
@@ -217,8 +234,8 @@ __device__ __forceinline__ void rn_adjoint(const RnShape& p, const RnAdjoint<T>&
 #pragma unroll
     for (int i = 0; i < V; ++i) dg[k][i] = 0.0;
   }
-  for (long r0 = begin + threadIdx.x / lanes, turn = begin; turn < end; r0 += groups * U, turn += groups * U) {
-    typename R::vec h[U][PL][NV], dy[U][PL][NV], dh[U][PL][NV];
+  struct Rows { typename R::vec h[U][PL][NV], dy[U][PL][NV], dh[U][PL][NV]; };
+  auto fetch = [&](long r0, Rows& o) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -226,17 +243,27 @@ __device__ __forceinline__ void rn_adjoint(const RnShape& p, const RnAdjoint<T>&
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
           const long row = min(r0 + u * groups, p.n - 1);
-          h[u][m][k] = R::load(a.h + row * a.hs + (l * l + m) * C, lane + k * lanes, C);
-          dy[u][m][k] = R::load(a.dy + row * a.dys + (l * l + m) * C, lane + k * lanes, C);
+          o.h[u][m][k] = R::load(a.h + row * a.hs + (l * l + m) * C, lane + k * lanes, C);
+          o.dy[u][m][k] = R::load(a.dy + row * a.dys + (l * l + m) * C, lane + k * lanes, C);
         }
-    if (a.dh) {
+    if (a.dh)
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int m = 0; m < PL; ++m)
 #pragma unroll
-          for (int k = 0; k < NV; ++k) dh[u][m][k] = R::load(a.dh + min(r0 + u * groups, p.n - 1) * a.dhs + (l * l + m) * C, lane + k * lanes, C);
+          for (int k = 0; k < NV; ++k) o.dh[u][m][k] = R::load(a.dh + min(r0 + u * groups, p.n - 1) * a.dhs + (l * l + m) * C, lane + k * lanes, C);
+  };
+  Rows now, then;
+  if constexpr (EARLY) fetch(begin + threadIdx.x / lanes, then);
+  for (long r0 = begin + threadIdx.x / lanes, turn = begin; turn < end; r0 += groups * U, turn += groups * U) {
+    if constexpr (EARLY) {
+      now = then;
+      fetch(r0 + groups * U, then);
+    } else {
+      fetch(r0, now);
     }
+    auto &h = now.h, &dy = now.dy, &dh = now.dh;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const long row = r0 + u * groups;
@@ -257,27 +284,53 @@ __device__ __forceinline__ void rn_adjoint(const RnShape& p, const RnAdjoint<T>&
       if constexpr (WIDE) __syncthreads();
       along = rn_row_sum<WIDE>(along, lanes, lds);
       if constexpr (WIDE) __syncthreads();
-      const double rho = rn_rsqrt(sum / ((double)PL * C) + (double)p.eps), back = along / ((double)PL * C) * rho * rho;
+      const double rho = rn_rsqrt(sum / ((double)PL * C) + (double)p.eps);
+      along = along / ((double)PL * C) * rho;
       if (!there) continue;
+      if (PL * C <= RN_SHORT) {
 #pragma unroll
-      for (int k = 0; k < NV; ++k)
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+          for (int m = 0; m < PL; ++m) {
+            typename R::vec dx;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+              const double hat = (double)(float)h[u][m][k][i] * rho;
+              const float d = (float)dy[u][m][k][i];
+              dg[k][i] += (double)d * hat;
+              double g = rho * ((double)(d * gain[k][i]) - hat * along);
+              if (a.dh) g += (double)(float)dh[u][m][k][i];
+              dx[i] = (T)(float)g;
+            }
+            R::store(a.dx + row * a.dxs + (l * l + m) * C, lane + k * lanes, C, dx);
+          }
+        continue;
+      }
+      // (as in rn_write: of rows of more than 2^64 rho is held times 2^64)
+      const bool large = rho < 0x1p-64;
+      const float by = (float)(large ? rho * 0x1p64 : rho), down = large ? 0x1p-64f : 1.0f, back = (float)along;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        float terms[V] = {};
 #pragma unroll
         for (int m = 0; m < PL; ++m) {
           typename R::vec dx;
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            const double v = (double)(float)h[u][m][k][i];
-            const float d = (float)dy[u][m][k][i];
-            dg[k][i] += (double)d * (v * rho);
-            double g = rho * ((double)(d * gain[k][i]) - v * back);
-            if (a.dh) g += (double)(float)dh[u][m][k][i];
-            dx[i] = (T)(float)g;
+            const float hat = (float)h[u][m][k][i] * down * by, d = (float)dy[u][m][k][i];
+            terms[i] = fmaf(d, hat, terms[i]);
+            float g = fmaf(-hat, back, d * gain[k][i]) * by * down;
+            if (a.dh) g += (float)dh[u][m][k][i];
+            dx[i] = (T)g;
           }
           R::store(a.dx + row * a.dxs + (l * l + m) * C, lane + k * lanes, C, dx);
         }
+#pragma unroll
+        for (int i = 0; i < V; ++i) dg[k][i] += (double)terms[i];
+      }
     }
   }
-  float* out = a.part + ((long)blockIdx.x * (p.lmax + 1) + l) * C;
+  float* out = a.part + (long)blockIdx.x * C;
   if constexpr (WIDE) {
 #pragma unroll
     for (int k = 0; k < NV; ++k)
@@ -304,34 +357,34 @@ __device__ __forceinline__ void rn_adjoint(const RnShape& p, const RnAdjoint<T>&
 }
 
 template <class T, bool EVEN, int NV>
-__global__ void __launch_bounds__(RN_THREADS) rn_rows_adjoint_kernel(RnShape p, RnAdjoint<T> a) {
+__global__ void __launch_bounds__(RN_THREADS) rn_rows_adjoint_kernel(RnShape p, RnSplit s, RnAdjoint<T> a) {
   extern __shared__ double rn_lds[];
-  rn_adjoint<T, EVEN, 1, NV == 1 ? 2 : 1, NV, false>(p, a, 0, rn_lds);
+  rn_adjoint<T, EVEN, 1, NV == 1 ? 2 : 1, NV, false, RvWidth<T>::V>(p, s, a, 0, rn_lds);
 }
 template <class T, bool EVEN, int NV>
-__global__ void __launch_bounds__(RN_THREADS) rn_wide_adjoint_kernel(RnShape p, RnAdjoint<T> a) {
+__global__ void __launch_bounds__(RN_THREADS) rn_wide_adjoint_kernel(RnShape p, RnSplit s, RnAdjoint<T> a) {
   extern __shared__ double rn_lds[];
-  rn_adjoint<T, EVEN, 1, 1, NV, true>(p, a, 0, rn_lds);
+  rn_adjoint<T, EVEN, 1, 1, NV, true, RvWidth<T>::V>(p, s, a, 0, rn_lds);
 }
-template <class T, bool EVEN>
-__global__ void __launch_bounds__(RN_THREADS) rn_degrees_adjoint_kernel(RnShape p, RnAdjoint<T> a) {
+template <class T, bool EVEN, int V>
+__global__ void __launch_bounds__(RN_THREADS) rn_degrees_adjoint_kernel(RnShape p, RnSplit s, RnAdjoint<T> a) {
   extern __shared__ double rn_lds[];
-  switch (p.lmax - blockIdx.y) {
-    case 0: rn_adjoint<T, EVEN, 1, 1, 1, false>(p, a, 0, rn_lds); break;
-    case 1: rn_adjoint<T, EVEN, 3, 1, 1, false>(p, a, 1, rn_lds); break;
-    case 2: rn_adjoint<T, EVEN, 5, 1, 1, false>(p, a, 2, rn_lds); break;
-    case 3: rn_adjoint<T, EVEN, 7, 1, 1, false>(p, a, 3, rn_lds); break;
-    default: rn_adjoint<T, EVEN, 9, 1, 1, false>(p, a, 4, rn_lds);
+  switch (rn_degree(p)) {
+    case 0: rn_adjoint<T, EVEN, 1, 1, 1, false, V>(p, s, a, 0, rn_lds); break;
+    case 1: rn_adjoint<T, EVEN, 3, 1, 1, false, V>(p, s, a, 1, rn_lds); break;
+    case 2: rn_adjoint<T, EVEN, 5, 1, 1, false, V>(p, s, a, 2, rn_lds); break;
+    case 3: rn_adjoint<T, EVEN, 7, 1, 1, false, V>(p, s, a, 3, rn_lds); break;
+    default: rn_adjoint<T, EVEN, 9, 1, 1, false, V>(p, s, a, 4, rn_lds);
   }
 }
 
 // A workgroup for a chunk of rows and a degree: its waves take the rows in turn.  The gradient of gamma is added in LDS a row after the other by
 // the wave whose turn it is.
 template <class T>
-__global__ void __launch_bounds__(RN_WAVES * 64) rn_any_adjoint_kernel(RnShape p, RnAdjoint<T> a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, degrees = p.lmax + 1, l = blockIdx.y, C = p.C;
+__global__ void __launch_bounds__(RN_WAVES * 64) rn_any_adjoint_kernel(RnShape p, RnSplit s, RnAdjoint<T> a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = rn_degree(p), C = p.C;
   const int first = l * l, last = (l + 1) * (l + 1);
-  const long begin = (long)blockIdx.x * a.rows, end = min(begin + a.rows, p.n);
+  const long begin = (long)(blockIdx.x / (p.lmax + 1)) * s.rows, end = min(begin + s.rows, p.n);
   for (long r0 = begin; r0 < end; r0 += RN_WAVES) {
     const long row = r0 + wave;
     double sum = 0.0, along = 0.0;
@@ -357,48 +410,33 @@ __global__ void __launch_bounds__(RN_WAVES * 64) rn_any_adjoint_kernel(RnShape p
           if (a.dh) v += (double)(float)a.dh[row * a.dhs + plane * C + c];
           a.dx[row * a.dxs + plane * C + c] = (T)(float)v;
         }
-        float* at = a.part + ((long)blockIdx.x * degrees + l) * C + c;
+        float* at = a.part + (long)blockIdx.x * C + c;
         *at = (row == begin ? 0.0f : *at) + (float)dg;
       }
     }
   }
 }
 
-// Adds the chunks' gradients of gamma: 16 columns a workgroup, each by 32 threads that take the chunks in turn, four of them under way
+// Adds the chunks' gradients of gamma: 16 channels of a degree a workgroup, each by 32 threads that take the chunks in turn, four of them under way
 constexpr int RN_JOIN = 512, RN_JOIN_TURNS = RN_JOIN / 16;
-__global__ void __launch_bounds__(RN_JOIN) rn_join_kernel(const float* part, int chunks, long n, float* out) {
+__global__ void __launch_bounds__(RN_JOIN) rn_join_kernel(RnShape p, RnSplit s, const float* part, float* dgamma) {
   __shared__ double lds[RN_JOIN_TURNS][17];
-  const long at = min((long)blockIdx.x * 16 + (threadIdx.x & 15), n - 1);
-  const int turn = threadIdx.x >> 4;
+  const int l = blockIdx.y, c = min((int)blockIdx.x * 16 + (int)(threadIdx.x & 15), p.C - 1), turn = threadIdx.x >> 4;
+  const int end = p.n ? s.chunks : 0;
   double sum = 0.0;
-  for (int k = turn; k < chunks; k += 4 * RN_JOIN_TURNS) {
+  for (int k = turn; k < end; k += 4 * RN_JOIN_TURNS) {
     float v[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) v[u] = part[min(k + u * RN_JOIN_TURNS, chunks - 1) * n + at];
+    for (int u = 0; u < 4; ++u) v[u] = part[((long)min(k + u * RN_JOIN_TURNS, end - 1) * (p.lmax + 1) + p.lmax - l) * p.C + c];
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      if (k + u * RN_JOIN_TURNS < chunks) sum += (double)v[u];
+      if (k + u * RN_JOIN_TURNS < end) sum += (double)v[u];
   }
   lds[turn][threadIdx.x & 15] = sum;
   __syncthreads();
-  if (threadIdx.x >= 16 || (long)blockIdx.x * 16 + threadIdx.x >= n) return;
+  if (threadIdx.x >= 16 || (int)(blockIdx.x * 16 + threadIdx.x) >= p.C) return;
   for (int k = 1; k < RN_JOIN_TURNS; ++k) sum += lds[k][threadIdx.x];
-  out[at] = (float)sum;
-}
-
-// Chunks of rows of the adjoint, the same for every type: about 2,048 workgroups, and no fewer than 16,384 values each, so that the chunks' gradients
-// of gamma are a small part of what is read
-struct RnSplit { long rows; int chunks; size_t bytes; };
-RnSplit rn_split(int64_t n, int lmax, int C) {
-  RnSplit s;
-  const long target = 2048 / (lmax + 1), least = 16384 / ((long)C * (lmax + 1));
-  s.rows = (n + target - 1) / target;
-  if (s.rows < least) s.rows = least;
-  s.rows = s.rows < 16 ? s.rows : (s.rows + 15) / 16 * 16;
-  if (s.rows < 1) s.rows = 1;
-  s.chunks = n ? (int)((n + s.rows - 1) / s.rows) : 1;
-  s.bytes = (size_t)s.chunks * (lmax + 1) * C * sizeof(float);
-  return s;
+  dgamma[l * p.C + c] = (float)sum;
 }
 
 int rn_check(egnn_ctx* ctx, const char* who, int32_t dtype, int64_t n, int32_t lmax, int32_t C, float eps) {
@@ -420,7 +458,7 @@ int rn_lanes(int vecs) {
 
 template <class T, bool EVEN>
 bool rn_forward_vectors(const RnShape& p, const RnForward<T>& a, int vecs, hipStream_t st) {
-  auto rows = [&](int groups) { return dim3((unsigned)((p.n + groups - 1) / groups), p.lmax + 1); };
+  auto rows = [&](int groups) { return dim3((unsigned)((p.n + groups - 1) / groups * (p.lmax + 1))); };
   const dim3 block(RN_THREADS);
   const int groups = RN_THREADS / p.lanes;
   if (p.lmax) {
@@ -456,23 +494,31 @@ int rn_forward(egnn_ctx* ctx, RnShape p, const RnForward<T>& a, hipStream_t st) 
 }
 
 template <class T, bool EVEN>
-bool rn_backward_vectors(const RnShape& p, const RnAdjoint<T>& a, int vecs, int chunks, hipStream_t st) {
+bool rn_backward_vectors(const RnShape& p, const RnSplit& s, const RnAdjoint<T>& a, int vecs, hipStream_t st) {
   constexpr int V = RvWidth<T>::V;
-  const dim3 grid(chunks, p.lmax + 1), block(RN_THREADS);
+  const dim3 grid(s.chunks * (p.lmax + 1)), block(RN_THREADS);
   const size_t lds = (size_t)RN_WAVES * vecs * V * sizeof(double);
   if (p.lmax) {
     if (p.lmax > 4 || vecs > 64) return false;
-    hipLaunchKernelGGL((rn_degrees_adjoint_kernel<T, EVEN>), grid, block, lds, st, p, a);
+    // 16-bit values in vectors of 8 bytes, as long as a wave has lanes for them: half the registers (20,000 x 25 x 64 bf16 67 us, with 16 bytes 76; fp32
+    // 119 and 113)
+    if (V == 8 && p.C <= 256) {
+      RnShape half = p;
+      half.lanes = rn_lanes((p.C + 3) / 4);
+      hipLaunchKernelGGL((rn_degrees_adjoint_kernel<T, EVEN, 4>), grid, block, lds, st, half, s, a);
+    } else {
+      hipLaunchKernelGGL((rn_degrees_adjoint_kernel<T, EVEN, V>), grid, block, lds, st, p, s, a);
+    }
   } else if (vecs <= 64) {
-    hipLaunchKernelGGL((rn_rows_adjoint_kernel<T, EVEN, 1>), grid, block, lds, st, p, a);
+    hipLaunchKernelGGL((rn_rows_adjoint_kernel<T, EVEN, 1>), grid, block, lds, st, p, s, a);
   } else if (vecs <= 128) {
-    hipLaunchKernelGGL((rn_rows_adjoint_kernel<T, EVEN, 2>), grid, block, lds, st, p, a);
+    hipLaunchKernelGGL((rn_rows_adjoint_kernel<T, EVEN, 2>), grid, block, lds, st, p, s, a);
   } else if (vecs <= 2 * RN_THREADS) {
-    hipLaunchKernelGGL((rn_wide_adjoint_kernel<T, EVEN, 2>), grid, block, RN_WAVES * sizeof(double), st, p, a);
+    hipLaunchKernelGGL((rn_wide_adjoint_kernel<T, EVEN, 2>), grid, block, RN_WAVES * sizeof(double), st, p, s, a);
   } else if (vecs <= 4 * RN_THREADS) {
-    hipLaunchKernelGGL((rn_wide_adjoint_kernel<T, EVEN, 4>), grid, block, RN_WAVES * sizeof(double), st, p, a);
+    hipLaunchKernelGGL((rn_wide_adjoint_kernel<T, EVEN, 4>), grid, block, RN_WAVES * sizeof(double), st, p, s, a);
   } else if (V == 4 && vecs <= 8 * RN_THREADS) {
-    if constexpr (V == 4) hipLaunchKernelGGL((rn_wide_adjoint_kernel<T, EVEN, 8>), grid, block, RN_WAVES * sizeof(double), st, p, a);
+    if constexpr (V == 4) hipLaunchKernelGGL((rn_wide_adjoint_kernel<T, EVEN, 8>), grid, block, RN_WAVES * sizeof(double), st, p, s, a);
   } else {
     return false;
   }
@@ -480,16 +526,16 @@ bool rn_backward_vectors(const RnShape& p, const RnAdjoint<T>& a, int vecs, int 
 }
 
 template <class T>
-int rn_backward(egnn_ctx* ctx, RnShape p, RnAdjoint<T> a, const RnSplit& s, float* dgamma, hipStream_t st) {
-  const long n = (long)(p.lmax + 1) * p.C;
+int rn_backward(egnn_ctx* ctx, RnShape p, RnAdjoint<T> a, float* dgamma, hipStream_t st) {
   const int vecs = (p.C + RvWidth<T>::V - 1) / RvWidth<T>::V, size = sizeof(T);
+  const RnSplit s = rn_split(p.n, p.lmax, p.C);
   p.lanes = rn_lanes(vecs);
-  if (s.chunks == 1) a.part = dgamma;
+  const bool alone = p.n && s.chunks == 1 && p.lmax == 0;          // one chunk: its gradient of gamma is that of all
+  if (alone) a.part = dgamma;
   const bool even = p.C % RvWidth<T>::V == 0 && rv_aligned({a.h, a.dy, a.dh, a.dx, a.gamma}, {a.hs * size, a.dys * size, a.dh ? a.dhs * size : 0, a.dxs * size});
-  if (p.n && !(even ? rn_backward_vectors<T, true>(p, a, vecs, s.chunks, st) : rn_backward_vectors<T, false>(p, a, vecs, s.chunks, st)))
-    hipLaunchKernelGGL(rn_any_adjoint_kernel<T>, dim3((unsigned)s.chunks, p.lmax + 1), dim3(RN_THREADS), 0, st, p, a);
-  if (!p.n || s.chunks > 1)
-    hipLaunchKernelGGL(rn_join_kernel, dim3((unsigned)((n + 15) / 16)), dim3(RN_JOIN), 0, st, (const float*)a.part, p.n ? s.chunks : 0, n, dgamma);
+  if (p.n && !(even ? rn_backward_vectors<T, true>(p, s, a, vecs, st) : rn_backward_vectors<T, false>(p, s, a, vecs, st)))
+    hipLaunchKernelGGL(rn_any_adjoint_kernel<T>, dim3(s.chunks * (p.lmax + 1)), dim3(RN_THREADS), 0, st, p, s, a);
+  if (!alone) hipLaunchKernelGGL(rn_join_kernel, dim3((p.C + 15) / 16, p.lmax + 1), dim3(RN_JOIN), 0, st, p, s, (const float*)a.part, dgamma);
   EGNN_LAUNCH_CHECK(ctx, "rms_norm_backward");
   return EGNN_OK;
 }
@@ -524,7 +570,7 @@ extern "C" int egnn_rms_norm(egnn_ctx* ctx, int32_t dtype, const void* x, int64_
 extern "C" int egnn_rms_norm_workspace_bytes(const egnn_ctx* ctx, int64_t n_rows, int32_t lmax, int32_t channels, size_t* bytes) {
   if (!ctx || !bytes || n_rows < 0 || n_rows > 0x7fffffff || lmax < 0 || lmax > 15 || channels < 1 || channels > 65536)
     return egnn_fail(const_cast<egnn_ctx*>(ctx), EGNN_EINVAL, "rms_norm_workspace_bytes: bad argument");
-  *bytes = rn_split(n_rows, lmax, channels).bytes;
+  *bytes = (size_t)rn_split(n_rows, lmax, channels).chunks * (lmax + 1) * channels * sizeof(float);
   return EGNN_OK;
 }
 
@@ -537,12 +583,13 @@ extern "C" int egnn_rms_norm_backward(egnn_ctx* ctx, int32_t dtype, const void* 
   if (!gamma || !dgamma || (n_rows > 0 && (!h || !dy || !dx))) return egnn_fail(ctx, EGNN_EINVAL, "rms_norm_backward: null pointer");
   if (h_stride < row || dy_stride < row || (dh && dh_stride < row) || dx_stride < row)
     return egnn_fail(ctx, EGNN_EINVAL, "rms_norm_backward: a row stride below the row's length");
-  const RnSplit s = rn_split(n_rows, lmax, channels);
-  if (!ws || (uintptr_t)ws % 256 || ws_bytes < s.bytes)
+  size_t need = 0;
+  egnn_rms_norm_workspace_bytes(ctx, n_rows, lmax, channels, &need);
+  if (!ws || (uintptr_t)ws % 256 || ws_bytes < need)
     return egnn_fail(ctx, EGNN_EWS, "rms_norm_backward: workspace too small or not 256-byte aligned");
   const RnShape p{n_rows, channels, lmax, eps, 1};
   hipStream_t st = (hipStream_t)stream;
-#define RN_CALL(T) return rn_backward<T>(ctx, p, {(const T*)h, (const T*)dy, (const T*)dh, (T*)dx, (float*)ws, h_stride, dy_stride, dh_stride, dx_stride, s.rows, gamma}, s, dgamma, st)
+#define RN_CALL(T) return rn_backward<T>(ctx, p, {(const T*)h, (const T*)dy, (const T*)dh, (T*)dx, (float*)ws, h_stride, dy_stride, dh_stride, dx_stride, gamma}, dgamma, st)
   if (dtype == EGNN_F32) RN_CALL(float);
   if (dtype == EGNN_F16) RN_CALL(_Float16);
   RN_CALL(__bf16);

@@ -1,4 +1,4 @@
-// Rows read and written in vectors of 16 bytes, whatever their length and alignment, by lanes that keep a vector as it lies in memory.
+// Rows read and written in vectors of 16 bytes (or 8), whatever their length and alignment, by lanes that keep a vector as it lies in memory.
 #pragma once
 #include "row_types.h"
 
@@ -6,9 +6,9 @@ template <class T> struct RvWidth { static constexpr int V = 16 / sizeof(T); };
 
 // EVEN: every row begins at a multiple of 16 bytes and is a multiple of 16 bytes long.  Otherwise vectors are aligned to a value only, and
 // the last one of a row may be a part, whose values go one by one.
-template <class T, bool EVEN>
+template <class T, bool EVEN, int WIDTH = RvWidth<T>::V>
 struct Rv {
-  static constexpr int V = RvWidth<T>::V;
+  static constexpr int V = WIDTH;
   typedef T vec __attribute__((ext_vector_type(V)));
   typedef vec loose __attribute__((aligned(sizeof(T))));
 
@@ -42,12 +42,10 @@ struct Rv {
   // the same for V floats beside the row
   static __device__ __forceinline__ void load_floats(const float* row, int j, int n, float (&v)[V]) {
     if constexpr (EVEN) {
-      const float4* at = (const float4*)(row + min(j, n / V - 1) * V);
+      typedef float floats __attribute__((ext_vector_type(V)));
+      const floats u = *(const floats*)(row + min(j, n / V - 1) * V);
 #pragma unroll
-      for (int i = 0; i < V; i += 4) {
-        const float4 u = at[i / 4];
-        v[i] = u.x; v[i + 1] = u.y; v[i + 2] = u.z; v[i + 3] = u.w;
-      }
+      for (int i = 0; i < V; ++i) v[i] = u[i];
     } else {
 #pragma unroll
       for (int i = 0; i < V; ++i) v[i] = row[min(j * V + i, n - 1)];
