@@ -1,0 +1,146 @@
+"""The calls of a residual block in 8 bits run together, as residual_block.py does, against the oracles' chain.
+
+Each product starts from the codes that the device made; those are checked against the values they stand for (half a step of e4m3), so that the chain has no
+tolerance but its operators' own: norm 3 U32, product 2 (18 + K / 128) U32 of the terms' magnitudes, adjoint of the norm 6 U32 of its terms' and what the
+product before it is off."""
+import numpy as np
+import pytest
+
+from oracle import block_oracle as K, residual_oracle as R
+from tests.residual_util import U32, check_codes, codes, exponents, values
+
+pytestmark = pytest.mark.gpu
+
+
+def make(lmax, channels, n, n_species, seed):
+    import torch
+    from paper_2507_03840_amd import binding as B
+    from paper_2507_03840_amd.residual_block import ResidualBlock
+    lib = B.Egnn(lmax, channels, 16, 10.0, 200.0)
+    rng = np.random.default_rng(seed)
+    species = torch.from_numpy(rng.integers(0, n_species, n).astype(np.int32)).cuda()
+    block = ResidualBlock(lib, species, n_species, seed=seed)
+    block.gamma.add_(torch.from_numpy(0.2 * rng.standard_normal(block.gamma.shape).astype(np.float32)).cuda())
+    block.bias.add_(torch.from_numpy(rng.standard_normal(block.bias.shape).astype(np.float32)).cuda()).mul_(block.degree0)
+    t = lambda: torch.from_numpy(rng.standard_normal((n, lib.dim, channels)).astype(np.float32)).cuda()
+    return lib, block, species.cpu().numpy(), t(), t(), t(), t()
+
+
+@pytest.mark.parametrize("lmax,channels,n,n_species", [(2, 16, 50, 2), (1, 32, 200, 3), (4, 64, 150, 2), (0, 128, 300, 4)])
+def test_chain(lmax, channels, n, n_species):
+    import torch
+    lib, block, species, x, r, dout, dh = make(lmax, channels, n, n_species, 7)
+    rows, gamma = n * lib.dim, values(block.gamma)
+    out, h = block.forward(x, r)
+    assert torch.equal(h, x + r)
+    ry = R.rms_norm(values(h), gamma)
+    assert (np.abs(values(block.y) - ry) <= 4 * U32 * np.abs(ry)).all()
+    _, _, q, s = lib.egnn_rms_norm(x, block.gamma, residual=r, y=False, q=None)
+    check_codes(q, s, ry.reshape(rows, channels), 3 * U32)
+    ptr, perm = K.group_rows(species, n_species, lmax)
+    w, we = R.quantise_matrices(values(block.W))
+    assert np.array_equal(codes(block.code[0]), w) and np.array_equal(codes(block.code[2]), w.transpose(0, 2, 1))
+    W = R.values_of_matrices(w, we)
+    z, size = K.grouped_linear(R.values_of_rows(codes(q).reshape(rows, channels), exponents(s).reshape(rows, -1)), W, ptr, perm, values(block.bias))
+    assert (np.abs(values(out).reshape(rows, channels) - z) <= 2 * (18 + channels / 128) * U32 * size + U32 * np.abs(z)).all()
+
+    dx, grads = block.backward(dout, dh)
+    d64 = values(dout).reshape(rows, channels)
+    dq, de, _ = R.quantise_rows(d64)
+    dy, dsize = K.grouped_linear(R.values_of_rows(dq, de), W.transpose(0, 2, 1), ptr, perm)
+    off = (2 * (18 + channels / 128) * U32 * dsize + U32 * np.abs(dy)).reshape(n, lib.dim, channels)
+    rdx, rdg, dterms, gterms = R.rms_norm_backward(values(h), dy.reshape(n, lib.dim, channels), gamma, values(dh))
+    _, _, through, goff = R.rms_norm_backward(values(h), off, gamma)                    # what the product was off, through the norm's adjoint
+    assert (np.abs(values(dx) - rdx) <= 6 * U32 * dterms + U32 * np.abs(rdx) + through).all()
+    assert (np.abs(values(grads["gamma"]) - rdg) <= 32 * U32 * gterms + goff).all()
+    _, dW, db, _, sW, sb = K.grouped_linear_backward(values(block.y).reshape(rows, channels), values(block.W), d64, ptr, perm)
+    assert (np.abs(values(grads["W"]) - dW) <= 64 * U32 * sW).all()
+    assert (np.abs(values(grads["bias"]) - db * values(block.degree0)) <= 64 * U32 * sb).all()
+    assert torch.equal(block.forward(x, r, keep=False)[0], out)
+
+
+def test_gradient_against_differences():
+    """Differences of the block without its roundings to 8 bits, in fp64.  Codes are within 2^-4 of their values (more below 2^-6 of a block's scale: 2^-10 / 448 of
+    its largest), and two of them meet in each term on the way back, one in the stored rows: a directional derivative is within (1 + 2^-4)^2 - 1 of the
+    sum of its terms' magnitudes."""
+    import torch
+    lib, block, species, x, r, dout, dh = make(1, 32, 40, 2, 11)
+    n, dim, c = x.shape
+    ptr, perm = K.group_rows(species, 2, 1)
+    block.forward(x, r)
+    dx, grads = block.backward(dout, dh)
+    rng = np.random.default_rng(1)
+    h64, g64, W64, d64, dh64 = values(x) + values(r), values(block.gamma), values(block.W), values(dout), values(dh)
+
+    def loss(h, gamma, W):
+        z, _ = K.grouped_linear(R.rms_norm(h, gamma).reshape(n * dim, c), W, ptr, perm, values(block.bias))
+        return (z.reshape(n, dim, c) * d64).sum() + (h * dh64).sum()
+
+    for _ in range(4):
+        u, v, w, t = rng.standard_normal(h64.shape), rng.standard_normal(g64.shape), rng.standard_normal(W64.shape), 1e-5
+        for a, b, e, got in ((u, 0, 0, (values(dx) * u)), (0, v, 0, (values(grads["gamma"]) * v)), (0, 0, w, (values(grads["W"]) * w))):
+            want = (loss(h64 + t * a, g64 + t * b, W64 + t * e) - loss(h64 - t * a, g64 - t * b, W64 - t * e)) / (2 * t)
+            assert abs(got.sum() - want) <= ((1 + 2.0 ** -4) ** 2 - 1) * np.abs(got).sum()
+
+
+def test_stack_and_steps():
+    """Gradients of a stack flow through every block; a step changes the weights by what the optimiser says and makes their codes again; a gradient that is
+    not finite changes nothing."""
+    import torch
+    from paper_2507_03840_amd import binding as B
+    from paper_2507_03840_amd.residual_block import ResidualStack
+    lib = B.Egnn(2, 16, 16, 10.0, 200.0)
+    species = torch.arange(60, dtype=torch.int32, device="cuda") % 2
+    stack = ResidualStack(lib, species, 2, 3, seed=5)
+    x, d = torch.randn(60, 9, 16, device="cuda"), torch.randn(60, 9, 16, device="cuda")
+    out = stack.forward(x)
+    h, v = None, x
+    for block in stack.blocks:
+        v, h = block.forward(v, h)
+    assert torch.equal(out, v + h)
+    dx, grads = stack.backward(d)
+    assert all(torch.isfinite(g).all() and g.abs().sum() > 0 for one in grads for g in one.values()) and torch.isfinite(dx).all()
+    before = [[t.clone() for t in (b.W, b.bias, b.gamma, b.momentum)] for b in stack.blocks]
+    scaled, lr = [{k: g.clone() for k, g in one.items()} for one in grads], 0.01
+    norm = stack.step(grads, lr, max_norm=0.5)
+    want = np.sqrt(sum((values(g) ** 2).sum() for one in scaled for g in one.values()))
+    assert abs(norm / want - 1) < 1e-6 and norm > 0.5
+    for block, one, (W, bias, gamma, momentum) in zip(stack.blocks, scaled, before):
+        f = 0.5 / (want + 1e-6)
+        rW, _ = K.muon_step(values(W), values(one["W"]) * f, values(momentum), lr)
+        assert np.abs(values(block.W) - rW).max() <= 1e-6
+        assert np.abs(values(block.gamma) - (values(gamma) - lr * f * values(one["gamma"]))).max() <= 1e-6
+        assert np.abs(values(block.bias) - (values(bias) - lr * f * values(one["bias"]))).max() <= 1e-6
+        fresh = lib.egnn_quantise_matrices(block.W, qt=None)
+        assert all(torch.equal(a.float(), b.float()) for a, b in zip(block.code, fresh))
+    before = [b.W.clone() for b in stack.blocks]
+    grads[1]["W"][0, 0, 0] = float("nan")
+    assert np.isnan(stack.step(grads, lr)) and all(torch.equal(b.W, w) for b, w in zip(stack.blocks, before))
+
+
+def test_captured_step_of_a_block():
+    """Forward and adjoint of a block in one graph, replayed with eager work between, against the eager calls."""
+    import torch
+    lib, block, species, x, r, dout, dh = make(2, 32, 100, 2, 13)
+    block.forward(x, r), block.backward(dout, dh)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, h = block.forward(x, r)
+        dx, grads = block.backward(dout, dh)
+        norm = lib.egnn_clip_gradients([grads["W"], grads["gamma"]], 1.0)
+    for _ in range(3):
+        x.mul_(1.2), dout.mul_(0.7)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (out, h, dx, grads["W"], grads["gamma"], grads["bias"], norm)]
+        eager_out, eager_h = block.forward(x, r)
+        eager_dx, eager = block.backward(dout, dh)
+        eager_norm = lib.egnn_clip_gradients([eager["W"], eager["gamma"]], 1.0)
+        assert all(torch.equal(a, b) for a, b in zip(got, (eager_out, eager_h, eager_dx, eager["W"], eager["gamma"], eager["bias"], eager_norm)))
+
+
+def test_training_runs():
+    from paper_2507_03840_amd.residual_block import train
+    losses, norms = train(steps=5, verbose=False)
+    assert len(losses) == 5 and np.isfinite(losses).all() and np.isfinite(norms).all()
