@@ -587,7 +587,8 @@ int egnn_muon_step(egnn_ctx* ctx, const float* W, const float* g, const float* m
  *   fp32 and fp16 results: products of codes are exact, sums fp32.  bf16 results: the 8-bit matrix instructions add products eight at a time, cut off at
  *   2^-13 of the largest of the eight (at most 2^-10 of the terms' magnitudes together; 1.5e-5 of a result's norm on normally distributed
  *   values), and these sums in fp32.  Results in less than 2^-126 may be zero.  The adjoint is the same call with the codes of dy and
- *   those of the transposed matrices (dx) and egnn_grouped_linear_backward without dx (dW, db).
+ *   those of the transposed matrices (dx) and egnn_grouped_linear_backward without dx (dW, db).  More than 2^24 tiles of 128 x 128 results (65,535 groups with
+ *   rows by 65,536 columns) are refused.
  *
  * egnn_clip_gradients: norm[0] = sqrt of the sum of the squares of all values of all tensors, norm[1] = min(1, max_norm / (norm[0] + 1e-6)) (both device),
  *   and every tensor times norm[1], rounded to its dtype, to its `out` (which may be its data).  A norm that is not finite in fp32 leaves

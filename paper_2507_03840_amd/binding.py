@@ -231,7 +231,9 @@ class TensorList:
             if t.dtype not in DTYPES:
                 raise ValueError(f"float32, float16 or bfloat16 required, not {t.dtype}")
             d.data, d.out, d.n, d.dtype = _at(t, t.shape, t.dtype), _at(o, t.shape, t.dtype), t.numel(), DTYPES[t.dtype]
-        _here(*self.tensors, *self.out)
+        self.device = self.tensors[0].get_device() if self.tensors else -1
+        if any(t.get_device() != self.device for t in (*self.tensors, *self.out)):
+            raise ValueError("tensors of one device required")
 
 
 def _f3(a):
@@ -1019,7 +1021,7 @@ class Egnn:
             raise ValueError("a TensorList says itself where results go")
         t = tensors if isinstance(tensors, TensorList) else TensorList(tensors, out)
         norm = torch.empty(2, dtype=torch.float32, device="cuda") if norm is None else norm
-        _here(norm, ws)
+        _here(norm, ws, *t.tensors[:1])
         ws, at, size = self._room(ws, self.lib.egnn_clip_gradients_workspace_bytes, C.addressof(t.desc), len(t.tensors))
         self._check(self.lib.egnn_clip_gradients(self.ctx, C.addressof(t.desc), len(t.tensors), max_norm, _at(norm, (2,)), at, size, _stream()))
         return norm

@@ -13,7 +13,7 @@ __global__ void __launch_bounds__(QT_THREADS) qt_rows_kernel(const T* x, long x_
   typedef Rv<T, EVEN> R;
   constexpr int V = R::V, BL = C8_BLOCK / V;
   const int blocks = (cols + C8_BLOCK - 1) / C8_BLOCK, vecs = (cols + V - 1) / V, lane = threadIdx.x & (lanes - 1), groups = QT_THREADS / lanes;
-  const long items = n * blocks, item0 = (long)blockIdx.x * groups * QT_AHEAD + threadIdx.x / lanes;
+  const long items = n * blocks, item0 = ((long)blockIdx.y * gridDim.x + blockIdx.x) * groups * QT_AHEAD + threadIdx.x / lanes;
   typename R::vec x_in[QT_AHEAD];
   long row[QT_AHEAD];
   int j[QT_AHEAD];
@@ -115,9 +115,10 @@ int qt_rows(egnn_ctx* ctx, const void* x, int64_t x_stride, int64_t n, int32_t c
   int lanes = 1;
   while (lanes * V < cols && lanes * V < C8_BLOCK) lanes *= 2;
   const long each = (long)QT_THREADS / lanes * QT_AHEAD, grid = (n * c8_blocks(cols) + each - 1) / each;
-  if (grid * QT_THREADS > 0xffffffffl) return egnn_fail(ctx, EGNN_EINVAL, "quantise_rows: more than 2^32 threads' worth of values");
+  // (folded where more than 2^32 threads would go along one axis)
+  const dim3 blocks = grid < 1l << 23 ? dim3((unsigned)grid) : dim3(1u << 23, (unsigned)((grid + (1l << 23) - 1) >> 23));
   const bool even = cols % V == 0 && rv_aligned({x}, {x_stride * (int64_t)sizeof(T)});
-#define QT_CALL(E) hipLaunchKernelGGL((qt_rows_kernel<T, E>), dim3((unsigned)grid), dim3(QT_THREADS), 0, st, (const T*)x, (long)x_stride, (long)n, cols, lanes, \
+#define QT_CALL(E) hipLaunchKernelGGL((qt_rows_kernel<T, E>), blocks, dim3(QT_THREADS), 0, st, (const T*)x, (long)x_stride, (long)n, cols, lanes, \
                                       (uint8_t*)q, (long)q_stride, (uint8_t*)scale)
   if (even) QT_CALL(true); else QT_CALL(false);
 #undef QT_CALL

@@ -53,8 +53,12 @@ __device__ __forceinline__ double rn_row_sum(double v, int lanes, double* lds) {
   return v;
 }
 
+// Number of a workgroup: a grid of more than 2^23 is folded, as no more than 2^32 threads go along one axis
+__device__ __forceinline__ long rn_block() { return (long)blockIdx.y * gridDim.x + blockIdx.x; }
+dim3 rn_grid(long blocks) { return blocks < 1l << 23 ? dim3((unsigned)blocks) : dim3(1u << 23, (unsigned)((blocks + (1l << 23) - 1) >> 23)); }
+
 // Degree of a workgroup: workgroups go through the degrees of a run of rows, the longest first, before the next rows, so that short ones run beside long ones
-__device__ __forceinline__ int rn_degree(const RnShape& p) { return p.lmax - (int)(blockIdx.x % (p.lmax + 1)); }
+__device__ __forceinline__ int rn_degree(const RnShape& p) { return p.lmax - (int)(rn_block() % (p.lmax + 1)); }
 
 // U rows at a time of one degree, PL planes each, by `lanes` lanes with NV vectors of a plane each (WIDE: by the workgroup).  All of them are
 // read before anything is written.
@@ -65,7 +69,7 @@ __device__ __forceinline__ void rn_write(const RnShape& p, const RnForward<T>& a
   __shared__ double lds[RN_WAVES];
   const int lanes = WIDE ? RN_THREADS : p.lanes, lane = threadIdx.x & (lanes - 1), groups = RN_THREADS / lanes, C = p.C;
   const int dim = (p.lmax + 1) * (p.lmax + 1), vecs = (C + V - 1) / V, blocks = (C + C8_BLOCK - 1) / C8_BLOCK;
-  const long row0 = (long)(blockIdx.x / (p.lmax + 1)) * groups * U + threadIdx.x / lanes;
+  const long row0 = rn_block() / (p.lmax + 1) * groups * U + threadIdx.x / lanes;
   typename R::vec h[U][PL][NV];
 #pragma unroll
   for (int u = 0; u < U; ++u)
@@ -165,7 +169,7 @@ __device__ __forceinline__ float rn_sum(const RnForward<T>& a, long row, int at)
 template <class T>
 __global__ void __launch_bounds__(RN_WAVES * 64) rn_any_kernel(RnShape p, RnForward<T> a) {
   const int lane = threadIdx.x & 63, degrees = p.lmax + 1;
-  const long item = (long)blockIdx.x * RN_WAVES + (threadIdx.x >> 6);
+  const long item = rn_block() * RN_WAVES + (threadIdx.x >> 6);
   if (item >= p.n * degrees) return;
   const long row = item / degrees;
   const int l = (int)(item % degrees), first = l * l, last = (l + 1) * (l + 1), dim = degrees * degrees, C = p.C;
@@ -212,7 +216,7 @@ template <class T>
 struct RnAdjoint {
   const T *h, *dy, *dh;   // dh may be NULL
   T* dx;
-  float* part;            // [chunks][lmax + 1][C], the highest degree first
+  float* part;            // [chunks][lmax + 1][C], the highest degree first; doubles where rows are added there one by one
   long hs, dys, dhs, dxs;
   const float* gamma;
 };
@@ -378,7 +382,7 @@ __global__ void __launch_bounds__(RN_THREADS) rn_degrees_adjoint_kernel(RnShape 
   }
 }
 
-// A workgroup for a chunk of rows and a degree: its waves take the rows in turn.  The gradient of gamma is added in LDS a row after the other by
+// A workgroup for a chunk of rows and a degree, of any sizes: its waves take the rows in turn.  The gradient of gamma is added a row after the other by
 // the wave whose turn it is.
 template <class T>
 __global__ void __launch_bounds__(RN_WAVES * 64) rn_any_adjoint_kernel(RnShape p, RnSplit s, RnAdjoint<T> a) {
@@ -410,8 +414,8 @@ __global__ void __launch_bounds__(RN_WAVES * 64) rn_any_adjoint_kernel(RnShape p
           if (a.dh) v += (double)(float)a.dh[row * a.dhs + plane * C + c];
           a.dx[row * a.dxs + plane * C + c] = (T)(float)v;
         }
-        float* at = a.part + (long)blockIdx.x * C + c;
-        *at = (row == begin ? 0.0f : *at) + (float)dg;
+        double* at = (double*)a.part + (long)blockIdx.x * C + c;
+        *at = (row == begin ? 0.0 : *at) + dg;
       }
     }
   }
@@ -419,13 +423,14 @@ __global__ void __launch_bounds__(RN_WAVES * 64) rn_any_adjoint_kernel(RnShape p
 
 // Adds the chunks' gradients of gamma: 16 channels of a degree a workgroup, each by 32 threads that take the chunks in turn, four of them under way
 constexpr int RN_JOIN = 512, RN_JOIN_TURNS = RN_JOIN / 16;
-__global__ void __launch_bounds__(RN_JOIN) rn_join_kernel(RnShape p, RnSplit s, const float* part, float* dgamma) {
+template <class P>
+__global__ void __launch_bounds__(RN_JOIN) rn_join_kernel(RnShape p, RnSplit s, const P* part, float* dgamma) {
   __shared__ double lds[RN_JOIN_TURNS][17];
   const int l = blockIdx.y, c = min((int)blockIdx.x * 16 + (int)(threadIdx.x & 15), p.C - 1), turn = threadIdx.x >> 4;
   const int end = p.n ? s.chunks : 0;
   double sum = 0.0;
   for (int k = turn; k < end; k += 4 * RN_JOIN_TURNS) {
-    float v[4];
+    P v[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) v[u] = part[((long)min(k + u * RN_JOIN_TURNS, end - 1) * (p.lmax + 1) + p.lmax - l) * p.C + c];
 #pragma unroll
@@ -458,7 +463,7 @@ int rn_lanes(int vecs) {
 
 template <class T, bool EVEN>
 bool rn_forward_vectors(const RnShape& p, const RnForward<T>& a, int vecs, hipStream_t st) {
-  auto rows = [&](int groups) { return dim3((unsigned)((p.n + groups - 1) / groups * (p.lmax + 1))); };
+  auto rows = [&](int groups) { return rn_grid((p.n + groups - 1) / groups * (p.lmax + 1)); };
   const dim3 block(RN_THREADS);
   const int groups = RN_THREADS / p.lanes;
   if (p.lmax) {
@@ -487,7 +492,7 @@ int rn_forward(egnn_ctx* ctx, RnShape p, const RnForward<T>& a, hipStream_t st) 
   const bool even = p.C % RvWidth<T>::V == 0 && rv_aligned({a.x, a.r, a.h, a.y, a.gamma}, {a.xs * size, a.r ? a.rs * size : 0, a.h ? a.hs * size : 0, a.y ? a.ys * size : 0});
   if (!(even ? rn_forward_vectors<T, true>(p, a, vecs, st) : rn_forward_vectors<T, false>(p, a, vecs, st))) {
     const long items = p.n * (p.lmax + 1);
-    hipLaunchKernelGGL(rn_any_kernel<T>, dim3((unsigned)((items + RN_WAVES - 1) / RN_WAVES)), dim3(RN_THREADS), 0, st, p, a);
+    hipLaunchKernelGGL(rn_any_kernel<T>, rn_grid((items + RN_WAVES - 1) / RN_WAVES), dim3(RN_THREADS), 0, st, p, a);
   }
   EGNN_LAUNCH_CHECK(ctx, "rms_norm");
   return EGNN_OK;
@@ -531,11 +536,16 @@ int rn_backward(egnn_ctx* ctx, RnShape p, RnAdjoint<T> a, float* dgamma, hipStre
   const RnSplit s = rn_split(p.n, p.lmax, p.C);
   p.lanes = rn_lanes(vecs);
   const bool alone = p.n && s.chunks == 1 && p.lmax == 0;          // one chunk: its gradient of gamma is that of all
-  if (alone) a.part = dgamma;
   const bool even = p.C % RvWidth<T>::V == 0 && rv_aligned({a.h, a.dy, a.dh, a.dx, a.gamma}, {a.hs * size, a.dys * size, a.dh ? a.dhs * size : 0, a.dxs * size});
-  if (p.n && !(even ? rn_backward_vectors<T, true>(p, s, a, vecs, st) : rn_backward_vectors<T, false>(p, s, a, vecs, st)))
+  RnAdjoint<T> direct = a;
+  if (alone) direct.part = dgamma;
+  const dim3 join((p.C + 15) / 16, p.lmax + 1);
+  if (!p.n || (even ? rn_backward_vectors<T, true>(p, s, direct, vecs, st) : rn_backward_vectors<T, false>(p, s, direct, vecs, st))) {
+    if (!alone) hipLaunchKernelGGL(rn_join_kernel<float>, join, dim3(RN_JOIN), 0, st, p, s, (const float*)a.part, dgamma);
+  } else {
     hipLaunchKernelGGL(rn_any_adjoint_kernel<T>, dim3(s.chunks * (p.lmax + 1)), dim3(RN_THREADS), 0, st, p, s, a);
-  if (!alone) hipLaunchKernelGGL(rn_join_kernel, dim3((p.C + 15) / 16, p.lmax + 1), dim3(RN_JOIN), 0, st, p, s, (const float*)a.part, dgamma);
+    hipLaunchKernelGGL(rn_join_kernel<double>, join, dim3(RN_JOIN), 0, st, p, s, (const double*)a.part, dgamma);
+  }
   EGNN_LAUNCH_CHECK(ctx, "rms_norm_backward");
   return EGNN_OK;
 }
@@ -570,7 +580,7 @@ extern "C" int egnn_rms_norm(egnn_ctx* ctx, int32_t dtype, const void* x, int64_
 extern "C" int egnn_rms_norm_workspace_bytes(const egnn_ctx* ctx, int64_t n_rows, int32_t lmax, int32_t channels, size_t* bytes) {
   if (!ctx || !bytes || n_rows < 0 || n_rows > 0x7fffffff || lmax < 0 || lmax > 15 || channels < 1 || channels > 65536)
     return egnn_fail(const_cast<egnn_ctx*>(ctx), EGNN_EINVAL, "rms_norm_workspace_bytes: bad argument");
-  *bytes = (size_t)rn_split(n_rows, lmax, channels).chunks * (lmax + 1) * channels * sizeof(float);
+  *bytes = (size_t)rn_split(n_rows, lmax, channels).chunks * (lmax + 1) * channels * sizeof(double);
   return EGNN_OK;
 }
 

@@ -317,6 +317,7 @@ __global__ void __launch_bounds__(SL_WAVES * 64, SIDE == 256 ? 1 : TWO || !__is_
   __shared__ __attribute__((aligned(1024))) uint8_t b0[ROOM], b1[TWO ? BUFFER : 16];
   __shared__ __attribute__((aligned(16))) uint8_t le0[SIDE], le1[SIDE];
   __shared__ int rows[SIDE];
+  __shared__ __attribute__((aligned(16))) float bias[SIDE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane & 31, half = lane >> 5, wr = wave >> 1, wn = wave & 1;
   long row_tile;
   int col_tile;
@@ -373,11 +374,13 @@ __global__ void __launch_bounds__(SL_WAVES * 64, SIDE == 256 ? 1 : TWO || !__is_
 
   // (of the blocks 0 and 1)
   const int scale0 = scale_at[0];
+  const float bias0 = p.bias ? p.bias[(long)t.g * p.N + min(n0 + mine, p.N - 1)] : 0.0f;
   int scale = scale_at[block_at(1)], ew = wscale_at[0], ew_next = wscale_at[block_at(1)];
   stage(b0, 0);
   if constexpr (TWO) stage(b1, 1);
   rows[mine] = (int)sl_row(p, min(t.begin + mine, t.end - 1));
   le0[scale_to] = (uint8_t)scale0;
+  bias[mine] = bias0;
   __builtin_amdgcn_s_waitcnt(SL_VMCNT(TWO ? 2 * LOADS : 0));        // the first block
   sl_barrier();
   unsigned eq = scales(le0), eq_next = eq;
@@ -479,10 +482,9 @@ __global__ void __launch_bounds__(SL_WAVES * 64, SIDE == 256 ? 1 : TWO || !__is_
   for (int i = 0; i < F; ++i)
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const int col = 32 * i + 8 * k + 4 * half, n = n0 + wn * COLS + col;
-      float b[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) b[e] = p.bias ? p.bias[(long)t.g * p.N + min(n + e, p.N - 1)] : 0.0f;
+      const int col = 32 * i + 8 * k + 4 * half;
+      const float4 b4 = *(const float4*)(bias + wn * COLS + col);
+      const float b[4] = {b4.x, b4.y, b4.z, b4.w};
 #pragma unroll
       for (int r = 0; r < F; ++r) {
         four u;

@@ -200,6 +200,11 @@ def test_many_rows(m):
     _, dg = m.egnn_rms_norm_backward(h, dy, g)
     _, want, _, _ = R.rms_norm_backward(values(h), values(dy), np.ones((1, c)))
     assert np.abs(values(dg) / want - 1).max() <= 32 * U32
+    for lmax, c in ((5, 3), (4, 7), (1, 300)):
+        h, dy = (torch.rand(20001, (lmax + 1) ** 2, c, device="cuda") + 1 for _ in range(2))
+        _, dg = m.egnn_rms_norm_backward(h, dy, torch.ones(lmax + 1, c, device="cuda"))
+        _, want, _, _ = R.rms_norm_backward(values(h), values(dy), np.ones((lmax + 1, c)))
+        assert np.abs(values(dg) / want - 1).max() <= 32 * U32
 
 
 def test_gradient_against_differences(m):
