@@ -42,7 +42,7 @@ def check(m, g, most):
         assert torch.equal(t, o)
 
 
-SIZES = [[1], [5], [0, 3, 0], [16384], [16385, 1, 16383], [100000, 7], [1023, 64, 64, 300001], [3, 70001, 5000, 1, 1, 2]]
+SIZES = [[1], [5], [0, 3, 0], [16380, 4], [4000, 4096, 1, 5000], [16384], [16385, 1, 16383], [100000, 7], [1023, 64, 64, 300001], [3, 70001, 5000, 1, 1, 2]]
 
 
 @pytest.mark.parametrize("types", [["float32"], ["float16"], ["bfloat16"], ["bfloat16", "float32", "float16"]])
