@@ -22,7 +22,7 @@ __global__ void __launch_bounds__(QT_THREADS) qt_rows_kernel(const T* x, long x_
     const long item = min(item0 + u * groups, items - 1);
     row[u] = blocks == 1 ? item : item <= 0xffffffffl ? (long)((unsigned)item / (unsigned)blocks) : item / blocks;
     j[u] = (int)(item - row[u] * blocks) * BL + lane;
-    x_in[u] = R::load(x + row[u] * x_stride, j[u], cols);
+    x_in[u] = R::load_any(x + row[u] * x_stride, j[u], cols);
   }
 #pragma unroll
   for (int u = 0; u < QT_AHEAD; ++u) {
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(QT_THREADS) qt_matrix_kernel(QtMatrices p, con
   const int rows = (int)min((long)C8_BLOCK, p.rows - r0), cols = (int)min((long)C8_BLOCK, p.cols - c0);
   typename R::vec in[EACH];
 #pragma unroll
-  for (int i = 0; i < EACH; ++i) in[i] = R::load(W + (b * p.rows + r0 + min(r + i * STEP, rows - 1)) * p.cols + c0, j, cols);
+  for (int i = 0; i < EACH; ++i) in[i] = R::load_any(W + (b * p.rows + r0 + min(r + i * STEP, rows - 1)) * p.cols + c0, j, cols);
   const bool whole = j * V < cols;          // (EVEN has the last vector again behind the end; it adds nothing to the largest magnitude)
   unsigned m = 0;
 #pragma unroll

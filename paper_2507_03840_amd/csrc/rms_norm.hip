@@ -14,7 +14,6 @@
 
 namespace {
 
-constexpr int RN_WIDE_ROWS = 1024;    // from so many rows on a wave takes a row of up to 512 vectors, below it a workgroup
 constexpr int RN_SHORT = 32;           // up to so many values the adjoint's differences are fp64
 constexpr int RN_THREADS = 256, RN_WAVES = RN_THREADS / 64;
 
@@ -466,17 +465,22 @@ bool rn_forward_vectors(const RnShape& p, const RnForward<T>& a, int vecs, hipSt
   auto rows = [&](int groups) { return rn_grid((p.n + groups - 1) / groups * (p.lmax + 1)); };
   const dim3 block(RN_THREADS);
   const int groups = RN_THREADS / p.lanes;
+  if (p.C < RvWidth<T>::V) return false;
   if (p.lmax) {
     if (p.lmax > 4 || vecs > 64) return false;
     hipLaunchKernelGGL((rn_degrees_kernel<T, EVEN>), rows(groups), block, 0, st, p, a);
   } else if (vecs <= 64) {
     hipLaunchKernelGGL((rn_rows_kernel<T, EVEN, 1>), rows(groups * 4), block, 0, st, p, a);
-  } else if (vecs <= 512 && p.n >= RN_WIDE_ROWS) {
-    if (vecs <= 128) hipLaunchKernelGGL((rn_rows_kernel<T, EVEN, 2>), rows(groups), block, 0, st, p, a);
-    else if (vecs <= 256) hipLaunchKernelGGL((rn_rows_kernel<T, EVEN, 4>), rows(groups), block, 0, st, p, a);
-    else hipLaunchKernelGGL((rn_rows_kernel<T, EVEN, 8>), rows(groups), block, 0, st, p, a);
+  // a wave up to 256 vectors, a workgroup above (20,000 rows bf16 with codes, wave : workgroup, 128 vectors 28 : 46 us, 256 56 : 59, 512 114 : 102;
+  // 64 to 2,048 rows of 128 or 256 within 5 %)
+  } else if (vecs <= 128) {
+    hipLaunchKernelGGL((rn_rows_kernel<T, EVEN, 2>), rows(groups), block, 0, st, p, a);
+  } else if (vecs <= 256) {
+    hipLaunchKernelGGL((rn_rows_kernel<T, EVEN, 4>), rows(groups), block, 0, st, p, a);
   } else if (vecs <= 2 * RN_THREADS) {
     hipLaunchKernelGGL((rn_wide_kernel<T, EVEN, 2>), rows(1), block, 0, st, p, a);
+  } else if (vecs <= 4 * RN_THREADS) {
+    hipLaunchKernelGGL((rn_wide_kernel<T, EVEN, 4>), rows(1), block, 0, st, p, a);
   } else if (vecs <= 8 * RN_THREADS) {
     hipLaunchKernelGGL((rn_wide_kernel<T, EVEN, 8>), rows(1), block, 0, st, p, a);
   } else {
@@ -503,6 +507,7 @@ bool rn_backward_vectors(const RnShape& p, const RnSplit& s, const RnAdjoint<T>&
   constexpr int V = RvWidth<T>::V;
   const dim3 grid(s.chunks * (p.lmax + 1)), block(RN_THREADS);
   const size_t lds = (size_t)RN_WAVES * vecs * V * sizeof(double);
+  if (p.C < V) return false;
   if (p.lmax) {
     if (p.lmax > 4 || vecs > 64) return false;
     // 16-bit values in vectors of 8 bytes, as long as a wave has lanes for them: half the registers (20,000 x 25 x 64 bf16 67 us, with 16 bytes 76; fp32

@@ -4,8 +4,20 @@
 
 template <class T> struct RvWidth { static constexpr int V = 16 / sizeof(T); };
 
+// v moved down by `by` words, zeros behind (any by >= 0; words moved by 1, 2 and 4 of them, each where its bit is set)
+template <int W>
+__device__ __forceinline__ void rv_move_words(unsigned (&v)[W], int by) {
+#pragma unroll
+  for (int step = 1; step < W; step *= 2)
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = by & step ? (i + step < W ? v[i + step] : 0u) : v[i];
+#pragma unroll
+  for (int i = 0; i < W; ++i) v[i] = by >= W ? 0u : v[i];
+}
+
 // EVEN: every row begins at a multiple of 16 bytes and is a multiple of 16 bytes long.  Otherwise vectors are aligned to a value only, and
-// the last one of a row may be a part, whose values go one by one.
+// the last one of a row may be a part: the row's last V values are read in its place and moved down by the values too many (loads are never under a
+// condition, as they would be waited for one by one); what is written of it goes value by value.  Rows of V values at least, but for load_any.
 template <class T, bool EVEN, int WIDTH = RvWidth<T>::V>
 struct Rv {
   static constexpr int V = WIDTH;
@@ -17,16 +29,30 @@ struct Rv {
     if constexpr (EVEN) {
       return *(const vec*)(row + min(j, n / V - 1) * V);
     } else {
-      vec v = {};
-      if ((j + 1) * V <= n) {
-        v = *(const loose*)(row + j * V);
-      } else {
+      constexpr int W = V * (int)sizeof(T) / 4;
+      const int at = min(j * V, n - V), over = j * V - at;
+      const loose u = *(const loose*)(row + at);
+      unsigned w[W];
+      __builtin_memcpy(w, &u, sizeof(w));
+      if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-          if (j * V + i < n) v[i] = row[j * V + i];
+        for (int i = 0; i < W; ++i) w[i] = over & 1 ? __builtin_amdgcn_alignbit(i + 1 < W ? w[i + 1] : 0u, w[i], 16) : w[i];
+        rv_move_words(w, over >> 1);
+      } else {
+        rv_move_words(w, over);
       }
+      vec v;
+      __builtin_memcpy(&v, w, sizeof(w));
       return v;
     }
+  }
+  static __device__ __forceinline__ vec load_any(const T* row, int j, int n) {
+    if (EVEN || n >= V) return load(row, j, n);
+    vec v = {};
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (j * V + i < n) v[i] = row[j * V + i];
+    return v;
   }
   static __device__ __forceinline__ void store(T* row, int j, int n, const vec& v) {
     if constexpr (EVEN) {
@@ -47,8 +73,14 @@ struct Rv {
 #pragma unroll
       for (int i = 0; i < V; ++i) v[i] = u[i];
     } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = row[min(j * V + i, n - 1)];
+      typedef float floats __attribute__((ext_vector_type(V)));
+      typedef floats loose_floats __attribute__((aligned(4)));
+      const int at = min(j * V, n - V);
+      const loose_floats u = *(const loose_floats*)(row + at);
+      unsigned w[V];
+      __builtin_memcpy(w, &u, sizeof(w));
+      rv_move_words(w, j * V - at);
+      __builtin_memcpy(v, w, sizeof(w));
     }
   }
 };
