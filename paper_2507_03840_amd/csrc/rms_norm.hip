@@ -206,7 +206,8 @@ RnSplit rn_split(int64_t n, int lmax, int C) {
   const long most = lmax ? 2048l / (lmax + 1) : 1024;
   RnSplit s;
   s.rows = std::max<long>(std::max<long>((n + most - 1) / most, 4096l / C), 1);
-  if (s.rows > 16) s.rows = (s.rows + 15) / 16 * 16;
+  const long whole = C >= 256 ? 4 : 16;          // rows that a workgroup takes at once, or a part of them
+  if (s.rows > whole) s.rows = (s.rows + whole - 1) / whole * whole;
   s.chunks = n ? (int)((n + s.rows - 1) / s.rows) : 1;
   return s;
 }
