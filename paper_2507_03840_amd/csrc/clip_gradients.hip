@@ -7,6 +7,9 @@
 // Two launches: pieces of the tensors are summed, each workgroup to a slot of its own; then every workgroup adds all slots, in the
 // same order, and scales its pieces.  No atomics: the same bits every time.  The tensors' addresses travel as kernel arguments, so that a call
 // copies nothing from host memory and can be captured; CG_TENSORS of them at a time.
+//
+// What bounds it is memory: the bound needs all gradients before the first is scaled, so they are read twice.  Measured: 100 M fp32 values to another place
+// 65 + 146 us (6.2 and 5.5 TB/s), 24 tensors of together 417,000 values 4.8 + 5.3.
 #include <algorithm>
 #include "row_vectors.h"
 

@@ -1,5 +1,8 @@
 // Rows and matrices to 8-bit codes (codes8.h): a scale for every 128 columns of a row, or for every 128 x 128 values of a matrix, whose
 // codes are also written transposed for the product of the way back.
+//
+// What bounds both is memory: everything is read once, into registers.  Measured: 300,000 x 64 fp32 rows 17.8 us (5.4 TB/s); 16 x 1024 x 512 fp32
+// matrices, both orders, 10.8 (512 workgroups of 128 x 128 values, 4.7 TB/s).
 #include "codes8.h"
 #include "row_vectors.h"
 

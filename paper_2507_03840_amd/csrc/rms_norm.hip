@@ -8,6 +8,13 @@
 //   dx = dh + rho (d - h rho^2 sum(d h) / L),  dgamma_{l,c} = sum over rows and m of dy h rho.
 // Sums over a row are fp64: squares of any fp32 value stay finite.  The two terms of dx, which cancel in short rows (for one value all but
 // eps rho^2 of them), are subtracted in fp64 in rows of up to 32 values, from a rho that is made again from h; in longer ones in fp32.
+//
+// What bounds it is memory: a row is read once, into registers, and written from there.  Short rows share a wave (a power of two of lanes each, four rows
+// under way), long ones have a wave or a workgroup; a degree is a row of its own, with all its planes on their way together.
+//
+// Measured: 2,350,179 x 64 bf16 with the residual, sum and codes out, 189 us (5.6 TB/s); 20,000 x 25 x 64 fp32, sum and y out, 87 (5.9); 20,000 x 1024
+// bf16 29 (5.6); 64 x 9 x 16 fp32 4.0.  The adjoint with the gradient from besides 122 (4.2 TB/s), and 37 (4.4), then 5 to join the chunks' gradients of
+// gamma: reading three tensors and writing one, it stays there with 8 or 16 bytes a lane, two to five waves a SIMD, one turn or many a workgroup.
 #include <algorithm>
 #include "codes8.h"
 #include "row_vectors.h"

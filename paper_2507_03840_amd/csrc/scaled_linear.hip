@@ -126,7 +126,7 @@ __device__ __forceinline__ void sl_item(long block, long items, int tiles_n, int
 constexpr int SL_WAVES = 4, SL_DOWN = 4;
 
 // ---- few rows -----------------------------------------------------------------------------------------------------------------
-// What bounds it is reading W once.  A workgroup makes 16 columns of up to 16 R rows; its waves take the blocks of k in turn, SL_AHEAD of them under way
+// What bounds it is reading W once (one row of 2048 by 4096 bf16 4.4 us for 8.4 MB: launch and a chain of two loads as much as memory).  A workgroup makes 16 columns of up to 16 R rows; its waves take the blocks of k in turn, SL_AHEAD of them under way
 // in each, and add up through LDS in the order of the waves.
 constexpr int SL_FEW = 8, SL_AHEAD = 4;
 template <class T, int R>
@@ -179,7 +179,8 @@ __global__ void __launch_bounds__(SL_FEW * 64) sl_few_kernel(SlArgs p) {
 
 // ---- many rows, one block of k ------------------------------------------------------------------------------------------------
 // Up to 128 of k and 32 F columns: what bounds it is memory, the rows in and out.  W stays in registers (H turns of 64 of k) while a wave takes a run of
-// 32-row tiles in the order by group, the next one's codes and the row numbers of the one after that under way.
+// 32-row tiles in the order by group, the next one's codes and the row numbers of the one after that under way.  Measured: 300,000 x 64 by 64 fp32 18.4 us
+// (5.2 TB/s), in 15 groups of rows in any order 20 to 24 (rows of 64 bytes are half a line each).
 struct SlWalk { int g; long at, end; };
 __device__ __forceinline__ SlWalk sl_next(const SlArgs& p, SlWalk t) {
   t.at += 32;
@@ -283,7 +284,9 @@ __global__ void __launch_bounds__(SL_WAVES * 64) sl_rows_kernel(SlArgs p, long s
 // A workgroup of four waves makes SIDE x SIDE results, a quarter each; a turn takes 64 of k, a block of 128 two turns.  Rows of both operands go
 // straight from memory to LDS, a block's 128 bytes of a row at once (16 bytes a lane), into one of two buffers, and from there to registers one turn ahead:
 // while a turn's products run, the next one's operands are read.  One barrier a block: behind it the next block is in LDS, and nobody reads this
-// one's buffer any more, so that the block after the next can be asked for.  A row's eight pieces of 16 bytes lie at (piece xor row / 2), so that 16 rows read
+// one's buffer any more, so that the block after the next can be asked for.  (Measured, 8192 x 4096 by 4096 bf16: 115 us, 2,390 TFLOP/s, matrix units 65 %
+// busy; with 64 bytes of a row at a time, four buffers and three turns ahead 152, as L2 has twice the requests; without the order of instructions
+// below 167; eight waves and no reading ahead 146.  With one buffer, three workgroups of 128 x 128 a compute unit: 20,000 x 512 by 1024 in 16 groups 27.)  A row's eight pieces of 16 bytes lie at (piece xor row / 2), so that 16 rows read
 // at once lie in all 64 banks.
 typedef __attribute__((address_space(3))) uint8_t sl_lds;
 typedef const __attribute__((address_space(1))) uint8_t sl_global;
