@@ -578,6 +578,9 @@ extern "C" int egnn_rms_norm(egnn_ctx* ctx, int32_t dtype, const void* x, int64_
   if (n_rows > 0 && h && h == y) return egnn_fail(ctx, EGNN_EINVAL, "rms_norm: h and y are two outputs");
   if (x_stride < row || (r && r_stride < row) || (h && h_stride < row) || (y && y_stride < row))
     return egnn_fail(ctx, EGNN_EINVAL, "rms_norm: a row stride below the row's length");
+  if (n_rows > 1 && ((h && ((h == x && h_stride != x_stride) || (h == r && h_stride != r_stride))) ||
+      (y && ((y == x && y_stride != x_stride) || (r && y == r && y_stride != r_stride)))))
+    return egnn_fail(ctx, EGNN_EINVAL, "rms_norm: a result in the place of an operand has its row stride");
   if (q && (q_stride < channels || q_stride % 16 || (uintptr_t)q % 16))
     return egnn_fail(ctx, EGNN_EINVAL, "rms_norm: rows of codes begin at multiples of 16 bytes");
   if (n_rows == 0) return EGNN_OK;
@@ -606,6 +609,8 @@ extern "C" int egnn_rms_norm_backward(egnn_ctx* ctx, int32_t dtype, const void* 
   if (!gamma || !dgamma || (n_rows > 0 && (!h || !dy || !dx))) return egnn_fail(ctx, EGNN_EINVAL, "rms_norm_backward: null pointer");
   if (h_stride < row || dy_stride < row || (dh && dh_stride < row) || dx_stride < row)
     return egnn_fail(ctx, EGNN_EINVAL, "rms_norm_backward: a row stride below the row's length");
+  if (n_rows > 1 && ((dx == h && dx_stride != h_stride) || (dx == dy && dx_stride != dy_stride) || (dh && dx == dh && dx_stride != dh_stride)))
+    return egnn_fail(ctx, EGNN_EINVAL, "rms_norm_backward: a result in the place of an operand has its row stride");
   size_t need = 0;
   egnn_rms_norm_workspace_bytes(ctx, n_rows, lmax, channels, &need);
   if (!ws || (uintptr_t)ws % 256 || ws_bytes < need)

@@ -31,14 +31,16 @@ ADJOINT = dict(dtype=BF16, h=P, hs=288, dy=P, dys=288, dh=P, dhs=288, n=10, lmax
 @pytest.mark.parametrize("change", [
     dict(dtype=3), dict(dtype=-1), dict(x=None), dict(xs=287), dict(rs=287), dict(n=-1), dict(n=2 ** 31), dict(lmax=-1), dict(lmax=16), dict(c=0),
     dict(c=65537), dict(gamma=None), dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(hs=287), dict(ys=287),
-    dict(h=P, r=None), dict(h=P, y=P), dict(y=None, q=None, scale=None), dict(q=None), dict(scale=None), dict(qs=31), dict(qs=40), dict(q=P + 8)])
+    dict(h=P, r=None), dict(h=P, y=P), dict(y=None, q=None, scale=None), dict(q=None), dict(scale=None), dict(qs=31), dict(qs=40), dict(q=P + 8),
+    dict(h=P, hs=300), dict(y=P, ys=300, h=None), dict(r=4 * P, y=4 * P, ys=289)])
 def test_rms_norm(m, change):
     refused(m, "egnn_rms_norm", NORM, EINVAL, **change)
 
 
 def test_rms_norm_backward(m):
     for change in (dict(dtype=3), dict(h=None), dict(dy=None), dict(dx=None), dict(dg=None), dict(gamma=None), dict(hs=287), dict(dys=287), dict(dhs=0),
-                   dict(dxs=287), dict(n=-1), dict(n=2 ** 31), dict(lmax=-1), dict(lmax=16), dict(c=0), dict(c=65537), dict(eps=0.0)):
+                   dict(dxs=287), dict(n=-1), dict(n=2 ** 31), dict(lmax=-1), dict(lmax=16), dict(c=0), dict(c=65537), dict(eps=0.0), dict(dxs=300),
+                   dict(dx=2 * P, dy=2 * P, dys=300), dict(dx=2 * P, dh=2 * P, dhs=290)):
         refused(m, "egnn_rms_norm_backward", ADJOINT, EINVAL, **change)
     for change in (dict(ws=None), dict(ws=P + 16), dict(size=100)):
         refused(m, "egnn_rms_norm_backward", ADJOINT, EWS, **change)
@@ -146,3 +148,13 @@ def test_places_of_codes():
         assert q.shape == (3, 4, n) and q.stride() == (4 * (-(-n // 16) * 16), -(-n // 16) * 16, 1) and s.shape == (3, 4, -(-n // 128))
         w, ws = B.empty_matrix_codes((2, 130, n), "cpu")
         assert w.stride() == (130 * (-(-n // 16) * 16), -(-n // 16) * 16, 1) and ws.shape == (2, 2, -(-n // 128))
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    from types import SimpleNamespace
+    from paper_2507_03840_amd import binding as B
+    monkeypatch.setattr(B, "_device", lambda: 0)
+    on = lambda k: SimpleNamespace(get_device=lambda: k, device=f"cuda:{k}")
+    B._here(on(0), None, False, on(0), on(-1))
+    with pytest.raises(ValueError, match="cuda:1"):
+        B._here(on(0), None, on(1))
