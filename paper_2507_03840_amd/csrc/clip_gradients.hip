@@ -144,7 +144,8 @@ int cg_check(egnn_ctx* ctx, const char* who, const egnn_tensor* t, int32_t count
   for (int32_t i = 0; i < count; ++i) {
     if (!rt_size(t[i].dtype)) return egnn_fail(ctx, EGNN_EINVAL, at + ": dtype must be EGNN_F32, EGNN_F16 or EGNN_BF16");
     if (t[i].n < 0 || t[i].n > ((int64_t)1 << 40)) return egnn_fail(ctx, EGNN_EINVAL, at + ": the values of a tensor must be in 0..2^40");
-    if (t[i].n > 0 && (!t[i].data || !t[i].out)) return egnn_fail(ctx, EGNN_EINVAL, at + ": null pointer");
+    if (!t[i].n) continue;
+    if (!t[i].data || !t[i].out) return egnn_fail(ctx, EGNN_EINVAL, at + ": null pointer");
     if ((uintptr_t)t[i].data % rt_size(t[i].dtype) || (uintptr_t)t[i].out % rt_size(t[i].dtype))
       return egnn_fail(ctx, EGNN_EINVAL, at + ": a tensor that is not aligned to its values");
   }

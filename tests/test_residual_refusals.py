@@ -158,3 +158,10 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
     B._here(on(0), None, False, on(0), on(-1))
     with pytest.raises(ValueError, match="cuda:1"):
         B._here(on(0), None, on(1))
+
+
+def test_addresses_of_tensors_without_values_are_not_looked_at(m):
+    n = ctypes.c_size_t()
+    for dtype in (F32, BF16):
+        t = tensors((P, P, 10, F32), (P + 1, P + 3, 0, dtype), (None, P + 1, 0, dtype))
+        assert m.lib.egnn_clip_gradients_workspace_bytes(m.ctx, ctypes.addressof(t), 3, ctypes.addressof(n)) == 0 and n.value > 0
