@@ -56,7 +56,8 @@ __device__ __forceinline__ SlTile sl_tile(const SlArgs& p, long tile) {
     const unsigned long long past = __ballot(before + sum > tile);
     if (past) {
       const int k = __ffsll((unsigned long long)past) - 1;
-      const long from = __shfl(b, k) + (tile - before - __shfl(sum - mine, k)) * SIDE;
+      // (at least 0: groups that overlap, which is no order of the rows, may number more tiles than an int holds)
+      const long from = max(__shfl(b, k) + (tile - before - __shfl(sum - mine, k)) * SIDE, 0l);
       return {g0 + k, from, min(from + SIDE, __shfl(e, k))};
     }
     before += __shfl(sum, 63);
