@@ -13,7 +13,7 @@
 // under way), long ones have a wave or a workgroup; a degree is a row of its own, with all its planes on their way together.
 //
 // Measured: 2,350,179 x 64 bf16 with the residual, sum and codes out, 189 us (5.6 TB/s); 20,000 x 25 x 64 fp32, sum and y out, 87 (5.9); 20,000 x 1024
-// bf16 29 (5.6); 64 x 9 x 16 fp32 4.0.  The adjoint with the gradient from besides 122 (4.2 TB/s), and 37 (4.4), then 5 to join the chunks' gradients of
+// bf16 29 (5.6); 64 x 9 x 16 fp32 4.0.  The adjoint with the gradient from besides 113 (4.5 TB/s), and 37 (4.4), then 5 to join the chunks' gradients of
 // gamma: reading three tensors and writing one, it stays there with 8 or 16 bytes a lane, two to five waves a SIMD, one turn or many a workgroup.
 #include <algorithm>
 #include "codes8.h"
