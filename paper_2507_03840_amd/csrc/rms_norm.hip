@@ -129,6 +129,10 @@ __device__ __forceinline__ void rn_write(const RnShape& p, const RnForward<T>& a
         float v[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = (float)h[u][m][k][i] * down * by * gain[k][i];
+        if (!EVEN && !(rho >= 0.0)) {       // a NaN in the row: the zeros behind its last value stay zeros
+#pragma unroll
+          for (int i = 0; i < V; ++i) v[i] = j * V + i < C ? v[i] : 0.0f;
+        }
         if (a.y && there) {
           typename R::vec y;
 #pragma unroll

@@ -259,3 +259,18 @@ def test_captured_and_on_another_stream(m):
         other = m.egnn_rms_norm(x, g, residual=r, q=None)
     torch.cuda.current_stream().wait_stream(stream)
     assert torch.equal(other[0], want[0]) and torch.equal(other[2].float(), want[2].float())
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("lmax,c", [(0, 9), (0, 33), (0, 50), (0, 70), (0, 300), (0, 1001), (0, 5003), (1, 33), (2, 50), (4, 13), (1, 601), (5, 7)])
+def test_padding_of_rows_that_are_not_finite(m, lmax, c, dtype):
+    """The bytes from the last code to the next multiple of 16 are zero whatever the row holds."""
+    import torch
+    dim = (lmax + 1) ** 2
+    x = torch.randn(6, dim, c, device="cuda").to(getattr(torch, dtype))
+    x[1, dim - 1, c // 2], x[2, 0, c - 1], x[3, dim - 1, 0], x[4] = float("nan"), float("inf"), -float("inf"), float("nan")
+    q = torch.full((6, dim, (c + 15) // 16 * 16), 9, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)[..., :c]
+    s = torch.full((6, dim, -(-c // 128)), 9, dtype=torch.uint8, device="cuda").view(torch.float8_e8m0fnu)
+    y, _, q, s = m.egnn_rms_norm(x, torch.ones(lmax + 1, c, device="cuda"), q=q, scale=s)
+    assert not padding(q).any()
+    assert torch.equal(torch.isnan(q.float()), torch.isnan(y)) and torch.isnan(y[4]).all() and torch.isnan(y[1, dim - 1]).all()
