@@ -223,7 +223,8 @@ class TensorList:
     Keeps them alive; made once for tensors that stay where they are."""
 
     def __init__(self, tensors, out=None):
-        self.tensors, self.out = list(tensors), list(tensors if out is None else out)
+        self.tensors = list(tensors)                # (once: it may be a generator)
+        self.out = list(self.tensors if out is None else out)
         if len(self.out) != len(self.tensors):
             raise ValueError(f"{len(self.tensors)} tensors, but {len(self.out)} places for results")
         self.desc = (TensorDesc * max(1, len(self.tensors)))()

@@ -161,3 +161,14 @@ def test_the_same_tensor_twice_is_refused(m):
     with pytest.raises(ValueError):
         m.egnn_clip_gradients(B.TensorList([t]), 1.0, out=[t])
     assert (t == 1).all()
+
+
+def test_a_generator_of_gradients(m):
+    import torch
+    torch.manual_seed(7)
+    g = [torch.randn(n, device="cuda") for n in (300, 5, 4000)]
+    out = [torch.empty_like(t) for t in g]
+    want = m.egnn_clip_gradients(g, 1.0, out=out)
+    a, b = [t.clone() for t in g], [torch.empty_like(t) for t in g]
+    assert torch.equal(m.egnn_clip_gradients((t for t in g), 1.0, out=(t for t in b)), want) and all(torch.equal(x, y) for x, y in zip(b, out))
+    assert torch.equal(m.egnn_clip_gradients((t for t in a), 1.0), want) and all(torch.equal(x, y) for x, y in zip(a, out))

@@ -165,3 +165,31 @@ def test_addresses_of_tensors_without_values_are_not_looked_at(m):
     for dtype in (F32, BF16):
         t = tensors((P, P, 10, F32), (P + 1, P + 3, 0, dtype), (None, P + 1, 0, dtype))
         assert m.lib.egnn_clip_gradients_workspace_bytes(m.ctx, ctypes.addressof(t), 3, ctypes.addressof(n)) == 0 and n.value > 0
+
+
+def test_a_list_of_tensors_from_a_generator():
+    """What can be gone through once is gone through once: results go to the tensors themselves."""
+    import torch
+    from paper_2507_03840_amd import binding as B
+
+    class Device:                                  # what the list asks of a device tensor
+        is_cuda, dtype = True, torch.float32
+
+        def __init__(self, at, n):
+            self.at, self.shape, self.n = at, torch.Size((n,)), n
+
+        is_contiguous = lambda self: True
+        data_ptr = lambda self: self.at
+        numel = lambda self: self.n
+        get_device = lambda self: 0
+
+    tensors = [Device(P, 5), Device(2 * P, 7), Device(3 * P, 0)]
+    got = B.TensorList(t for t in tensors)
+    assert got.tensors == tensors and got.out == tensors and got.device == 0
+    assert [(d.data, d.out, d.n, d.dtype) for d in got.desc] == [(P, P, 5, F32), (2 * P, 2 * P, 7, F32), (3 * P, 3 * P, 0, F32)]
+    elsewhere = [Device(k * P, t.n) for k, t in enumerate(tensors, 5)]
+    got = B.TensorList((t for t in tensors), (t for t in elsewhere))
+    assert [(d.data, d.out) for d in got.desc] == [(P, 5 * P), (2 * P, 6 * P), (3 * P, 7 * P)]
+    for out in ((t for t in elsewhere[:2]), (t for t in ())):
+        with pytest.raises(ValueError, match="places for results"):
+            B.TensorList((t for t in tensors), out)
