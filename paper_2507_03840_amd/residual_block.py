@@ -32,18 +32,20 @@ class ResidualBlock:
                                     lib.egnn_grouped_linear_workspace_bytes(n * lib.dim, n_species * degrees, c, c),
                                     lib.egnn_orthogonalise_workspace_bytes(n_species * degrees, c, c)), dtype=torch.uint8, device="cuda")
         self.code = lib.egnn_quantise_matrices(self.W, qt=None)
+        self.h = self.y = None                      # of the last forward pass that was kept
 
     def forward(self, x, h=None, keep=True):
-        """(x, sum so far) [n][(lmax + 1)^2][channels] -> (the next block's x, h); keep: what the adjoint needs."""
+        """(x, sum so far) [n][(lmax + 1)^2][channels] -> (the next block's x, h); keep: what the adjoint needs (else what an earlier pass kept goes too)."""
         n, dim, c = x.shape
         y, h, q, scale = self.lib.egnn_rms_norm(x, self.gamma, residual=h, y=None if keep else False, q=None)
         out = self.lib.egnn_scaled_linear(q, scale, *self.code[:2], ptr=self.ptr, perm=self.perm, bias=self.bias)
-        if keep:
-            self.h, self.y = h, y
+        self.h, self.y = (h, y) if keep else (None, None)
         return out.view(n, dim, c), h
 
     def backward(self, dout, dh=None):
-        """Gradients of the results -> (gradient of x, which is also that of the sum so far, gradients of the weights by name)."""
+        """Gradients of the last forward pass's results -> (gradient of x, which is also that of the sum so far, gradients of the weights by name)."""
+        if self.h is None:
+            raise RuntimeError("backward: the last forward pass kept nothing, or there was none")
         n, dim, c = dout.shape
         rows = dout.reshape(n * dim, c)
         dy = self.lib.egnn_scaled_linear(*self.lib.egnn_quantise_rows(rows), *self.code[2:], ptr=self.ptr, perm=self.perm)

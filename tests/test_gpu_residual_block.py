@@ -144,3 +144,25 @@ def test_training_runs():
     from paper_2507_03840_amd.residual_block import train
     losses, norms = train(steps=5, verbose=False)
     assert len(losses) == 5 and np.isfinite(losses).all() and np.isfinite(norms).all()
+
+
+def test_the_adjoint_is_that_of_the_last_forward_pass_that_was_kept_for_it():
+    """After a pass that keeps nothing, or none, there is nothing to go back through: another input's rows are not taken in their place."""
+    import torch
+    from paper_2507_03840_amd.residual_block import ResidualStack
+    lib, block, species, x, r, dout, dh = make(1, 32, 40, 2, 17)
+    with pytest.raises(RuntimeError, match="forward"):
+        block.backward(dout, dh)
+    block.forward(x, r)
+    want, grads = block.backward(dout, dh)
+    block.forward(r, x, keep=False)
+    with pytest.raises(RuntimeError, match="forward"):
+        block.backward(dout, dh)
+    block.forward(x, r)
+    again, more = block.backward(dout, dh)
+    assert torch.equal(again, want) and all(torch.equal(more[k], grads[k]) for k in grads)
+    stack = ResidualStack(lib, torch.from_numpy(species).cuda(), 2, 2)
+    stack.forward(x)
+    stack.forward(x, keep=False)
+    with pytest.raises(RuntimeError, match="forward"):
+        stack.backward(dout)
