@@ -274,3 +274,22 @@ def test_padding_of_rows_that_are_not_finite(m, lmax, c, dtype):
     y, _, q, s = m.egnn_rms_norm(x, torch.ones(lmax + 1, c, device="cuda"), q=q, scale=s)
     assert not padding(q).any()
     assert torch.equal(torch.isnan(q.float()), torch.isnan(y)) and torch.isnan(y[4]).all() and torch.isnan(y[1, dim - 1]).all()
+
+
+@pytest.mark.parametrize("c", [4, 5, 8, 12, 32])
+def test_terms_that_cancel_in_short_rows(m, c):
+    """One value v far above the others, zeros: of gamma dy - h rho^2 <gamma dy h> all but c eps / (v^2 + c eps) cancels, and rho d eps / mean is left.  That
+    share is 4.4e-8 at least; in fp64 a dozen roundings of 2^-53 leave it known to 12 * 2^-53 / 4.4e-8 < U32 / 2, gamma = 1 adds none, and the result is
+    rounded once: 2 U32."""
+    import torch
+    rng = np.random.default_rng(c)
+    n = 5000
+    v, d, at = rng.uniform(15, 30, n).astype(np.float32), rng.uniform(0.5, 2, n).astype(np.float32), rng.integers(0, c, n)
+    h, dy = np.zeros((2, n, 1, c), np.float32)
+    h[np.arange(n), 0, at], dy[np.arange(n), 0, at] = v, d
+    dx, _ = m.egnn_rms_norm_backward(torch.from_numpy(h).cuda(), torch.from_numpy(dy).cuda(), torch.ones(1, c, device="cuda"), eps=1e-5)
+    eps = float(np.float32(1e-5))
+    mean = v.astype(np.float64) ** 2 / c + eps
+    want = d * eps / mean / np.sqrt(mean)
+    got = values(dx)[np.arange(n), 0, at]
+    assert np.abs(got / want - 1).max() <= 2 * U32
