@@ -564,8 +564,8 @@ int egnn_muon_step(egnn_ctx* ctx, const float* W, const float* g, const float* m
  *   and a byte e + 127 (e8m0) for every block of 128 values: e is the least integer for which the block's largest finite magnitude times 2^-e
  *   is at most 448, but at least -127 (a block of zeros).  Values that are not finite become NaN and do not count for the scale.
  *   Calls that read scales take bytes 0..254.
- *   Rows of codes begin at multiples of 16 bytes (*_stride: bytes from one row to the next); the bytes from the last code to the next multiple
- *   of 16 are zero: the calls that write codes write them, the call that reads codes takes them to be.
+ *   Rows of codes begin at multiples of 16 bytes (*_stride: bytes from one row to the next) and have room up to the next multiple of 16 behind the
+ *   last code: the calls that write codes write zeros there, the call that reads codes may read that far, and what lies there counts for nothing.
  *   Rows of n_cols codes have ceil(n_cols / 128) scales, contiguous from row to row.  Matrices [batch][rows][cols] of codes (row stride
  *   q_stride, matrices rows * q_stride apart) have a scale for every 128 x 128 values: [batch][ceil(rows / 128)][ceil(cols / 128)].
  *

@@ -997,7 +997,8 @@ class Egnn:
 
     def egnn_scaled_linear(self, q, scale, w, w_scale, ptr=None, perm=None, bias=None, y=None, dtype=torch.float32):
         """y = W_g x + bias_g for the rows of every group, x [n][n_in] and W [groups][n_out][n_in] in codes with their scales (rows of codes of more
-        axes are taken as one row after the other); without ptr one group of all rows.  y, or a new tensor of `dtype` [n][n_out]."""
+        axes are taken as one row after the other); without ptr one group of all rows.  y, or a new tensor of `dtype` [n][n_out].  Codes may be the first
+        columns of wider ones: what lies behind the last counts for nothing."""
         _here(q, scale, w, w_scale, ptr, perm, bias, y)
         groups, n_out, n_in = w.shape
         q_at, q_row, s_at = _code_rows(q, scale, q.shape if q.shape[-1] == n_in else (*q.shape[:-1], n_in))

@@ -94,6 +94,18 @@ __device__ __forceinline__ sl_i8 sl_load(const uint8_t* row, int k, int K) {
   return sl_i8{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w};
 }
 
+// What is read behind column K, up to a multiple of 16, is no part of a row, whatever lies there: zero.  (After the loads, so that none waits; kernels
+// for K of no multiple of 16, ODD, are apart.  They take the last block behind all others where masks among these would cost registers: the tiles of 256
+// spilled 87, 309 us instead of 120 for 8192 x 4090 by 4096 bf16; 4096 of k 115.)
+__device__ __forceinline__ uint4 sl_first(const uint4& v, int count) {
+  auto word = [](unsigned w, int bytes) { return bytes >= 4 ? w : bytes > 0 ? w & ((1u << 8 * bytes) - 1) : 0u; };
+  return make_uint4(word(v.x, count), word(v.y, count - 4), word(v.z, count - 8), word(v.w, count - 12));
+}
+__device__ __forceinline__ void sl_trim(sl_i8& v, int k, int K) {
+  const uint4 a = sl_first(make_uint4(v[0], v[1], v[2], v[3]), K - k), b = sl_first(make_uint4(v[4], v[5], v[6], v[7]), K - k - 16);
+  v = sl_i8{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w};
+}
+
 // 16 bytes of results to columns n .. of a row
 template <class T>
 __device__ __forceinline__ void sl_store_piece(const SlArgs& p, T* y, int n, const uint4& v) {
@@ -130,7 +142,7 @@ constexpr int SL_WAVES = 4, SL_DOWN = 4;
 // What bounds it is reading W once (one row of 2048 by 4096 bf16 4.4 us for 8.4 MB: launch and a chain of two loads as much as memory).  A workgroup makes 16 columns of up to 16 R rows; its waves take the blocks of k in turn, SL_AHEAD of them under way
 // in each, and add up through LDS in the order of the waves.
 constexpr int SL_FEW = 8, SL_AHEAD = 4;
-template <class T, int R>
+template <class T, int R, bool ODD>
 __global__ void __launch_bounds__(SL_FEW * 64) sl_few_kernel(SlArgs p) {
   constexpr bool EXACT = !__is_same(T, __bf16);
   __shared__ sl_f4 lds[SL_FEW][R][64];
@@ -146,17 +158,18 @@ __global__ void __launch_bounds__(SL_FEW * 64) sl_few_kernel(SlArgs p) {
     qs[r] = p.qs + row * p.kb;
   }
   sl_f4 sum[R] = {};
-  for (int b0 = wave; b0 < p.kb; b0 += SL_FEW * SL_AHEAD) {
+  const int whole = ODD ? p.kb - 1 : p.kb, K = ODD ? whole * C8_BLOCK : p.K;        // ODD: the last block is taken apart
+  for (int b0 = wave; b0 < whole; b0 += SL_FEW * SL_AHEAD) {
     sl_i8 wv[SL_AHEAD], qv[SL_AHEAD][R];
     int ew[SL_AHEAD], eq[SL_AHEAD][R];
 #pragma unroll
     for (int u = 0; u < SL_AHEAD; ++u) {
       const int b = b0 + u * SL_FEW, k = b * C8_BLOCK + 32 * quarter, at = min(b, p.kb - 1);
-      wv[u] = sl_load(w, k, p.K);
+      wv[u] = sl_load(w, k, K);
       ew[u] = ws[at];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        qv[u][r] = sl_load(q[r], k, p.K);
+        qv[u][r] = sl_load(q[r], k, K);
         eq[u][r] = qs[r][at];
       }
     }
@@ -165,8 +178,25 @@ __global__ void __launch_bounds__(SL_FEW * 64) sl_few_kernel(SlArgs p) {
 #pragma unroll
       for (int r = 0; r < R; ++r) sum[r] = sl_mma<EXACT>(wv[u], qv[u][r], sum[r], ew[u], eq[u][r]);
   }
+  if (ODD && wave == whole % SL_FEW) {
+    const int k = whole * C8_BLOCK + 32 * quarter;
+    sl_i8 wv = sl_load(w, k, p.K), qv[R];
+    int eq[R];
 #pragma unroll
-  for (int r = 0; r < R; ++r) lds[wave][r][lane] = sum[r];
+    for (int r = 0; r < R; ++r) {
+      qv[r] = sl_load(q[r], k, p.K);
+      eq[r] = qs[r][whole];
+    }
+    sl_trim(wv, k, p.K);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      sl_trim(qv[r], k, p.K);
+      lds[wave][r][lane] = sl_mma<EXACT>(wv, qv[r], sum[r], ws[whole], eq[r]);
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < R; ++r) lds[wave][r][lane] = sum[r];
+  }
   __syncthreads();
   for (int i = threadIdx.x; i < R * 256; i += SL_FEW * 64) {
     const int col = i & 15, row = i >> 4, at = (row & 15) + 16 * (col >> 2);        // lane and element that hold it
@@ -193,7 +223,7 @@ __device__ __forceinline__ SlWalk sl_next(const SlArgs& p, SlWalk t) {
   return t;
 }
 
-template <class T, int H, int F>
+template <class T, int H, int F, bool ODD>
 __global__ void __launch_bounds__(SL_WAVES * 64) sl_rows_kernel(SlArgs p, long share) {
   constexpr bool EXACT = !__is_same(T, __bf16);
   typedef float sl_f16 __attribute__((ext_vector_type(16)));
@@ -218,6 +248,12 @@ __global__ void __launch_bounds__(SL_WAVES * 64) sl_rows_kernel(SlArgs p, long s
   };
   // results go through LDS, so that rows are written whole; a row's pieces lie at (piece xor row), for the banks
   auto swizzle = [](int r) { return PIECES >= 16 ? r & 15 : PIECES == 8 ? r >> 1 & 7 : r >> 2 & 3; };
+  sl_i8 keep[ODD ? H : 1];
+#pragma unroll
+  for (int h = 0; h < (ODD ? H : 0); ++h) {
+    keep[h] = sl_i8{-1, -1, -1, -1, -1, -1, -1, -1};
+    sl_trim(keep[h], 64 * h + 32 * half, p.K);
+  }
   long row = row_of(now), row_then = row_of(then);
   Rows v = fetch(row);
   sl_i8 w[F][H];
@@ -235,9 +271,17 @@ __global__ void __launch_bounds__(SL_WAVES * 64) sl_rows_kernel(SlArgs p, long s
         for (int h = 0; h < H; ++h) w[i][h] = sl_load(p.w + ((long)now.g * p.N + n) * p.w_stride, 64 * h + 32 * half, p.K);
         ew[i] = p.ws[(long)now.g * p.nb + min(n0 + 32 * i, p.N - 1) / C8_BLOCK];
       }
+      if constexpr (ODD)
+#pragma unroll
+        for (int i = 0; i < F; ++i)
+#pragma unroll
+          for (int h = 0; h < H; ++h) w[i][h] &= keep[h];
       if (lane < 32 * F) ((float*)bias)[lane] = p.bias ? p.bias[(long)now.g * p.N + min(n0 + lane, p.N - 1)] : 0.0f;
       sl_wave_sync();
     }
+    if constexpr (ODD)
+#pragma unroll
+      for (int h = 0; h < H; ++h) v.q[h] &= keep[h];
 #pragma unroll
     for (int i = 0; i < F; ++i) {
       sl_f16 sum;
@@ -310,7 +354,7 @@ __device__ __forceinline__ void sl_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-template <class T, int SIDE, bool TWO>
+template <class T, int SIDE, bool TWO, bool ODD>
 __global__ void __launch_bounds__(SL_WAVES * 64, SIDE == 256 ? 1 : TWO || !__is_same(T, __bf16) ? 2 : 3) sl_tile_kernel(SlArgs p, long tiles) {
   constexpr bool EXACT = !__is_same(T, __bf16);
   constexpr int F = SIDE / 64;                                        // fragments of 32 rows of a wave, of either operand
@@ -370,9 +414,22 @@ __global__ void __launch_bounds__(SL_WAVES * 64, SIDE == 256 ? 1 : TWO || !__is_
     if constexpr (F == 4) return *(const unsigned*)(le + wr * COLS + j * F);
     else return (unsigned)*(const uint16_t*)(le + wr * COLS + j * F);
   };
-  auto stage = [&](uint8_t* buffer, int b) {
-    sl_stage<LOADS>(q_row, buffer, b * C8_BLOCK + piece, p.K);
-    sl_stage<LOADS>(w_row, buffer + SIDE * C8_BLOCK, b * C8_BLOCK + piece, p.K);
+  auto stage_up_to = [&](uint8_t* buffer, int b, int K) {
+    sl_stage<LOADS>(q_row, buffer, b * C8_BLOCK + piece, K);
+    sl_stage<LOADS>(w_row, buffer + SIDE * C8_BLOCK, b * C8_BLOCK + piece, K);
+  };
+  const int whole = ODD ? p.kb - 1 : p.kb, K = ODD && TWO ? whole * C8_BLOCK : p.K;       // ODD with two buffers: the last block is taken apart
+  auto stage = [&](uint8_t* buffer, int b) { stage_up_to(buffer, b, K); };
+  // ODD, the last block has arrived: the piece that K ends inside is trimmed where it lies, by the lane that asked for it
+  auto trim = [&](uint8_t* buffer) {
+    sl_wave_sync();
+    const int left = p.K - whole * C8_BLOCK - piece;
+    if (left <= 0 || left >= 16) return;
+#pragma unroll 4
+    for (int i = 0; i < 2 * LOADS; ++i) {
+      uint4* at = (uint4*)(buffer + (i * SL_WAVES + wave) * 1024 + lane * 16);      // (rows of W behind those of the codes)
+      *at = sl_first(*at, left);
+    }
   };
   auto block_at = [&](int b) { return min(b, p.kb - 1); };
 
@@ -386,6 +443,7 @@ __global__ void __launch_bounds__(SL_WAVES * 64, SIDE == 256 ? 1 : TWO || !__is_
   le0[scale_to] = (uint8_t)scale0;
   bias[mine] = bias0;
   __builtin_amdgcn_s_waitcnt(SL_VMCNT(TWO ? 2 * LOADS : 0));        // the first block
+  if (ODD && !TWO && whole == 0) trim(b0);
   sl_barrier();
   unsigned eq = scales(le0), eq_next = eq;
 
@@ -451,10 +509,10 @@ __global__ void __launch_bounds__(SL_WAVES * 64, SIDE == 256 ? 1 : TWO || !__is_
   };
   if constexpr (TWO) {
     fetch(b0, 0, even);
-    for (int b = 0; b < p.kb; b += 2) {                   // (what lies behind K: zeros)
+    for (int b = 0; b < whole; b += 2) {                  // (what lies behind K: zeros)
       block(b, b0, b1, le1);
       if constexpr (SIDE < 256)
-        if (b + 1 >= p.kb) break;
+        if (b + 1 >= whole) break;
       block(b + 1, b1, b0, le0);
     }
   } else {
@@ -471,9 +529,22 @@ __global__ void __launch_bounds__(SL_WAVES * 64, SIDE == 256 ? 1 : TWO || !__is_
       ew = ew_next;
       ew_next = wscale_at[block_at(b + 1)];
       __builtin_amdgcn_s_waitcnt(SL_VMCNT(0));
+      if (ODD && b == whole) trim(b0);
       sl_barrier();
       eq = scales(le0);
     }
+  }
+  if constexpr (ODD && TWO) {                             // eq and ew are those of the last block
+    __builtin_amdgcn_s_waitcnt(SL_VMCNT(0));
+    sl_barrier();                                         // nothing is on its way to the buffer any more, and nobody reads it
+    stage_up_to(b0, whole, p.K);
+    __builtin_amdgcn_s_waitcnt(SL_VMCNT(0));
+    trim(b0);
+    sl_barrier();
+    fetch(b0, 0, even);
+    products(even, false);
+    fetch(b0, 1, even);
+    products(even, true);
   }
 
   // Results through LDS, a buffer for each wave, so that rows are written whole; a row's pieces of 16 bytes lie at (piece xor row), for the banks.
@@ -517,28 +588,28 @@ int sl_launched(egnn_ctx* ctx) {
 }
 int sl_too_many(egnn_ctx* ctx) { return egnn_fail(ctx, EGNN_EINVAL, "scaled_linear: more than 2^32 threads' worth of results"); }
 
-template <class T, int SIDE, bool TWO>
+template <class T, int SIDE, bool TWO, bool ODD>
 int sl_tiles(egnn_ctx* ctx, SlArgs p, hipStream_t st) {
   p.tiles_n = (p.N + SIDE - 1) / SIDE;
   const long items = sl_row_tiles(p, SIDE) * p.tiles_n;
   if (items * SL_WAVES * 64 > 0xffffffffl) return sl_too_many(ctx);
-  hipLaunchKernelGGL((sl_tile_kernel<T, SIDE, TWO>), dim3((unsigned)items), dim3(SL_WAVES * 64), 0, st, p, items);
+  hipLaunchKernelGGL((sl_tile_kernel<T, SIDE, TWO, ODD>), dim3((unsigned)items), dim3(SL_WAVES * 64), 0, st, p, items);
   return sl_launched(ctx);
 }
 
-template <class T, int H, int F>
+template <class T, int H, int F, bool ODD>
 int sl_rows(egnn_ctx* ctx, const SlArgs& p, hipStream_t st) {
   // as many waves as run at once: two a SIMD with their 150 to 190 registers, four of the narrow ones (300,000 x 64 by 64 fp32 in 15 groups 24.3 us with
   // 2,048 waves, 29.4 with 4,096; 2,000,000 x 16 by 16 33.5 and 23.2)
   const long waves = F == 1 ? 4096 : 2048, tiles = sl_row_tiles(p, 32), share = (tiles + waves - 1) / waves;
-  hipLaunchKernelGGL((sl_rows_kernel<T, H, F>), dim3((unsigned)((tiles + share * SL_WAVES - 1) / (share * SL_WAVES))), dim3(SL_WAVES * 64), 0, st, p, share);
+  hipLaunchKernelGGL((sl_rows_kernel<T, H, F, ODD>), dim3((unsigned)((tiles + share * SL_WAVES - 1) / (share * SL_WAVES))), dim3(SL_WAVES * 64), 0, st, p, share);
   return sl_launched(ctx);
 }
 
-template <class T, int R>
+template <class T, int R, bool ODD>
 int sl_few(egnn_ctx* ctx, SlArgs p, hipStream_t st) {
   p.tiles_n = (p.N + 15) / 16;
-  hipLaunchKernelGGL((sl_few_kernel<T, R>), dim3((unsigned)(sl_row_tiles(p, 16 * R) * p.tiles_n)), dim3(SL_FEW * 64), 0, st, p);
+  hipLaunchKernelGGL((sl_few_kernel<T, R, ODD>), dim3((unsigned)(sl_row_tiles(p, 16 * R) * p.tiles_n)), dim3(SL_FEW * 64), 0, st, p);
   return sl_launched(ctx);
 }
 
@@ -552,24 +623,24 @@ int sl_few(egnn_ctx* ctx, SlArgs p, hipStream_t st) {
 //   * else tiles of 128: bf16 with two buffers as long as there is about one for each compute unit (2048 x 4096 by 2048 33 and, with one buffer, 39), with
 //     one buffer, three workgroups per compute unit, above that (20,000 x 512 by 1024 25.6 and 22.4).  fp32 and fp16 have one buffer always: twice the products
 //     and the sums of a block beside those of all leave no registers for more (20,000 x 512 by 1024 fp32 59 and 52).
-template <class T>
+template <class T, bool ODD>
 int sl_product(egnn_ctx* ctx, SlArgs p, hipStream_t st) {
   constexpr bool EXACT = !__is_same(T, __bf16);
   p.even = (uintptr_t)p.y % 16 == 0 && p.y_stride * sizeof(T) % 16 == 0;
   if (p.K <= C8_BLOCK && p.N <= 64) {
-    if (p.K <= 64) return p.N <= 32 ? sl_rows<T, 1, 1>(ctx, p, st) : sl_rows<T, 1, 2>(ctx, p, st);
-    return p.N <= 32 ? sl_rows<T, 2, 1>(ctx, p, st) : sl_rows<T, 2, 2>(ctx, p, st);
+    if (p.K <= 64) return p.N <= 32 ? sl_rows<T, 1, 1, ODD>(ctx, p, st) : sl_rows<T, 1, 2, ODD>(ctx, p, st);
+    return p.N <= 32 ? sl_rows<T, 2, 1, ODD>(ctx, p, st) : sl_rows<T, 2, 2, ODD>(ctx, p, st);
   }
   const long each = p.n / p.G;
   const int R = each <= 16 ? 1 : each <= 32 ? 2 : 4;
   if (sl_row_tiles(p, 16 * R) * ((p.N + 15) / 16) <= (EXACT ? 512 : 256))
-    return R == 1 ? sl_few<T, 1>(ctx, p, st) : R == 2 ? sl_few<T, 2>(ctx, p, st) : sl_few<T, 4>(ctx, p, st);
+    return R == 1 ? sl_few<T, 1, ODD>(ctx, p, st) : R == 2 ? sl_few<T, 2, ODD>(ctx, p, st) : sl_few<T, 4, ODD>(ctx, p, st);
   if constexpr (!EXACT) {
     const long large = sl_row_tiles(p, 256) * ((p.N + 255) / 256), places = (large + EGNN_CUS - 1) / EGNN_CUS * EGNN_CUS;
-    if (p.K >= 2048 && large * 10 >= places * 7) return sl_tiles<T, 256, true>(ctx, p, st);
-    if (sl_row_tiles(p, 128) * ((p.N + 127) / 128) <= 3 * EGNN_CUS / 2) return sl_tiles<T, 128, true>(ctx, p, st);
+    if (p.K >= 2048 && large * 10 >= places * 7) return sl_tiles<T, 256, true, ODD>(ctx, p, st);
+    if (sl_row_tiles(p, 128) * ((p.N + 127) / 128) <= 3 * EGNN_CUS / 2) return sl_tiles<T, 128, true, ODD>(ctx, p, st);
   }
-  return sl_tiles<T, 128, false>(ctx, p, st);
+  return sl_tiles<T, 128, false, ODD>(ctx, p, st);
 }
 
 }  // namespace
@@ -591,7 +662,7 @@ extern "C" int egnn_scaled_linear(egnn_ctx* ctx, const void* q, int64_t q_stride
   const SlArgs p{n_rows, n_in, n_out, n_groups, c8_blocks(n_in), c8_blocks(n_out), (const uint8_t*)q, (const uint8_t*)q_scale, (const uint8_t*)w,
                  (const uint8_t*)w_scale, q_stride, w_stride, y_stride, bias, ptr, perm, y, 0, false};
   hipStream_t st = (hipStream_t)stream;
-  if (dtype == EGNN_F32) return sl_product<float>(ctx, p, st);
-  if (dtype == EGNN_F16) return sl_product<_Float16>(ctx, p, st);
-  return sl_product<__bf16>(ctx, p, st);
+  if (dtype == EGNN_F32) return n_in % 16 ? sl_product<float, true>(ctx, p, st) : sl_product<float, false>(ctx, p, st);
+  if (dtype == EGNN_F16) return n_in % 16 ? sl_product<_Float16, true>(ctx, p, st) : sl_product<_Float16, false>(ctx, p, st);
+  return n_in % 16 ? sl_product<__bf16, true>(ctx, p, st) : sl_product<__bf16, false>(ctx, p, st);
 }

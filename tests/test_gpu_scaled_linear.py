@@ -317,3 +317,22 @@ def test_captured_and_the_same_every_time(m):
                 graph.replay()
                 torch.cuda.synchronize()
                 assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,k,out,groups", [(1, 1, 8, 1), (9, 100, 40, 1), (300, 20, 33, 1), (500, 50, 64, 3), (700, 100, 17, 2), (70, 90, 64, 1), (20, 130, 70, 1),
+                                            (5, 2049, 48, 1), (130, 1001, 200, 1), (900, 200, 300, 4), (1300, 650, 520, 1), (3600, 2057, 3400, 1), (5120, 140, 5000, 1),
+                                            (3600, 2177, 3400, 1)])
+def test_columns_of_wider_codes(m, n, k, out, groups, dtype):
+    """Bytes behind the last code of a row, up to a multiple of 16, are not part of it: codes taken out of wider ones, and NaN there."""
+    import torch
+    torch.manual_seed(k)
+    wide = (k + 15) // 16 * 16 + 16
+    ptr = None if groups == 1 else torch.tensor([0] + [n * (g + 1) // groups for g in range(groups)], dtype=torch.int32, device="cuda")
+    a, b = m.egnn_quantise_rows(torch.randn(n, k, device="cuda")), m.egnn_quantise_matrices(torch.randn(groups, out, k, device="cuda"))[:2]
+    want = m.egnn_scaled_linear(*a, *b, ptr=ptr, dtype=getattr(torch, dtype))
+    for qfill, wfill in ((0x7F, 0x7F), (0x38, 0x38), (0xFF, 0x01)):
+        q = torch.full((n, wide), qfill, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+        w = torch.full((groups, out, wide), wfill, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+        q[:, :k], w[:, :, :k] = a[0], b[0]
+        assert torch.equal(m.egnn_scaled_linear(q[:, :k], a[1], w[:, :, :k], b[1], ptr=ptr, dtype=getattr(torch, dtype)), want)
