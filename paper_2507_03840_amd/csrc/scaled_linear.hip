@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(SL_WAVES * 64) sl_rows_kernel(SlArgs p, long s
 // at once lie in all 64 banks.
 typedef __attribute__((address_space(3))) uint8_t sl_lds;
 typedef const __attribute__((address_space(1))) uint8_t sl_global;
-#define SL_VMCNT(n) (((n)&15) | ((n) >> 4) << 14 | 0xf70)      // the operand of s_waitcnt that waits until at most n loads are out
+constexpr int SL_ARRIVED = 0xf70;                              // the operand of s_waitcnt that waits until no load is out
 
 template <int LOADS>
 __device__ __forceinline__ void sl_stage(const uint8_t* const (&row)[LOADS], uint8_t* to, int k, int K) {
@@ -442,7 +442,8 @@ __global__ void __launch_bounds__(SL_WAVES * 64, SIDE == 256 ? 1 : TWO || !__is_
   rows[mine] = (int)sl_row(p, min(t.begin + mine, t.end - 1));
   le0[scale_to] = (uint8_t)scale0;
   bias[mine] = bias0;
-  __builtin_amdgcn_s_waitcnt(SL_VMCNT(TWO ? 2 * LOADS : 0));        // the first block
+  // (both blocks: the writes to LDS just above, of values that were loaded, wait for every load before them)
+  __builtin_amdgcn_s_waitcnt(SL_ARRIVED);
   if (ODD && !TWO && whole == 0) trim(b0);
   sl_barrier();
   unsigned eq = scales(le0), eq_next = eq;
@@ -487,7 +488,7 @@ __global__ void __launch_bounds__(SL_WAVES * 64, SIDE == 256 ? 1 : TWO || !__is_
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(SL_VMCNT(0));              // this wave's part of the next block is in LDS
+    __builtin_amdgcn_s_waitcnt(SL_ARRIVED);              // this wave's part of the next block is in LDS
     sl_barrier();
     __builtin_amdgcn_sched_barrier(0);
     eq_next = scales(le);
@@ -528,17 +529,17 @@ __global__ void __launch_bounds__(SL_WAVES * 64, SIDE == 256 ? 1 : TWO || !__is_
       scale = scale_at[block_at(b + 1)];
       ew = ew_next;
       ew_next = wscale_at[block_at(b + 1)];
-      __builtin_amdgcn_s_waitcnt(SL_VMCNT(0));
+      __builtin_amdgcn_s_waitcnt(SL_ARRIVED);
       if (ODD && b == whole) trim(b0);
       sl_barrier();
       eq = scales(le0);
     }
   }
   if constexpr (ODD && TWO) {                             // eq and ew are those of the last block
-    __builtin_amdgcn_s_waitcnt(SL_VMCNT(0));
+    __builtin_amdgcn_s_waitcnt(SL_ARRIVED);
     sl_barrier();                                         // nothing is on its way to the buffer any more, and nobody reads it
     stage_up_to(b0, whole, p.K);
-    __builtin_amdgcn_s_waitcnt(SL_VMCNT(0));
+    __builtin_amdgcn_s_waitcnt(SL_ARRIVED);
     trim(b0);
     sl_barrier();
     fetch(b0, 0, even);
@@ -548,7 +549,7 @@ __global__ void __launch_bounds__(SL_WAVES * 64, SIDE == 256 ? 1 : TWO || !__is_
   }
 
   // Results through LDS, a buffer for each wave, so that rows are written whole; a row's pieces of 16 bytes lie at (piece xor row), for the banks.
-  __builtin_amdgcn_s_waitcnt(SL_VMCNT(0));
+  __builtin_amdgcn_s_waitcnt(SL_ARRIVED);
   __syncthreads();
   uint8_t* out = TWO ? (wave & 1 ? b1 : b0) + (wave >> 1) * OUT : b0 + wave * OUT;
   auto swizzle = [](int row) { return PIECES == 16 ? row & 15 : row >> 1 & 7; };
