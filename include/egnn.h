@@ -577,7 +577,8 @@ int egnn_muon_step(egnn_ctx* ctx, const float* W, const float* g, const float* m
  *   finite values and NaN for the infinite ones, a row with a NaN all NaN.
  * egnn_rms_norm_backward: dx = dh + J^T dy with h the sum that the forward call wrote (its x, without a residual) and dh, which may be NULL,
  *   the gradient that reaches h besides; dx is the gradient of x and of r.  dgamma [lmax + 1][channels].  Both overwritten.  dx may be dy, dh or h
- *   (same stride).  ws: egnn_rms_norm_workspace_bytes.
+ *   (same stride).  What is not finite in h or dy stays in its row and degree, and in the channels of dgamma that it is a term of.
+ *   ws: egnn_rms_norm_workspace_bytes.
  *
  * egnn_quantise_rows: x [n_rows][n_cols] to codes and scales.  n_cols in 1..65536.
  * egnn_quantise_matrices: W [batch][rows][cols] (contiguous) to codes and scales; qt, scale_t (both or neither): those of the transposed

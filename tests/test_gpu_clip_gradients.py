@@ -172,3 +172,27 @@ def test_a_generator_of_gradients(m):
     a, b = [t.clone() for t in g], [torch.empty_like(t) for t in g]
     assert torch.equal(m.egnn_clip_gradients((t for t in g), 1.0, out=(t for t in b)), want) and all(torch.equal(x, y) for x, y in zip(b, out))
     assert torch.equal(m.egnn_clip_gradients((t for t in a), 1.0), want) and all(torch.equal(x, y) for x, y in zip(a, out))
+
+
+@pytest.mark.parametrize("where", ["elsewhere", "in place"])
+def test_past_the_caches(m, where):
+    """More than 128 MB of gradients, whose results go past the caches; tensors that begin anywhere, and what lies beside them."""
+    import torch
+    torch.manual_seed(6)
+    whole = [torch.randn(n, device="cuda").to(t) for n, t in ((30_000_013, torch.float32), (17, torch.float32), (9_000_005, torch.bfloat16), (5_000_011, torch.float16))]
+    g = [t[3:-2] for t in whole]
+    kept = [t.clone() for t in whole]
+    want = sum(float(t.double().square().sum()) for t in g) ** 0.5
+    most = 0.4 * want
+    room = [torch.full_like(t, 3.0) for t in whole] if where == "elsewhere" else whole
+    norm = values(m.egnn_clip_gradients(g, most, out=[t[3:-2] for t in room]))
+    factor = float(np.float32(most)) / (want + 1e-6)
+    assert abs(norm[0] - want) <= 2 * U32 * want and abs(norm[1] - factor) <= 4 * U32 * factor
+    for t, k, r in zip(whole, kept, room):
+        name = str(t.dtype).split(".")[1]
+        exact = k[3:-2].double() * factor
+        assert ((r[3:-2].double() - exact).abs() <= (6 * U32 + HALF_STEP[name]) * exact.abs() + FLOOR[name]).all()
+        beside = k if where == "in place" else torch.full_like(k, 3.0)
+        assert torch.equal(r[:3], beside[:3]) and torch.equal(r[-2:], beside[-2:])
+        if where == "elsewhere":
+            assert torch.equal(t, k)

@@ -293,3 +293,56 @@ def test_terms_that_cancel_in_short_rows(m, c):
     want = d * eps / mean / np.sqrt(mean)
     got = values(dx)[np.arange(n), 0, at]
     assert np.abs(got / want - 1).max() <= 2 * U32
+
+
+def check_adjoint(m, n, lmax, c, dtype, up=True):
+    """The adjoint alone, over more rows than the chunks are."""
+    import torch
+    rng = np.random.default_rng([3, n, c])
+    shape = (n, (lmax + 1) ** 2, c)
+    h, dy, dh = (tensor(rng, shape, dtype) for _ in range(3))
+    gamma = (1 + 0.3 * rng.standard_normal((lmax + 1, c))).astype(np.float32)
+    dx, dgamma = m.egnn_rms_norm_backward(h, dy, torch.from_numpy(gamma).cuda(), dh=dh if up else None)
+    rdx, rdg, size, terms = R.rms_norm_backward(values(h), values(dy), gamma, values(dh) if up else None)
+    assert (np.abs(values(dx) - rdx) <= 6 * U32 * size + HALF_STEP[dtype] * np.abs(rdx) + FLOOR[dtype]).all()
+    assert (np.abs(values(dgamma) - rdg) <= 32 * U32 * terms + 1e-37).all()
+
+
+@pytest.mark.parametrize("dtype,n,c", [("float32", 2500, 1024), ("float32", 2051, 2044), ("float32", 1100, 4096), ("float32", 1030, 8188), ("float32", 1027, 4097),
+                                       ("bfloat16", 2500, 2048), ("bfloat16", 1100, 4096), ("float16", 1030, 8190), ("bfloat16", 2051, 1030),
+                                       ("float32", 9001, 300), ("float32", 4099, 512), ("bfloat16", 9001, 1000), ("float16", 8200, 777), ("float32", 1500, 9000)])
+def test_adjoint_of_chunks_of_wide_rows(m, dtype, n, c):
+    """More rows than chunks (1,024), so that a workgroup's turns follow one another in the same LDS."""
+    check_adjoint(m, n, 0, c, dtype, up=n % 2 == 0)
+
+
+@pytest.mark.parametrize("dtype,n,lmax,c", [("float32", 9001, 1, 64), ("bfloat16", 5003, 4, 40), ("float16", 5000, 2, 300), ("float32", 3001, 3, 33), ("bfloat16", 2501, 5, 16)])
+def test_adjoint_of_chunks_of_degrees(m, dtype, n, lmax, c):
+    check_adjoint(m, n, lmax, c, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("lmax,c", [(0, 3), (0, 8), (0, 33), (0, 64), (0, 600), (0, 3000), (1, 16), (2, 50), (4, 8), (5, 3)])
+def test_adjoint_of_what_is_not_finite(m, lmax, c, dtype):
+    """It stays in its row and degree, and in the channels of gamma whose terms it is in; everything else has the bits that it has without it."""
+    import torch
+    rng = np.random.default_rng(17)
+    shape, l = (40, (lmax + 1) ** 2, c), lmax
+    h, dy, dh = (tensor(rng, shape, dtype) for _ in range(3))
+    g = torch.from_numpy((1 + 0.3 * rng.standard_normal((lmax + 1, c))).astype(np.float32)).cuda()
+    clean, _ = m.egnn_rms_norm_backward(h, dy, g, dh=dh)
+    planes = slice(l * l, (l + 1) ** 2)
+    h[3, l * l, 1], h[11, l * l, c - 1], h[21, l * l, 0] = float("inf"), float("nan"), -float("inf")
+    dy[30, l * l, 2], dh[33, l * l, 1] = float("nan"), float("nan")
+    dx, dgamma = m.egnn_rms_norm_backward(h, dy, g, dh=dh)
+    bad = torch.zeros(shape, dtype=torch.bool, device="cuda")
+    for r in (3, 11, 21, 30):
+        bad[r, planes] = True
+    bad[33, l * l, 1] = True
+    assert torch.isnan(dx[bad]).all() and torch.equal(dx[~bad], clean[~bad])
+    assert torch.isnan(dgamma[l]).all() and torch.isfinite(dgamma[:l]).all()             # (a row with a NaN has none but NaN in its norm)
+    h[11, l * l, c - 1] = 0.5
+    _, dgamma = m.egnn_rms_norm_backward(h, dy, g, dh=dh)
+    where = torch.zeros(c, dtype=torch.bool, device="cuda")
+    where[:3] = True
+    assert torch.isnan(dgamma[l][where]).all() and torch.isfinite(dgamma[l][~where]).all()
