@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 
 from oracle import block_oracle as K, residual_oracle as R
-from tests.residual_util import U32, check_codes, codes, exponents, values
+from tests.residual_util import U32, check_codes, check_gradients, codes, exponents, values
 
 pytestmark = pytest.mark.gpu
 
@@ -166,3 +166,18 @@ def test_the_adjoint_is_that_of_the_last_forward_pass_that_was_kept_for_it():
     stack.forward(x, keep=False)
     with pytest.raises(RuntimeError, match="forward"):
         stack.backward(dout)
+
+
+@pytest.mark.parametrize("lmax,channels,n,n_species", [(1, 32, 40, 2), (2, 16, 30, 3), (0, 64, 50, 2)])
+def test_gradients_against_differences_of_the_loss(lmax, channels, n, n_species):
+    """Directions of random signs against the loss with its roundings to 8 bits held, and along the gradient against the loss without them: a bound that the
+    same gradients negated, without dh, without the norm's adjoint or in another order do not keep."""
+    lib, block, species, x, r, dout, dh = make(lmax, channels, n, n_species, 23)
+    rows = n * lib.dim
+    _, h = block.forward(x, r)
+    dx, grads = block.backward(dout, dh)
+    ptr, perm = K.group_rows(species, n_species, lmax)
+    d64 = values(dout).reshape(rows, channels)
+    case = dict(h=values(h), gamma=values(block.gamma), W=values(block.W), d=d64, dh=values(dh), ptr=ptr, perm=perm,
+                W8=R.values_of_matrices(codes(block.code[0]), exponents(block.code[1])), d8=R.values_of_rows(*R.quantise_rows(d64)[:2]))
+    check_gradients(case, values(dx), values(grads["gamma"]), values(grads["W"]), off=64 * U32)

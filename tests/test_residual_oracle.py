@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from oracle import block_oracle as K, residual_oracle as R
+from tests.residual_util import U32, block_case, check_gradients
 
 
 def test_codes_are_those_of_e4m3():
@@ -76,3 +77,42 @@ def test_clip():
     norm, factor, out = R.clip([np.array([np.inf, 1.0])], 1.0)
     assert factor == 0.0 and out[0][1] == 1.0 and R.clip([np.array([np.nan])], 1.0)[1] == 0.0
     assert R.clip([np.array([2e38, 3e38])], 1.0)[1] == 0.0
+
+
+MISTAKES = {
+    "dx negated": lambda c, dx, dg, dW, dy: (-dx, dg, dW),
+    "dgamma negated": lambda c, dx, dg, dW, dy: (dx, -dg, dW),
+    "dW negated": lambda c, dx, dg, dW, dy: (dx, dg, -dW),
+    "dh left out": lambda c, dx, dg, dW, dy: (dx - c["dh"], dg, dW),
+    "noise for dx": lambda c, dx, dg, dW, dy: (np.random.default_rng(1).standard_normal(dx.shape), dg, dW),
+    "dW transposed": lambda c, dx, dg, dW, dy: (dx, dg, dW.transpose(0, 2, 1)),
+    "dW of another group": lambda c, dx, dg, dW, dy: (dx, dg, dW[::-1]),
+    "dW's entries in another order": lambda c, dx, dg, dW, dy: (dx, dg, np.random.default_rng(2).permutation(dW.ravel()).reshape(dW.shape)),
+    "no adjoint of the norm": lambda c, dx, dg, dW, dy: (dy + c["dh"], dg, dW),
+    "the norm taken for a constant factor": lambda c, dx, dg, dW, dy: (_scaled(c, dy), dg, dW),
+    "one degree's dgamma missing": lambda c, dx, dg, dW, dy: (dx, np.concatenate([dg[:-1], 0 * dg[-1:]]), dW),
+    "dx a sixteenth too long": lambda c, dx, dg, dW, dy: (dx * (1 + 2.0 ** -4), dg, dW),
+}
+
+
+def _scaled(c, dy):
+    """gamma dy / rms + dh: without the term along h."""
+    out = c["dh"].copy()
+    for l in range(len(c["gamma"])):
+        at = slice(l * l, (l + 1) ** 2)
+        out[:, at] += dy[:, at] * c["gamma"][l] / np.sqrt((c["h"][:, at] ** 2).mean((1, 2), keepdims=True) + 1e-5)
+    return out
+
+
+@pytest.mark.parametrize("lmax,channels,n,n_species", [(1, 32, 40, 2), (2, 16, 30, 3), (0, 130, 20, 2)])
+def test_the_check_of_a_block_s_gradients_notices_mistakes(lmax, channels, n, n_species):
+    case, dx, dgamma, dW, dy = block_case(np.random.default_rng(channels), lmax, channels, n, n_species)
+    check_gradients(case, dx, dgamma, dW)
+    rounded = [v.astype(np.float32).astype(np.float64) for v in (dx, dgamma, dW)]
+    check_gradients(case, *rounded, off=64 * U32)
+    for name, mistake in MISTAKES.items():
+        try:
+            check_gradients(case, *mistake(case, dx, dgamma, dW, dy), off=64 * U32)
+        except AssertionError:
+            continue
+        pytest.fail(name)
