@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(SL_WAVES * 64) sl_rows_kernel(SlArgs p, long s
 // while a turn's products run, the next one's operands are read.  One barrier a block: behind it the next block is in LDS, and nobody reads this
 // one's buffer any more, so that the block after the next can be asked for.  (Measured, 8192 x 4096 by 4096 bf16: 115 us, 2,390 TFLOP/s, matrix units 65 %
 // busy; with 64 bytes of a row at a time, four buffers and three turns ahead 152, as L2 has twice the requests; without the order of instructions
-// below 167; eight waves and no reading ahead 146.  With one buffer, three workgroups of 128 x 128 a compute unit: 20,000 x 512 by 1024 in 16 groups 27.)  A row's eight pieces of 16 bytes lie at (piece xor row / 2), so that 16 rows read
+// below 167; eight waves and no reading ahead 146.  With one buffer, three workgroups of 128 x 128 a compute unit: 20,000 x 512 by 1024 in 16 groups of rows in any order 28.)  A row's eight pieces of 16 bytes lie at (piece xor row / 2), so that 16 rows read
 // at once lie in all 64 banks.
 typedef __attribute__((address_space(3))) uint8_t sl_lds;
 typedef const __attribute__((address_space(1))) uint8_t sl_global;
@@ -615,15 +615,16 @@ int sl_few(egnn_ctx* ctx, SlArgs p, hipStream_t st) {
 }
 
 // Which kernel (times in us):
-//   * up to 128 of k and 64 columns: W in registers (300,000 x 64 by 64 fp32 24, tiles 50; 100,000 x 128 by 64 bf16 10 and 12);
+//   * up to 128 of k and 64 columns: W in registers (300,000 x 64 by 64 fp32 in 15 groups of rows in any order 23, tiles 45; 100,000 x 128
+//     by 64 bf16 9.2 and 11.2);
 //   * where 16 columns by the rows of an average group, 64 at most, make no more workgroups than 256 (512 for fp32 and fp16): k over the waves of a workgroup
 //     (128 x 2048 by 1024 bf16, 128 workgroups, 10.7, tiles 13.1; by 4096, 512 of them, 18.5 and 13.3; fp32 21 and 28);
 //   * bf16 tiles of 256, one workgroup per compute unit, where k is 2,048 at least and the last round of 256 of them is full enough that seven in ten places are
 //     used on average (4096 x 4096 by 4096 60, tiles of 128 87; 10,000 rows, 640 tiles, 162 and 184; 5120 rows, 320 tiles, 102 and 93; with 1,024 of k
 //     and 10,000 rows 66 and 57);
-//   * else tiles of 128: bf16 with two buffers as long as there is about one for each compute unit (2048 x 4096 by 2048 33 and, with one buffer, 39), with
-//     one buffer, three workgroups per compute unit, above that (20,000 x 512 by 1024 25.6 and 22.4).  fp32 and fp16 have one buffer always: twice the products
-//     and the sums of a block beside those of all leave no registers for more (20,000 x 512 by 1024 fp32 59 and 52).
+//   * else tiles of 128: bf16 with two buffers as long as there is about one for each compute unit (2048 x 4096 by 2048 32 and, with one buffer, 39), with
+//     one buffer, three workgroups per compute unit, above that (20,000 x 512 by 1024 in one group 25.1 and 21.7, in 16 of rows in any order 33 and 28).  fp32 and fp16 have one buffer always: twice the products
+//     and the sums of a block beside those of all leave no registers for more (20,000 x 512 by 1024 fp32 in one group 45 and 40, in 16 57 and 51).
 template <class T, bool ODD>
 int sl_product(egnn_ctx* ctx, SlArgs p, hipStream_t st) {
   constexpr bool EXACT = !__is_same(T, __bf16);
