@@ -160,7 +160,7 @@ def _blocks(n):
 
 def empty_codes(shape, device="cuda"):
     """(codes [...][n], scales [...][ceil(n / 128)]) for rows of n values: torch.float8_e4m3fn in rows from multiples of 16 bytes on, and
-    torch.float8_e8m0fnu."""
+    torch.float8_e8m0fnu.  Calls that write codes also write zeros behind the last of a row, up to a multiple of 16."""
     *rows, n = shape
     return (torch.empty((*rows, (n + 15) // 16 * 16), dtype=CODES, device=device)[..., :n],
             torch.empty((*rows, _blocks(n)), dtype=SCALES, device=device))
